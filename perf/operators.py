@@ -3,7 +3,7 @@
 tree     attention of a tree of drafted tokens over the paged cache (one pass of one layer)
 rope     rotary encoding of new tokens' queries and keys, keys and values appended to the paged cache
 commit   the accepted path's cached rows moved together behind the committed context
-fork     a sequence's cached prefix handed to another row of the page table: whole pages shared, the last one copied
+fork     a sequence's cached prefix handed to another row of the page table: whole pages shared, the tokens of a last partial one copied
 release  rows forked at a page boundary and dropped again, then the list of the pages that nobody holds
 """
 import math
@@ -342,8 +342,9 @@ def _plain_fork(s):
     s["counts"][new] = torch.where(rest.squeeze(1) > 0, 1, s["counts"][new])
     if s["case"]["op"] == "fork":
         for pool in s["pools"]:
-            pages = pool.view(s["counts"].shape[0], -1)
-            pages[new] = torch.where(rest > 0, pages[partial.clamp(min=0)], pages[new])
+            pages = pool.view(s["counts"].shape[0], -1, PAGE, s["case"]["dim"])
+            held = torch.arange(PAGE, device=src.device)[None, :] < rest                   # the slots that hold a token
+            pages[new] = torch.where(held[:, None, :, None], pages[partial.clamp(min=0)], pages[new])
     return s["pools"], s["table"], s["counts"]
 
 
@@ -404,7 +405,7 @@ def work(case):
     C, P = case["children"], case["parents"]
     pages = (case["len_lo"] + case["len_hi"]) / 2 / PAGE
     if op == "fork":
-        return {"bytes": C * (15 / 16 * 2 * PAGE * row * case["layers"] + 20 + 16 * pages), "flops": 0}
+        return {"bytes": C * (7.5 * 2 * row * case["layers"] + 20 + 16 * pages), "flops": 0}
     total = P * ((case["len_hi"] + PAGE - 1) // PAGE) + C + 5
     return {"bytes": C * pages * 16 + C * 16 + total * 4 + (C + 5) * 4, "flops": 0}
 
@@ -482,10 +483,10 @@ def exact(case, seed):
         return pools, None
     if op == "fork":
         src, lens, new = s["src"].tolist(), s["lens"].tolist(), s["new"].tolist()
-        pools = [p.double().view(s["counts"].shape[0], -1) for p in s["pools"]]
+        pools = [p.double().view(s["counts"].shape[0], -1, PAGE, D) for p in s["pools"]]
         for p in pools:
             for c in range(case["children"]):
                 if lens[c] % PAGE:
-                    p[new[c]] = p[int(table[src[c], lens[c] // PAGE])]
+                    p[new[c], :, :lens[c] % PAGE] = p[int(table[src[c], lens[c] // PAGE]), :, :lens[c] % PAGE]
         return [p.view(-1) for p in pools], None, None
     return None
