@@ -16,9 +16,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libopw_attn.so")
 SOURCES = [os.path.join(_HERE, "csrc", "opw_attn.cu"), os.path.join(_HERE, "csrc", "opw_noalloc.cu"),
-           os.path.join(_HERE, "csrc", "opw_linear_attn.cu"), os.path.join(_HERE, "csrc", "opw_afd.cu")]
+           os.path.join(_HERE, "csrc", "opw_linear_attn.cu"), os.path.join(_HERE, "csrc", "opw_afd.cu"),
+           os.path.join(_HERE, "csrc", "opw_tree_attn.cu"), os.path.join(_HERE, "csrc", "opw_draft.cu"),
+           os.path.join(_HERE, "csrc", "opw_pages.cu")]
 HEADERS = [os.path.join(_HERE, "csrc", "opw_kernels.cuh"), os.path.join(_HERE, "csrc", "opw_afd_gemm.cuh"), os.path.join(_ROOT, "include", "opw_attn.h"),
-           os.path.join(_ROOT, "include", "opw_linear_attn.h"), os.path.join(_ROOT, "include", "opw_afd.h")]
+           os.path.join(_ROOT, "include", "opw_linear_attn.h"), os.path.join(_ROOT, "include", "opw_afd.h"),
+           os.path.join(_ROOT, "include", "opw_draft.h"), os.path.join(_ROOT, "include", "opw_pages.h"),
+           os.path.join(_HERE, "csrc", "opw_stage.h"), os.path.join(_HERE, "csrc", "opw_tree_kernels.cuh")]
 
 OPW_FLAG_NO_PDL = 1
 OPW_FLAG_COPY_STREAMS = 2
@@ -35,6 +39,8 @@ EXPORTS = [
     "opw_attn_stage_shape", "opw_afd_module_workspace_bytes", "opw_afd_module_create", "opw_afd_module_step",
     "opw_afd_module_intermediates", "opw_afd_module_destroy", "opw_afd_module_poll_error",
     "opw_afd_module_launch_count", "opw_afd_module_set_trace", "opw_hbm_read_probe",
+    "opw_rope_table", "opw_rope_append", "opw_tree_mask", "opw_tree_attn_workspace_bytes", "opw_tree_attn_create",
+    "opw_tree_attn_destroy", "opw_tree_attention", "opw_kv_commit", "opw_kv_fork", "opw_kv_release", "opw_kv_free_pages",
 ]
 
 
@@ -97,6 +103,16 @@ class PlanOp(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("attention", StepItem), ("linear", LinearItem), ("afd", AfdItem)]
 
 
+class RopeConfig(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_context", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("amplitude", ctypes.c_double)]
+
+
+OPW_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+OPW_ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
+OPW_TREE_MAX_NODES = 64
 OPW_OP_ATTENTION, OPW_OP_LINEAR, OPW_OP_AFD_MODULE = 0, 1, 2
 OPW_PLAN_GRAPH, OPW_PLAN_ADVANCE, OPW_PLAN_OVERLAP = 1, 2, 4
 OPW_AFD_LIBRARY_GEMM, OPW_AFD_NO_PDL, OPW_AFD_NO_CLUSTER = 1, 2, 4
@@ -203,6 +219,28 @@ def lib() -> ctypes.CDLL:
     L.opw_afd_module_intermediates.argtypes = [vp] + [ctypes.POINTER(vp)] * 4
     L.opw_afd_module_destroy.restype = ctypes.c_int
     L.opw_afd_module_destroy.argtypes = [vp]
+    L.opw_rope_table.restype = ctypes.c_int
+    L.opw_rope_table.argtypes = [ctypes.POINTER(RopeConfig), ctypes.POINTER(ctypes.c_double)]
+    L.opw_rope_append.restype = ctypes.c_int
+    L.opw_rope_append.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]
+    L.opw_tree_mask.restype = ctypes.c_int
+    L.opw_tree_mask.argtypes = [i32, vp, vp, vp]
+    L.opw_tree_attn_workspace_bytes.restype = ctypes.c_size_t
+    L.opw_tree_attn_workspace_bytes.argtypes = [vp, i32]
+    L.opw_tree_attn_create.restype = ctypes.c_int
+    L.opw_tree_attn_create.argtypes = [vp, i32, ctypes.c_uint32, vp, ctypes.c_size_t, ctypes.POINTER(vp)]
+    L.opw_tree_attn_destroy.restype = ctypes.c_int
+    L.opw_tree_attn_destroy.argtypes = [vp]
+    L.opw_tree_attention.restype = ctypes.c_int
+    L.opw_tree_attention.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.opw_kv_commit.restype = ctypes.c_int
+    L.opw_kv_commit.argtypes = [vp, ctypes.POINTER(i32), i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    L.opw_kv_fork.restype = ctypes.c_int
+    L.opw_kv_fork.argtypes = [vp, ctypes.POINTER(i32), i32, i32, vp, vp, vp, vp, i32, vp, vp, vp]
+    L.opw_kv_release.restype = ctypes.c_int
+    L.opw_kv_release.argtypes = [vp, i32, vp, vp, i32, vp, vp, i64, vp]
+    L.opw_kv_free_pages.restype = ctypes.c_int
+    L.opw_kv_free_pages.argtypes = [vp, vp, i64, vp, i64, vp, vp]
     L.opw_attn_stage_launch_count.restype = i64
     L.opw_attn_stage_launch_count.argtypes = [vp]
     L.opw_attn_stage_destroy.restype = ctypes.c_int
@@ -465,6 +503,104 @@ def opw_attn_stage_destroy(stage: Optional[int]) -> None:
     _check(lib().opw_attn_stage_destroy(stage), "opw_attn_stage_destroy")
 
 
+def opw_rope_table(rotary_dim: int, *, theta: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                   original_context: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0):
+    """Turns per position of each pair, then the amplitude: a list of rotary_dim / 2 + 1 floats (64 bits)."""
+    cfg = RopeConfig(ctypes.sizeof(RopeConfig), rotary_dim, OPW_ROPE_SCALINGS[scaling], 0, theta, factor, original_context, low, high,
+                     amplitude)
+    out = (ctypes.c_double * (max(rotary_dim, 0) // 2 + 1))()
+    _check(lib().opw_rope_table(ctypes.byref(cfg), out), "opw_rope_table")
+    return list(out)
+
+
+def opw_rope_append(stage: int, layer: int, rows: int, rotary_dim: int, layout: int, table: int, q: Optional[int], q_stride: int,
+                    k: int, k_stride: int, v: int, v_stride: int, seq: int, slots: int, positions: int, page_table: int,
+                    q_out: Optional[int], stream: Optional[int] = None) -> None:
+    _check(lib().opw_rope_append(stage, layer, rows, rotary_dim, layout, table, q, q_stride, k, k_stride, v, v_stride, seq, slots,
+                                 positions, page_table, q_out, stream), "opw_rope_append")
+
+
+def opw_tree_mask(parents: Sequence[int]):
+    """(mask words, depths) of a tree given by each node's parent (-1: the committed context)."""
+    n = len(parents)
+    par, mask, depth = (ctypes.c_int32 * n)(*parents), (ctypes.c_uint64 * n)(), (ctypes.c_int32 * n)()
+    _check(lib().opw_tree_mask(n, par, mask, depth), "opw_tree_mask")
+    return list(mask), list(depth)
+
+
+def opw_tree_attn_workspace_bytes(stage: int, max_nodes: int) -> int:
+    return int(lib().opw_tree_attn_workspace_bytes(stage, max_nodes))
+
+
+def opw_tree_attn_create(stage: int, max_nodes: int, workspace: int, workspace_bytes: int, flags: int = 0) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().opw_tree_attn_create(stage, max_nodes, flags, workspace, workspace_bytes, ctypes.byref(h)), "opw_tree_attn_create")
+    return h.value
+
+
+def opw_tree_attn_destroy(tree: Optional[int]) -> None:
+    _check(lib().opw_tree_attn_destroy(tree), "opw_tree_attn_destroy")
+
+
+def opw_tree_attention(tree: int, layer: int, batch: int, nodes: int, q: int, tree_mask: int, positions: int, ctx_lens: int,
+                       tree_lens: int, page_table: int, out: int, lse: Optional[int] = None, stream: Optional[int] = None) -> None:
+    _check(lib().opw_tree_attention(tree, layer, batch, nodes, q, tree_mask, positions, ctx_lens, tree_lens, page_table, out, lse,
+                                    stream), "opw_tree_attention")
+
+
+def _layer_array(layers: Sequence[int]):
+    return (ctypes.c_int32 * len(layers))(*layers)
+
+
+def opw_kv_commit(stage: int, layers: Sequence[int], batch: int, nodes: int, accepted: int, accepted_lens: int, ctx_lens: int,
+                  page_table: int, new_lens: Optional[int] = None, stream: Optional[int] = None) -> None:
+    _check(lib().opw_kv_commit(stage, _layer_array(layers), len(layers), batch, nodes, accepted, accepted_lens, ctx_lens, page_table,
+                               new_lens, stream), "opw_kv_commit")
+
+
+def opw_kv_fork(stage: int, layers: Sequence[int], n: int, src_rows: int, dst_rows: int, lens: int, new_pages: int, num_rows: int,
+                page_table: int, refcounts: int, stream: Optional[int] = None) -> None:
+    _check(lib().opw_kv_fork(stage, _layer_array(layers), len(layers), n, src_rows, dst_rows, lens, new_pages, num_rows, page_table,
+                             refcounts, stream), "opw_kv_fork")
+
+
+def opw_kv_release(stage: int, n: int, rows: int, keep_lens: Optional[int], num_rows: int, page_table: int, refcounts: int,
+                   num_pages: int, stream: Optional[int] = None) -> None:
+    _check(lib().opw_kv_release(stage, n, rows, keep_lens, num_rows, page_table, refcounts, num_pages, stream), "opw_kv_release")
+
+
+def opw_kv_free_pages(stage: int, refcounts: int, num_pages: int, free_list: Optional[int], max_list: int, count: int,
+                      stream: Optional[int] = None) -> None:
+    _check(lib().opw_kv_free_pages(stage, refcounts, num_pages, free_list, max_list, count, stream), "opw_kv_free_pages")
+
+
+def _need(where: str, device, dtype, *tensors) -> None:
+    """The kernels see addresses only: a tensor of another type, device or memory order would be read wrongly."""
+    for t in tensors:
+        if t.dtype is not dtype or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{where}: expected contiguous {dtype} tensors on {device}, got {t.dtype} on {t.device}"
+                             f"{'' if t.is_contiguous() else ' (not contiguous)'}")
+
+
+def _shapes(where: str, *pairs) -> None:
+    for t, shape in pairs:
+        if t.shape != shape:
+            raise ValueError(f"{where}: expected a tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+class Rope:
+    """A rotary encoding: its parameters and their table on the device (see opw_rope_table)."""
+
+    def __init__(self, rotary_dim: int, *, layout: str = "half", theta: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                 original_context: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0, device="cuda"):
+        import torch
+
+        self.rotary_dim, self.layout = rotary_dim, OPW_ROPE_LAYOUTS[layout]
+        self.table = torch.tensor(opw_rope_table(rotary_dim, theta=theta, scaling=scaling, factor=factor,
+                                                 original_context=original_context, low=low, high=high, amplitude=amplitude),
+                                  dtype=torch.float64, device=device)
+
+
 class Stage:
     """Convenience owner of one stage handle over caller-provided torch tensors.
 
@@ -499,6 +635,7 @@ class Stage:
         cfg.workspace = base
         cfg.workspace_bytes = nbytes
         self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
+        self.max_pages_per_seq = max_pages_per_seq
         self.handle = opw_attn_stage_create(cfg)
 
     @staticmethod
@@ -542,6 +679,91 @@ class Stage:
         opw_attn_stage_set_trace(self.handle, self.trace.data_ptr(), self.trace.numel() * 8)
         return self.trace
 
+    def _own_stream(self):
+        """The current stream of the stage's device, whichever device is current."""
+        import torch
+
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _table_ok(self, where, page_table, rows):
+        import torch
+
+        _need(where, self.device, torch.int32, page_table)
+        if page_table.dim() != 2 or page_table.shape[0] < rows or page_table.shape[1] != self.max_pages_per_seq:
+            raise ValueError(f"{where}: page_table must be [at least {rows}, {self.max_pages_per_seq}]")
+
+    def rope_append(self, layer, rope, q, k, v, seq, slots, positions, page_table, q_out):
+        """Rotate q into q_out, append rotated k and v to the cache; q, k, v: [rows, heads, head_dim], rows may be strided
+        (views into one projection).  q = q_out = None: keys and values only."""
+        import torch
+
+        where, D, rows = "rope_append", self.head_dim, seq.shape[0]
+        _need(where, self.device, torch.int32, seq, slots, positions)
+        _shapes(where, (slots, seq.shape), (positions, seq.shape), (k, (rows, self.num_kv_heads, D)), (v, (rows, self.num_kv_heads, D)))
+        self._table_ok(where, page_table, 1)
+        for t in (k, v) if q is None else (q, k, v):
+            if t.dtype is not torch.bfloat16 or t.device != self.device or t.stride(2) != 1 or t.stride(1) != D:
+                raise ValueError(f"{where}: q, k, v must be bfloat16 on {self.device} with contiguous heads")
+        if q is not None:
+            _need(where, self.device, torch.bfloat16, q_out)
+            _shapes(where, (q, (rows, self.num_q_heads, D)), (q_out, q.shape))
+        if rope.table.device != self.device:
+            raise ValueError(f"{where}: the rotary table is on {rope.table.device}")
+        opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(),
+                        None if q is None else q.data_ptr(), 0 if q is None else q.stride(0), k.data_ptr(), k.stride(0),
+                        v.data_ptr(), v.stride(0), seq.data_ptr(), slots.data_ptr(), positions.data_ptr(), page_table.data_ptr(),
+                        None if q is None else q_out.data_ptr(), self._own_stream())
+
+    def kv_commit(self, layers, accepted, accepted_lens, ctx_lens, page_table, new_lens=None):
+        """Move the rows of the accepted nodes together behind each sequence's context, in all of `layers`."""
+        import torch
+
+        where, batch = "kv_commit", ctx_lens.shape[0]
+        _need(where, self.device, torch.int32, accepted, accepted_lens, ctx_lens)
+        _shapes(where, (accepted_lens, ctx_lens.shape), (accepted, (batch, accepted.shape[1])))
+        self._table_ok(where, page_table, batch)
+        if new_lens is not None:
+            _need(where, self.device, torch.int32, new_lens)
+            _shapes(where, (new_lens, ctx_lens.shape))
+        opw_kv_commit(self.handle, layers, batch, accepted.shape[1], accepted.data_ptr(), accepted_lens.data_ptr(),
+                      ctx_lens.data_ptr(), page_table.data_ptr(), None if new_lens is None else new_lens.data_ptr(),
+                      self._own_stream())
+
+    def kv_fork(self, layers, src_rows, dst_rows, lens, new_pages, page_table, refcounts):
+        """Let table rows dst_rows share the first lens tokens of src_rows; a last partial page is copied to new_pages."""
+        import torch
+
+        where, n = "kv_fork", src_rows.shape[0]
+        _need(where, self.device, torch.int32, src_rows, dst_rows, lens, new_pages, refcounts)
+        _shapes(where, (dst_rows, (n,)), (lens, (n,)), (new_pages, (n,)))
+        self._table_ok(where, page_table, 1)
+        page = self.num_kv_heads * 2 * 16 * self.head_dim
+        if refcounts.numel() < min(self.pools[i].numel() // page for i in layers):
+            raise ValueError(f"{where}: refcounts must have an entry per page")
+        opw_kv_fork(self.handle, layers, n, src_rows.data_ptr(), dst_rows.data_ptr(), lens.data_ptr(), new_pages.data_ptr(),
+                    page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(), self._own_stream())
+
+    def kv_release(self, rows, keep_lens, page_table, refcounts):
+        """Drop the pages of table rows behind their first keep_lens tokens (None: all)."""
+        import torch
+
+        where = "kv_release"
+        _need(where, self.device, torch.int32, rows, refcounts)
+        self._table_ok(where, page_table, 1)
+        if keep_lens is not None:
+            _need(where, self.device, torch.int32, keep_lens)
+            _shapes(where, (keep_lens, rows.shape))
+        opw_kv_release(self.handle, rows.shape[0], rows.data_ptr(), None if keep_lens is None else keep_lens.data_ptr(),
+                       page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(), refcounts.numel(), self._own_stream())
+
+    def kv_free_pages(self, refcounts, free_list, count):
+        """List the pages nobody holds, ascending, in free_list; their number in count."""
+        import torch
+
+        _need("kv_free_pages", self.device, torch.int32, refcounts, free_list, count)
+        opw_kv_free_pages(self.handle, refcounts.data_ptr(), refcounts.numel(), free_list.data_ptr(), free_list.numel(),
+                          count.data_ptr(), self._own_stream())
+
     def packed_host_buffers(self, batch):
         """One pinned host buffer holding q, k_new, v_new, positions at the packed offsets;
         returns (buffer, q, k_new, v_new, positions) -- the last four are views into it."""
@@ -565,6 +787,52 @@ class Stage:
     def close(self):
         if getattr(self, "handle", None):
             opw_attn_stage_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class TreeAttention:
+    """Owner of one tree-attention handle of a stage and of its workspace.  Calls of one handle must not overlap."""
+
+    def __init__(self, stage: Stage, max_nodes: int = OPW_TREE_MAX_NODES):
+        import torch
+
+        self.stage, self.max_nodes = stage, max_nodes
+        nbytes = opw_tree_attn_workspace_bytes(stage.handle, max_nodes)
+        if nbytes == 0:
+            raise OpwError(OPW_ERR_INVALID_ARG, "opw_tree_attn_workspace_bytes")
+        self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=stage.device)
+        base = (self.workspace.data_ptr() + 255) // 256 * 256
+        self.handle = opw_tree_attn_create(stage.handle, max_nodes, base, nbytes)
+
+    def attention(self, layer, q, tree_mask, positions, ctx_lens, tree_lens, page_table, out, lse=None):
+        """q, out: bf16 [batch, nodes, Hq, D]; tree_mask: int64 [batch, nodes] (the bits of a uint64); positions: int32
+        [batch, nodes]; lse: fp32 [batch, nodes, Hq] or None."""
+        import torch
+
+        where, st = "tree attention", self.stage
+        batch, nodes = q.shape[0], q.shape[1]
+        _need(where, st.device, torch.bfloat16, q, out)
+        _need(where, st.device, torch.int32, positions, ctx_lens, tree_lens)
+        _need(where, st.device, torch.int64, tree_mask)
+        _shapes(where, (q, (batch, nodes, st.num_q_heads, st.head_dim)), (out, q.shape), (tree_mask, (batch, nodes)),
+                (positions, (batch, nodes)), (ctx_lens, (batch,)), (tree_lens, (batch,)))
+        st._table_ok(where, page_table, batch)
+        if lse is not None:
+            _need(where, st.device, torch.float32, lse)
+            _shapes(where, (lse, (batch, nodes, st.num_q_heads)))
+        opw_tree_attention(self.handle, layer, batch, nodes, q.data_ptr(), tree_mask.data_ptr(), positions.data_ptr(),
+                           ctx_lens.data_ptr(), tree_lens.data_ptr(), page_table.data_ptr(), out.data_ptr(),
+                           None if lse is None else lse.data_ptr(), st._own_stream())
+
+    def close(self):
+        if getattr(self, "handle", None):
+            opw_tree_attn_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

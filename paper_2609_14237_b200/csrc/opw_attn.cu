@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "opw_kernels.cuh"
+#include "opw_stage.h"
 
 namespace {
 
@@ -161,6 +162,26 @@ struct opw_attn_stage {
   cudaStream_t s_in, s_out;
   cudaEvent_t e_in, e_k, e_out;
 };
+
+opw_stage_view opw_view_of(opw_attn_stage_t* st) {
+  opw_stage_view v;
+  v.device = st->cfg.device;
+  v.num_layers = st->cfg.num_layers;
+  v.Hq = st->cfg.num_q_heads;
+  v.Hkv = st->cfg.num_kv_heads;
+  v.D = st->cfg.head_dim;
+  v.max_batch = st->cfg.max_batch;
+  v.max_pages = st->cfg.max_pages_per_seq;
+  v.sms = st->sms;
+  v.window = st->window.data();
+  v.num_pages = st->num_pages.data();
+  v.pool = st->pool.data();
+  v.status = reinterpret_cast<uint32_t*>(st->ws + st->lay.status);
+  v.launches = &st->launches;
+  v.scale_log2e = st->scale_log2e;
+  v.pdl = (st->cfg.flags & OPW_FLAG_NO_PDL) == 0;
+  return v;
+}
 
 extern "C" {
 

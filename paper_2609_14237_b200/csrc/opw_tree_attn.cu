@@ -1,0 +1,176 @@
+// Host side of tree attention (include/opw_draft.h): argument checks, choice of kernel, launches.
+#include <cstdint>
+#include <new>
+
+#include "opw_draft.h"
+#include "opw_stage.h"
+#include "opw_tree_kernels.cuh"
+
+namespace {
+
+constexpr size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+struct TreeLayout {
+  size_t cum, partials, total;
+};
+
+struct Variant {              // a kernel, and how it cuts rows and keys
+  int row_block, keys, workers;
+};
+
+Variant pick(const opw_stage_view& v, int nodes) {
+  const int rows = nodes * (v.Hq / v.Hkv);
+  Variant k;
+  k.keys = 16;
+  k.row_block = rows <= 16 || v.D == 256 ? 16 : 32;
+  k.workers = v.sms * (v.D == 64 ? 12 : v.D == 128 ? 8 : 6);
+  return k;
+}
+
+TreeLayout carve(const opw_stage_view& v, int max_nodes) {
+  TreeLayout L;
+  L.cum = 0;
+  L.partials = align_up((size_t)(opw_tree::kMaxTreeBatch + 1) * 8);
+  size_t most = 0;            // over every number of nodes a call may have
+  for (int n = 1; n <= max_nodes; ++n) {
+    const Variant k = pick(v, n);
+    const size_t need = (size_t)k.workers * 2 * k.row_block * (v.D + 2) * 4;
+    if (need > most) most = need;
+  }
+  L.total = L.partials + align_up(most);
+  return L;
+}
+
+template <int D, int MT>
+cudaError_t raise_smem() {
+  return cudaFuncSetAttribute(opw_tree::tree_warp_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)opw_tree::WarpTree<D, MT>::smem(opw_tree::kMaxTreeBatch));
+}
+
+template <int D, int MT>
+cudaError_t launch_warp(const opw_stage_view& v, const opw_tree::TreeParams& p, cudaStream_t stream) {
+  using C = opw_tree::WarpTree<D, MT>;
+  return opw_launch(opw_tree::tree_warp_kernel<D, MT>, dim3(v.sms), dim3(C::kWarps * 32), C::smem(p.batch), stream, v.pdl, 1, p);
+}
+
+}  // namespace
+
+struct opw_tree_attn {
+  opw_attn_stage_t* stage;
+  int32_t max_nodes;
+  TreeLayout lay;
+  unsigned char* ws;
+};
+
+extern "C" opw_status_t opw_tree_mask(int32_t nodes, const int32_t* parents, uint64_t* mask, int32_t* depth) {
+  if (nodes < 1 || nodes > OPW_TREE_MAX_NODES || !parents || !mask) return OPW_ERR_INVALID_ARG;
+  for (int i = 0; i < nodes; ++i)
+    if (parents[i] < -1 || parents[i] >= i) return OPW_ERR_INVALID_ARG;
+  for (int i = 0; i < nodes; ++i) {
+    const int up = parents[i];
+    mask[i] = (up >= 0 ? mask[up] : 0ull) | 1ull << i;
+    if (depth) depth[i] = up >= 0 ? depth[up] + 1 : 0;
+  }
+  return OPW_OK;
+}
+
+extern "C" size_t opw_tree_attn_workspace_bytes(const opw_attn_stage_t* stage, int32_t max_nodes) {
+  if (!stage || max_nodes < 1 || max_nodes > OPW_TREE_MAX_NODES) return 0;
+  return carve(opw_view_of(const_cast<opw_attn_stage_t*>(stage)), max_nodes).total;
+}
+
+extern "C" opw_status_t opw_tree_attn_create(opw_attn_stage_t* stage, int32_t max_nodes, uint32_t flags, void* workspace,
+                                             size_t workspace_bytes, opw_tree_attn_t** out) {
+  if (!stage || !out || !workspace || flags != 0) return OPW_ERR_INVALID_ARG;
+  if (max_nodes < 1 || max_nodes > OPW_TREE_MAX_NODES || (uintptr_t)workspace % 256) return OPW_ERR_INVALID_ARG;
+  const opw_stage_view v = opw_view_of(stage);
+  const TreeLayout lay = carve(v, max_nodes);
+  if (workspace_bytes < lay.total) return OPW_ERR_CAPACITY;
+  opw_device_guard guard(v.device);
+  if (!guard.ok()) return OPW_ERR_CUDA;
+  cudaError_t e;
+  if (v.D == 64) {
+    e = raise_smem<64, 1>();
+    if (e == cudaSuccess) e = raise_smem<64, 2>();
+  } else if (v.D == 128) {
+    e = raise_smem<128, 1>();
+    if (e == cudaSuccess) e = raise_smem<128, 2>();
+  } else {
+    e = raise_smem<256, 1>();
+  }
+  if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
+  opw_tree_attn* t = new (std::nothrow) opw_tree_attn();
+  if (!t) return OPW_ERR_INVALID_ARG;
+  t->stage = stage;
+  t->max_nodes = max_nodes;
+  t->lay = lay;
+  t->ws = static_cast<unsigned char*>(workspace);
+  *out = t;
+  return OPW_OK;
+}
+
+extern "C" opw_status_t opw_tree_attn_destroy(opw_tree_attn_t* tree) {
+  delete tree;
+  return OPW_OK;
+}
+
+extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer, int32_t batch, int32_t nodes, const void* q,
+                                           const uint64_t* tree_mask, const int32_t* positions, const int32_t* ctx_lens,
+                                           const int32_t* tree_lens, const int32_t* page_table, void* out, float* lse,
+                                           void* cuda_stream) {
+  if (!tree || batch < 0 || nodes < 1) return OPW_ERR_INVALID_ARG;
+  const opw_stage_view v = opw_view_of(tree->stage);
+  if (layer < 0 || layer >= v.num_layers) return OPW_ERR_INVALID_ARG;
+  if (!q || !tree_mask || !positions || !ctx_lens || !tree_lens || !page_table || !out) return OPW_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)tree_mask % 8 ||
+      ((uintptr_t)positions | (uintptr_t)ctx_lens | (uintptr_t)tree_lens | (uintptr_t)page_table | (uintptr_t)lse) % 4)
+    return OPW_ERR_INVALID_ARG;
+  if (nodes > tree->max_nodes || batch > v.max_batch || batch > opw_tree::kMaxTreeBatch) return OPW_ERR_CAPACITY;
+  const size_t bytes = (size_t)batch * nodes * v.Hq * v.D * 2;
+  if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return OPW_ERR_INVALID_ARG;
+  if (batch == 0) return OPW_OK;
+  const Variant k = pick(v, nodes);
+  opw_tree::TreeCombineParams c;
+  opw_tree::TreeParams& p = c.t;
+  p.pool = static_cast<const __nv_bfloat16*>(v.pool[layer]);
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.mask = tree_mask;
+  p.positions = positions;
+  p.ctx_lens = ctx_lens;
+  p.tree_lens = tree_lens;
+  p.page_table = page_table;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.lse = lse;
+  p.partials = reinterpret_cast<float*>(tree->ws + tree->lay.partials);
+  p.cum = reinterpret_cast<int64_t*>(tree->ws + tree->lay.cum);
+  p.status = v.status;
+  p.num_pages = v.num_pages[layer];
+  p.batch = batch;
+  p.nodes = nodes;
+  p.Hq = v.Hq;
+  p.Hkv = v.Hkv;
+  p.G = v.Hq / v.Hkv;
+  p.max_pages = v.max_pages;
+  p.window = v.window[layer];
+  p.scale_log2e = v.scale_log2e;
+  c.D = v.D;
+  c.row_block = k.row_block;
+  c.keys = k.keys;
+  c.max_blocks = (nodes * p.G + k.row_block - 1) / k.row_block;
+  c.workers = k.workers;
+  opw_device_guard guard(v.device);
+  if (!guard.ok()) return OPW_ERR_CUDA;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (v.D == 64) e = k.row_block == 16 ? launch_warp<64, 1>(v, p, stream) : launch_warp<64, 2>(v, p, stream);
+  else if (v.D == 128) e = k.row_block == 16 ? launch_warp<128, 1>(v, p, stream) : launch_warp<128, 2>(v, p, stream);
+  else e = launch_warp<256, 1>(v, p, stream);
+  if (e == cudaSuccess) {
+    *v.launches += 1;
+    e = opw_launch(opw_tree::tree_combine_kernel, dim3((unsigned)batch * v.Hkv * c.max_blocks, v.D / opw_tree::kTreeCombineCols),
+                   dim3(opw_tree::kTreeCombineThreads), 0, stream, v.pdl, 1, c);
+  }
+  if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
+  *v.launches += 1;
+  return OPW_OK;
+}

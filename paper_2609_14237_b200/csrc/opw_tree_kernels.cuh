@@ -1,0 +1,571 @@
+// Device code of tree attention (include/opw_draft.h): the queries of a sequence's drafted tokens, nodes x G rows per kv head,
+// over the paged cache.  sm_100a only.
+//
+// Row r of (sequence b, kv head g) is node r / G with query head g * G + r % G.  Rows are taken in blocks, and a
+// "unit" is one (b, g, row block, key tile); units are ordered that way and the U units of a launch are cut into equal
+// contiguous shares, one per worker.  A share meets at most two row blocks that it does not cover completely, its first
+// and its last; those leave (unnormalised O, maximum, sum) in the worker's two partial slots and are merged by
+// tree_combine_kernel, the others are finished on the spot.  Shares follow from the lengths alone: deterministic.
+//
+// A key is hidden from a row by the window (position), by the row's mask word (drafted keys) or by the end of the sequence.
+// Only tiles that hold such a key take the masked path.  There a hidden score becomes -inf, so that whatever the
+// key row holds has no effect; and since 0 * NaN is NaN in the product with V, cached values that are not finite are
+// taken out of the tile and added, by plain arithmetic, to the rows that do see them.
+#pragma once
+
+#define OPW_NAMESPACE opw_tree
+#include "opw_kernels.cuh"
+
+namespace opw_tree {
+
+constexpr int kMaxTreeBatch = 4096;
+
+struct TreeParams {
+  const __nv_bfloat16* pool;
+  const __nv_bfloat16* q;
+  const uint64_t* mask;
+  const int32_t* positions;
+  const int32_t* ctx_lens;
+  const int32_t* tree_lens;
+  const int32_t* page_table;
+  __nv_bfloat16* out;
+  float* lse;
+  float* partials;       // [workers * 2][row_block * (D + 2)]: O rows, then maxima, then sums
+  int64_t* cum;          // [batch + 1] units before sequence b (written by block 0 for the combine)
+  uint32_t* status;
+  int64_t num_pages;
+  int32_t batch, nodes, Hq, Hkv, G, max_pages, window;
+  float scale_log2e;
+};
+
+// What of sequence b takes part: context length, tree size, first key that any node can see, end, row blocks.
+struct Span {
+  int32_t ctx, tree, lo, n, blocks;
+  bool cut;              // the lengths did not fit the table or the call: recorded as OPW_ERR_BAD_PAGE
+};
+__device__ __forceinline__ Span span_of(const TreeParams& p, int b, int row_block) {
+  Span s;
+  s.ctx = p.ctx_lens[b];
+  s.tree = p.tree_lens[b];
+  s.cut = false;
+  if (s.ctx < 0 || s.tree <= 0) { s.ctx = s.tree = s.lo = s.n = s.blocks = 0; return s; }
+  if (s.tree > p.nodes) { s.tree = p.nodes; s.cut = true; }
+  int64_t n = (int64_t)s.ctx + s.tree;
+  const int64_t cap = (int64_t)p.max_pages * kPage;
+  if (n > cap) { n = cap; s.cut = true; }
+  s.n = (int32_t)n;
+  s.lo = (p.window > 0 && s.ctx >= p.window) ? s.ctx - p.window + 1 : 0;
+  if (s.lo > s.n) s.lo = s.n;
+  s.blocks = (s.tree * p.G + row_block - 1) / row_block;
+  return s;
+}
+// key tiles of `keys` keys (a multiple of the page) that cover [lo, n), counted from lo's page
+__device__ __forceinline__ int32_t tiles_of(const Span& s, int keys) {
+  if (s.n <= s.lo) return 0;
+  const int32_t first = s.lo / kPage * kPage;
+  return (s.n - first + keys - 1) / keys;
+}
+
+// Units before each sequence, for the whole block: cum[0..batch] in shared memory.  Also records cut lengths (block 0).
+__device__ __forceinline__ void scan_units(const TreeParams& p, int64_t* cum, int row_block, int keys) {
+  __shared__ int64_t wsum[32];
+  __shared__ int64_t carry;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) carry = 0;
+  __syncthreads();
+  for (int base = 0; base < p.batch; base += blockDim.x) {
+    const int b = base + threadIdx.x;
+    int64_t cnt = 0;
+    if (b < p.batch) {
+      const Span s = span_of(p, b, row_block);
+      if (s.cut && blockIdx.x == 0) atomicOr(p.status, kErrBadPage);
+      cnt = (int64_t)tiles_of(s, keys) * s.blocks * p.Hkv;
+    }
+    int64_t incl = cnt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 31) wsum[warp] = incl;
+    __syncthreads();
+    int64_t before = carry;
+    for (int w = 0; w < warp; ++w) before += wsum[w];
+    if (b < p.batch) cum[b] = before + incl - cnt;
+    __syncthreads();
+    if (threadIdx.x == blockDim.x - 1) carry = before + incl;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) cum[p.batch] = carry;
+  __syncthreads();
+}
+// the sequence that holds unit u < cum[batch]
+__device__ __forceinline__ int find_sequence(const int64_t* cum, int batch, int64_t u) {
+  int lo = 0, hi = batch;                    // cum[lo] <= u < cum[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (cum[mid] <= u) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Which keys row r sees, apart from the end of the sequence.
+struct RowView {
+  uint64_t bits;         // drafted keys, those outside the window taken out
+  int32_t lo;            // first context key
+};
+__device__ __forceinline__ RowView row_view(const TreeParams& p, int b, const Span& s, int node) {
+  RowView v;
+  v.bits = p.mask[(int64_t)b * p.nodes + node];
+  v.lo = 0;
+  if (s.tree < 64) v.bits &= (1ull << s.tree) - 1ull;
+  if (p.window > 0) {
+    const int32_t* pos = p.positions + (int64_t)b * p.nodes;
+    const int32_t own = pos[node] > s.ctx ? pos[node] : s.ctx;
+    v.lo = own - p.window + 1;               // may be negative
+    for (int m = 0; m < s.tree; ++m) {
+      const int32_t at = pos[m] > s.ctx ? pos[m] : s.ctx;
+      if (at < v.lo) v.bits &= ~(1ull << m);
+    }
+  }
+  return v;
+}
+// The first context key that the window hides from no node (a whole warp asks).
+__device__ __forceinline__ int32_t window_border(const TreeParams& p, int b, const Span& s, int lane) {
+  if (p.window == 0) return 0;
+  int32_t border = s.lo;
+  const int32_t* pos = p.positions + (int64_t)b * p.nodes;
+  for (int i = lane; i < s.tree; i += 32) border = max(border, pos[i] - p.window + 1);
+  return __reduce_max_sync(0xffffffffu, border);
+}
+__device__ __forceinline__ bool sees(const RowView& v, int32_t ctx, int32_t key) {
+  if (key < ctx) return key >= v.lo;
+  const uint32_t m = (uint32_t)(key - ctx);
+  return m < 64u && ((v.bits >> m) & 1ull);
+}
+__device__ __forceinline__ bool any_not_finite(const uint4& w) {   // of eight bf16
+  auto bad = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
+  return bad(w.x) || bad(w.y) || bad(w.z) || bad(w.w);
+}
+__device__ __forceinline__ float bf16_at(uint32_t addr) {
+  uint16_t h;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(addr));
+  return __uint_as_float((uint32_t)h << 16);
+}
+
+// ---------------------------------------------------------------------------------
+// few rows: every warp streams its own units, as the stage's decode kernel does
+// ---------------------------------------------------------------------------------
+// A unit is one page; a row block is MT * 16 rows, the accumulators of MT matrix tiles in registers.  While the rows of
+// one (b, g) fit the block the cache is read once and HBM bounds the kernel.
+template <int D, int MT>
+struct WarpTree {
+  static constexpr int kTile = 2 * kPage * D * 2;
+  static constexpr int kRows = 16 * MT;
+  static constexpr int kWarps = D == 64 ? 12 : D == 128 ? 8 : 6;
+  static constexpr int kStages = 2;
+  static size_t smem(int batch) {
+    return (size_t)kWarps * kStages * kTile + (size_t)kWarps * kStages * 8 + (size_t)(batch + 1) * 8;
+  }
+};
+
+template <int D, int MT>
+__global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_kernel(TreeParams p) {
+  using C = WarpTree<D, MT>;
+  constexpr int KS = D / 16, NT = D / 8, ROWB = D * 2, TILE = C::kTile;
+  constexpr uint32_t kFirst = 1u << 28, kLast = 1u << 29, kBad = 1u << 30, kPageBits = kFirst - 1;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int warps = C::kWarps, stages = C::kStages;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)warps * stages * TILE);
+  int64_t* cum = reinterpret_cast<int64_t*>(bars + warps * stages);
+
+  scan_units(p, cum, C::kRows, kPage);
+  const int64_t U = cum[p.batch];
+  const int64_t workers = (int64_t)gridDim.x * warps, worker = (int64_t)blockIdx.x * warps + warp;
+  const uint32_t ring = smem_u32(smem + (size_t)warp * stages * TILE);
+  const uint32_t bar0 = smem_u32(bars + warp * stages);
+  if (lane == 0) {
+    for (int s = 0; s < stages; ++s) mbar_init(bar0 + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  }
+  __syncwarp();
+
+  const int64_t u0 = worker_begin(U, worker, workers), u1 = worker_begin(U, worker + 1, workers);
+  struct Desc { int32_t tile; uint32_t page; };
+  auto describe = [&](int64_t u) -> Desc {
+    Desc d = {0, 0u};
+    if (u >= u1) return d;
+    const int b = find_sequence(cum, p.batch, u);
+    const Span s = span_of(p, b, C::kRows);
+    const int32_t cnt = tiles_of(s, kPage);
+    const int64_t rem = u - cum[b];
+    const int32_t ri = (int32_t)(rem / cnt), i = (int32_t)(rem - (int64_t)ri * cnt), g = ri / s.blocks;
+    const int32_t lp = s.lo / kPage + i;
+    int64_t pid = p.page_table[(int64_t)b * p.max_pages + lp];
+    d.page = (uint32_t)lp | (i == 0 ? kFirst : 0u) | (i == cnt - 1 ? kLast : 0u);
+    if (pid < 0 || pid >= p.num_pages) {      // never dereference a bad page: mask it out
+      atomicOr(p.status, kErrBadPage);
+      pid = 0;
+      d.page |= kBad;
+    }
+    d.tile = (int32_t)(pid * p.Hkv + g);
+    return d;
+  };
+  int64_t wbase = u0;
+  Desc wa = describe(u0 + lane), wb = describe(u0 + 32 + lane);
+  pdl_wait();                                 // up to here only this step's lengths and the page table were read
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i <= p.batch; i += blockDim.x) p.cum[i] = cum[i];
+
+  const uint64_t policy = l2_evict_first_policy();
+  auto issue = [&](int64_t u, int slot) {
+    const int rel = (int)(u - wbase);
+    const int32_t a = __shfl_sync(0xffffffffu, wa.tile, rel & 31), b = __shfl_sync(0xffffffffu, wb.tile, rel & 31);
+    if (lane == 0) {
+      const uint32_t bar = bar0 + 8 * slot;
+      mbar_expect_tx(bar, TILE);
+      bulk_load(ring + slot * TILE, reinterpret_cast<const unsigned char*>(p.pool) + (int64_t)(rel < 32 ? a : b) * TILE, TILE, bar,
+                policy);
+    }
+  };
+  int inflight = 0;
+  for (int s = 0; s < stages && u0 + s < u1; ++s) { issue(u0 + s, s); ++inflight; }
+
+  const int mi = lane >> 3, rr = lane & 7, qrow = lane >> 2, qcol = (lane & 3) * 2;
+  const uint32_t k_off = (uint32_t)((rr + 8 * (mi >> 1)) * ROWB), v_off = (uint32_t)(kPage * ROWB + (rr + 8 * (mi & 1)) * ROWB);
+  uint32_t qa[MT][KS][4];
+  float o[MT][NT][4], mx[MT][2], l[MT][2];
+  int b = 0, g = 0, rb = 0, rows = 0;
+  int32_t border = 0;
+  Span sp = {0, 0, 0, 0, 1, false};
+  bool from_first = false, on_first_row = true, failed = false;
+  int slot = 0;
+  uint32_t phase = 0;
+
+  for (int64_t u = u0; u < u1; ++u) {
+    if (u - wbase == 32) {
+      wbase += 32;
+      wa = wb;
+      wb = describe(wbase + 32 + lane);
+    }
+    const uint32_t page = __shfl_sync(0xffffffffu, wa.page, (int)(u - wbase));
+    const bool last = page & kLast;
+    if (u == u0 || (page & kFirst)) {         // a new row block: its queries, an empty state
+      from_first = page & kFirst;
+      b = find_sequence(cum, p.batch, u);
+      sp = span_of(p, b, C::kRows);
+      const int32_t ri = (int32_t)((u - cum[b]) / tiles_of(sp, kPage));
+      g = ri / sp.blocks;
+      rb = ri - g * sp.blocks;
+      rows = sp.tree * p.G - rb * C::kRows;   // of this block; may exceed it
+      border = window_border(p, b, sp, lane);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = mt * 16 + h * 8 + qrow;
+          const bool live = r < rows;
+          const int R = rb * C::kRows + r, node = R / p.G;
+          const __nv_bfloat16* qb = p.q + (((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G)) * D + qcol;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            qa[mt][ks][h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16) : 0u;
+            qa[mt][ks][2 + h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16 + 8) : 0u;
+          }
+          mx[mt][h] = -INFINITY;
+          l[mt][h] = 0.f;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
+      }
+    }
+    if (!mbar_wait_bounded(bar0 + 8 * slot, phase)) { failed = true; break; }
+    --inflight;
+    const uint32_t tile = ring + slot * TILE;
+    const int32_t key0 = (int32_t)(page & kPageBits) * kPage;
+
+    // ---- S = Q K^T ----
+    float x[MT][2][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) x[mt][nt][0] = x[mt][nt][1] = x[mt][nt][2] = x[mt][nt][3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      uint32_t r0, r1, r2, r3;
+      ldsm_x4(tile + k_off + ((((2 * ks + (mi & 1)) ^ rr)) << 4), r0, r1, r2, r3);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        mma_bf16(x[mt][0], qa[mt][ks][0], qa[mt][ks][1], qa[mt][ks][2], qa[mt][ks][3], r0, r1);
+        mma_bf16(x[mt][1], qa[mt][ks][0], qa[mt][ks][1], qa[mt][ks][2], qa[mt][ks][3], r2, r3);
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[mt][nt][e] *= p.scale_log2e;
+
+    const bool masked = key0 + kPage > sp.ctx || key0 < border || (page & kBad);
+    uint32_t odd = 0;                         // keys of the tile whose values are not all finite
+    if (masked) {
+      // Slots nobody may read (behind the end, before the window, a bad page) hold anything: their values are
+      // cleared.  The others are searched for values that are not finite.
+      for (int t = 0; t < kPage; ++t) {
+        const bool dead = key0 + t >= sp.n || key0 + t < sp.lo || (page & kBad);
+        bool found = false;
+        for (int off = lane * 16; off < ROWB; off += 512) {
+          const uint32_t a = tile + (uint32_t)(kPage * ROWB + t * ROWB + off);
+          uint4 w = make_uint4(0u, 0u, 0u, 0u);
+          if (!dead) {
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a));
+            found |= any_not_finite(w);
+          } else {
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+          }
+        }
+        if (__any_sync(0xffffffffu, found)) odd |= 1u << t;
+      }
+      __syncwarp();
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = mt * 16 + h * 8 + qrow;
+          if (r < rows && !(page & kBad)) {
+            const RowView v = row_view(p, b, sp, (rb * C::kRows + r) / p.G);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int32_t key = key0 + nt * 8 + qcol + e;
+                if (key >= sp.n || !sees(v, sp.ctx, key)) x[mt][nt][2 * h + e] = -INFINITY;
+              }
+          } else {
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) x[mt][nt][2 * h] = x[mt][nt][2 * h + 1] = -INFINITY;
+          }
+        }
+    }
+
+    // ---- online softmax (base 2) ----
+    uint32_t pa[MT][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float top[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float t = fmaxf(fmaxf(x[mt][0][2 * h], x[mt][0][2 * h + 1]), fmaxf(x[mt][1][2 * h], x[mt][1][2 * h + 1]));
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
+        top[h] = fmaxf(mx[mt][h], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2)));
+      }
+      if (__any_sync(0xffffffffu, top[0] > mx[mt][0] || top[1] > mx[mt][1])) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float a = mx[mt][h] == -INFINITY ? 0.f : fast_exp2(mx[mt][h] - top[h]);   // nothing summed yet: all zero
+          l[mt][h] *= a;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) { o[mt][nt][2 * h] *= a; o[mt][nt][2 * h + 1] *= a; }
+          mx[mt][h] = top[h];
+        }
+      }
+      float pr[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float m = mx[mt][h] == -INFINITY ? 0.f : mx[mt][h];
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            pr[nt][2 * h + e] = fast_exp2(x[mt][nt][2 * h + e] - m);
+            l[mt][h] += pr[nt][2 * h + e];
+          }
+      }
+      // P is rounded to bf16 for the product, the sum is not: the roundings average out over the keys
+      pa[mt][0] = pack_bf16(pr[0][0], pr[0][1]);
+      pa[mt][1] = pack_bf16(pr[0][2], pr[0][3]);
+      pa[mt][2] = pack_bf16(pr[1][0], pr[1][1]);
+      pa[mt][3] = pack_bf16(pr[1][2], pr[1][3]);
+    }
+    if (odd) {                                // rare: values that are not finite leave the tile
+      for (uint32_t rest = odd; rest; rest &= rest - 1) {
+        const int t = __ffs(rest) - 1;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = mt * 16 + h * 8 + qrow;
+            if (r >= rows || !sees(row_view(p, b, sp, (rb * C::kRows + r) / p.G), sp.ctx, key0 + t)) continue;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t a = tile + (uint32_t)(kPage * ROWB + t * ROWB + ((nt ^ (t & 7)) << 4) + (qcol + e) * 2);
+                const float val = bf16_at(a);
+                if (!isfinite(val)) o[mt][nt][2 * h + e] += val;
+              }
+          }
+      }
+      __syncwarp();
+      for (uint32_t rest = odd; rest; rest &= rest - 1) {
+        const int t = __ffs(rest) - 1;
+        for (int off = lane * 2; off < ROWB; off += 64) {
+          const uint32_t a = tile + (uint32_t)(kPage * ROWB + t * ROWB + off);
+          if (!isfinite(bf16_at(a))) asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)0) : "memory");
+        }
+      }
+      __syncwarp();
+    }
+    // ---- O += P V ----
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      uint32_t r0, r1, r2, r3;
+      ldsm_x4_t(tile + v_off + ((((2 * j + (mi >> 1)) ^ rr)) << 4), r0, r1, r2, r3);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        mma_bf16(o[mt][2 * j], pa[mt][0], pa[mt][1], pa[mt][2], pa[mt][3], r0, r1);
+        mma_bf16(o[mt][2 * j + 1], pa[mt][0], pa[mt][1], pa[mt][2], pa[mt][3], r2, r3);
+      }
+    }
+    __syncwarp();
+    if (u + stages < u1) {
+      if (lane == 0) fence_proxy_async();
+      issue(u + stages, slot);
+      ++inflight;
+    }
+    if (++slot == stages) { slot = 0; phase ^= 1u; }
+
+    if (last || u == u1 - 1) {                // the row block, or this worker's part of it, is done
+      const bool complete = from_first && last;
+      float* pb = p.partials + (2 * worker + (on_first_row ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float t = l[mt][h];
+          t += __shfl_xor_sync(0xffffffffu, t, 1);
+          t += __shfl_xor_sync(0xffffffffu, t, 2);
+          const int r = mt * 16 + h * 8 + qrow;
+          if (r >= rows) continue;
+          if (complete) {
+            const int R = rb * C::kRows + r, node = R / p.G;
+            const int64_t row = ((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
+            const float inv = t > 0.f ? 1.f / t : 0.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              *reinterpret_cast<uint32_t*>(p.out + row * D + nt * 8 + qcol) =
+                  pack_bf16(o[mt][nt][2 * h] * inv, o[mt][nt][2 * h + 1] * inv);
+            if (p.lse && (lane & 3) == 0)
+              p.lse[row] = t > 0.f ? (mx[mt][h] + log2f(t)) * 0.6931471805599453f : t == 0.f ? -INFINITY : t;
+          } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              *reinterpret_cast<float2*>(pb + r * D + nt * 8 + qcol) = make_float2(o[mt][nt][2 * h], o[mt][nt][2 * h + 1]);
+            if ((lane & 3) == 0) {
+              pb[C::kRows * D + r] = mx[mt][h];
+              pb[C::kRows * (D + 1) + r] = t;
+            }
+          }
+        }
+      on_first_row = false;
+    }
+  }
+  pdl_launch_dependents();
+  if (failed) {
+    // A copy did not arrive in time: record it, then give every copy still in flight a bounded chance to land.
+    if (lane == 0) atomicOr(p.status, kErrTimeout);
+    for (int i = 0; i < inflight; ++i) {
+      (void)mbar_wait_bounded(bar0 + 8 * slot, phase);
+      if (++slot == stages) { slot = 0; phase ^= 1u; }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// combine: merges the partials of row blocks that several workers share, and writes the rows that no worker has
+// ---------------------------------------------------------------------------------
+struct TreeCombineParams {
+  TreeParams t;
+  int32_t D, row_block, keys, max_blocks;    // max_blocks: row blocks of a full tree of `nodes`
+  int64_t workers;
+};
+constexpr int kTreeCombineThreads = 256;
+constexpr int kTreeCombineCols = 32;         // columns of a block's slice
+
+// grid (batch * Hkv * max_blocks, D / 32).  Each block merges 32 columns of one row block: first every row's maximum and sum over
+// the partials, then the weighted sums, a thread per four columns of a row.
+__global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const TreeCombineParams c) {
+  const TreeParams& p = c.t;
+  __shared__ float top_s[256], sum_s[256];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int rb = blockIdx.x % c.max_blocks, bg = blockIdx.x / c.max_blocks, g = bg % p.Hkv, b = bg / p.Hkv;
+  const Span s = span_of(p, b, c.row_block);
+  const int live = s.tree * p.G, r0 = rb * c.row_block;
+  const int r1 = min(r0 + c.row_block, p.nodes * p.G);           // rows [r0, r1) of this block exist in the output
+  const int D = c.D, col0 = blockIdx.y * kTreeCombineCols;
+  const int32_t cnt = tiles_of(s, c.keys);
+  auto out_row = [&](int R) {
+    const int node = R / p.G;
+    return ((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
+  };
+  // rows of nodes that are not there (or of a sequence with no key to see): zeros
+  for (int i = threadIdx.x; i < (r1 - r0) * (kTreeCombineCols / 8); i += kTreeCombineThreads) {
+    const int R = r0 + i / (kTreeCombineCols / 8);
+    if (R < live && cnt > 0) continue;
+    *reinterpret_cast<uint4*>(p.out + out_row(R) * D + col0 + i % (kTreeCombineCols / 8) * 8) = make_uint4(0u, 0u, 0u, 0u);
+    if (p.lse && blockIdx.y == 0 && i % (kTreeCombineCols / 8) == 0) p.lse[out_row(R)] = -INFINITY;
+  }
+  if (cnt == 0 || rb >= s.blocks) return;
+  const int64_t U = p.cum[p.batch];
+  const int64_t first = p.cum[b] + ((int64_t)g * s.blocks + rb) * cnt, end = first + cnt;
+  const int64_t wf = worker_of(U, first, c.workers), wl = worker_of(U, end - 1, c.workers);
+  if (wf == wl) return;                                          // finished by its worker
+  const int64_t slot_floats = (int64_t)c.row_block * (D + 2);
+  auto part = [&](int64_t w) -> const float* {                   // worker w's partial of this row block, or null
+    const int64_t a = worker_begin(U, w, c.workers);
+    if (a == worker_begin(U, w + 1, c.workers)) return nullptr;
+    return p.partials + (2 * w + (a >= first ? 0 : 1)) * slot_floats;
+  };
+  const int rows = min(live - r0, c.row_block);
+  for (int r = threadIdx.x; r < rows; r += kTreeCombineThreads) {
+    float m = -INFINITY, l = 0.f;
+    for (int64_t w = wf; w <= wl; ++w) {
+      const float* q = part(w);
+      if (!q) continue;
+      const float mw = __ldcg(q + c.row_block * D + r), lw = __ldcg(q + c.row_block * (D + 1) + r);
+      const float t = fmaxf(m, mw);
+      if (t != -INFINITY) l = l * exp2f(m - t) + lw * exp2f(mw - t);
+      m = t;
+    }
+    top_s[r] = m;
+    sum_s[r] = l;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * (kTreeCombineCols / 4); i += kTreeCombineThreads) {
+    const int r = i / (kTreeCombineCols / 4), col = col0 + i % (kTreeCombineCols / 4) * 4;
+    const float m = top_s[r], l = sum_s[r];
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int64_t w = wf; w <= wl; ++w) {
+      const float* q = part(w);
+      if (!q) continue;
+      const float mw = __ldcg(q + c.row_block * D + r);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(q + r * D + col));
+      if (mw == -INFINITY) continue;                             // this part of the row saw nothing
+      const float f = exp2f(mw - m);
+      acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    uint2 w2;
+    w2.x = pack_bf16(acc.x * inv, acc.y * inv);
+    w2.y = pack_bf16(acc.z * inv, acc.w * inv);
+    const int64_t row = out_row(r0 + r);
+    *reinterpret_cast<uint2*>(p.out + row * D + col) = w2;
+    if (p.lse && col == 0) p.lse[row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
+  }
+}
+
+}  // namespace opw_tree
