@@ -22,7 +22,8 @@ SOURCES = [os.path.join(_HERE, "csrc", "opw_attn.cu"), os.path.join(_HERE, "csrc
 HEADERS = [os.path.join(_HERE, "csrc", "opw_kernels.cuh"), os.path.join(_HERE, "csrc", "opw_afd_gemm.cuh"), os.path.join(_ROOT, "include", "opw_attn.h"),
            os.path.join(_ROOT, "include", "opw_linear_attn.h"), os.path.join(_ROOT, "include", "opw_afd.h"),
            os.path.join(_ROOT, "include", "opw_draft.h"), os.path.join(_ROOT, "include", "opw_pages.h"),
-           os.path.join(_HERE, "csrc", "opw_stage.h"), os.path.join(_HERE, "csrc", "opw_tree_kernels.cuh")]
+           os.path.join(_HERE, "csrc", "opw_stage.h"), os.path.join(_HERE, "csrc", "opw_tree_kernels.cuh"),
+           os.path.join(_HERE, "csrc", "opw_tree_mma.cuh")]
 
 OPW_FLAG_NO_PDL = 1
 OPW_FLAG_COPY_STREAMS = 2

@@ -1,10 +1,12 @@
 // Host side of tree attention (include/opw_draft.h): argument checks, choice of kernel, launches.
 #include <cstdint>
 #include <new>
+#include <vector>
 
 #include "opw_draft.h"
 #include "opw_stage.h"
 #include "opw_tree_kernels.cuh"
+#include "opw_tree_mma.cuh"
 
 namespace {
 
@@ -16,11 +18,21 @@ struct TreeLayout {
 
 struct Variant {              // a kernel, and how it cuts rows and keys
   int row_block, keys, workers;
+  bool mma;
 };
 
-Variant pick(const opw_stage_view& v, int nodes) {
+constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the shared memory beside the tiles
+
+Variant pick(const opw_stage_view& v, int nodes, int batch) {
   const int rows = nodes * (v.Hq / v.Hkv);
   Variant k;
+  k.mma = rows > 32 && v.D != 256 && batch <= kMmaMaxBatch;
+  if (k.mma) {
+    k.keys = opw_tree::kMmaKeys;
+    k.row_block = opw_tree::kMmaRows;
+    k.workers = v.sms;
+    return k;
+  }
   k.keys = 16;
   k.row_block = rows <= 16 || v.D == 256 ? 16 : 32;
   k.workers = v.sms * (v.D == 64 ? 12 : v.D == 128 ? 8 : 6);
@@ -33,9 +45,11 @@ TreeLayout carve(const opw_stage_view& v, int max_nodes) {
   L.partials = align_up((size_t)(opw_tree::kMaxTreeBatch + 1) * 8);
   size_t most = 0;            // over every number of nodes a call may have
   for (int n = 1; n <= max_nodes; ++n) {
-    const Variant k = pick(v, n);
-    const size_t need = (size_t)k.workers * 2 * k.row_block * (v.D + 2) * 4;
-    if (need > most) most = need;
+    for (int b : {1, kMmaMaxBatch + 1}) {
+      const Variant k = pick(v, n, b);
+      const size_t need = (size_t)k.workers * 2 * k.row_block * (v.D + 2) * 4;
+      if (need > most) most = need;
+    }
   }
   L.total = L.partials + align_up(most);
   return L;
@@ -53,6 +67,27 @@ cudaError_t launch_warp(const opw_stage_view& v, const opw_tree::TreeParams& p, 
   return opw_launch(opw_tree::tree_warp_kernel<D, MT>, dim3(v.sms), dim3(C::kWarps * 32), C::smem(p.batch), stream, v.pdl, 1, p);
 }
 
+template <int D>
+cudaError_t launch_mma(const opw_stage_view& v, const CUtensorMap& map, const opw_tree::TreeParams& p, cudaStream_t stream) {
+  return opw_launch(opw_tree::tree_mma_kernel<D>, dim3(v.sms), dim3(opw_tree::kMmaThreads), opw_tree::MmaTree<D>::smem(p.batch), stream,
+                    v.pdl, 1, map, p);
+}
+
+typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// One layer's pool as [page and head][K, V][slot][64 dimensions at a time][64]; a box is 16 slots of 64 dimensions.  No
+// swizzle: the pool's own permutation is the one the tensor core expects.
+bool encode_pool(TensorMapEncodeFn fn, CUtensorMap* map, void* pool, const opw_stage_view& v, int64_t num_pages) {
+  const cuuint64_t row = (cuuint64_t)v.D * 2;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)v.D / 64, 16, 2, (cuuint64_t)num_pages * v.Hkv};
+  const cuuint64_t strides[4] = {128, row, 16 * row, 32 * row};
+  const cuuint32_t box[5] = {64, 1, 16, 1, 1}, elem[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, pool, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 struct opw_tree_attn {
@@ -60,6 +95,7 @@ struct opw_tree_attn {
   int32_t max_nodes;
   TreeLayout lay;
   unsigned char* ws;
+  std::vector<CUtensorMap> maps;   // of the layers' pools; empty at head_dim 256
 };
 
 extern "C" opw_status_t opw_tree_mask(int32_t nodes, const int32_t* parents, uint64_t* mask, int32_t* depth) {
@@ -98,9 +134,29 @@ extern "C" opw_status_t opw_tree_attn_create(opw_attn_stage_t* stage, int32_t ma
   } else {
     e = raise_smem<256, 1>();
   }
-  if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
+  if (e == cudaSuccess && v.D == 64)
+    e = cudaFuncSetAttribute(opw_tree::tree_mma_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)opw_tree::MmaTree<64>::smem(kMmaMaxBatch));
+  if (e == cudaSuccess && v.D == 128)
+    e = cudaFuncSetAttribute(opw_tree::tree_mma_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)opw_tree::MmaTree<128>::smem(kMmaMaxBatch));
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
+  if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !fn) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   opw_tree_attn* t = new (std::nothrow) opw_tree_attn();
   if (!t) return OPW_ERR_INVALID_ARG;
+  try {
+    t->maps.resize(v.D == 256 ? 0 : v.num_layers);
+  } catch (...) {
+    delete t;
+    return OPW_ERR_INVALID_ARG;
+  }
+  for (size_t i = 0; i < t->maps.size(); ++i)
+    if (!encode_pool(reinterpret_cast<TensorMapEncodeFn>(fn), &t->maps[i], v.pool[i], v, v.num_pages[i])) {
+      delete t;
+      return OPW_ERR_CUDA;
+    }
   t->stage = stage;
   t->max_nodes = max_nodes;
   t->lay = lay;
@@ -129,7 +185,7 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   const size_t bytes = (size_t)batch * nodes * v.Hq * v.D * 2;
   if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return OPW_ERR_INVALID_ARG;
   if (batch == 0) return OPW_OK;
-  const Variant k = pick(v, nodes);
+  const Variant k = pick(v, nodes, batch);
   opw_tree::TreeCombineParams c;
   opw_tree::TreeParams& p = c.t;
   p.pool = static_cast<const __nv_bfloat16*>(v.pool[layer]);
@@ -162,7 +218,8 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   if (!guard.ok()) return OPW_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (v.D == 64) e = k.row_block == 16 ? launch_warp<64, 1>(v, p, stream) : launch_warp<64, 2>(v, p, stream);
+  if (k.mma) e = v.D == 64 ? launch_mma<64>(v, tree->maps[layer], p, stream) : launch_mma<128>(v, tree->maps[layer], p, stream);
+  else if (v.D == 64) e = k.row_block == 16 ? launch_warp<64, 1>(v, p, stream) : launch_warp<64, 2>(v, p, stream);
   else if (v.D == 128) e = k.row_block == 16 ? launch_warp<128, 1>(v, p, stream) : launch_warp<128, 2>(v, p, stream);
   else e = launch_warp<256, 1>(v, p, stream);
   if (e == cudaSuccess) {

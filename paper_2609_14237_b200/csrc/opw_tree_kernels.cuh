@@ -538,7 +538,8 @@ __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const
       if (!q) continue;
       const float mw = __ldcg(q + c.row_block * D + r), lw = __ldcg(q + c.row_block * (D + 1) + r);
       const float t = fmaxf(m, mw);
-      if (t != -INFINITY) l = l * exp2f(m - t) + lw * exp2f(mw - t);
+      // a part that saw nothing has the maximum -inf and the sum 0 (or NaN, from a NaN score): weight 1
+      l = (m == -INFINITY ? l : l * exp2f(m - t)) + (mw == -INFINITY ? lw : lw * exp2f(mw - t));
       m = t;
     }
     top_s[r] = m;
@@ -554,8 +555,7 @@ __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const
       if (!q) continue;
       const float mw = __ldcg(q + c.row_block * D + r);
       const float4 v = __ldcg(reinterpret_cast<const float4*>(q + r * D + col));
-      if (mw == -INFINITY) continue;                             // this part of the row saw nothing
-      const float f = exp2f(mw - m);
+      const float f = mw == -INFINITY ? 1.f : exp2f(mw - m);     // -inf: this part of the row saw nothing, O is 0
       acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
     }
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;

@@ -1,0 +1,585 @@
+// Tree attention on the 5th-generation tensor cores, for trees whose rows (nodes x group) fill matrix tiles.
+//
+// One CTA per SM: two softmax warpgroups ("slots"), a TMA producer and an MMA issuer.  Slot s owns a query tile of
+// 128 rows in shared memory and, in TMEM, a score tile S_s (128 x 128 fp32, its first 64 columns reused for P in bf16)
+// and an accumulator O_s (128 x D fp32).  Per key tile of 128 keys (eight pages):
+//     S_s = Q_s K^T      tcgen05.mma, both operands in shared memory
+//     P_s = 2^(S - m)    a thread per row: S from TMEM to registers, P back to TMEM
+//     O_s += P_s V       tcgen05.mma, P from TMEM, V from shared memory
+// A row block of up to 256 rows shares every key tile between the slots (slot s = rows 128 s ...).  One of up to 128
+// rows gives each slot every other key tile, and the two (O, m, l) are joined at the end.  Either way one slot's
+// softmax runs under the other's products.
+//
+// The cache needs no re-layout: a cached row's 16-byte words are permuted by XOR with slot mod 8, which is what the
+// 128-byte swizzle of the tensor core expects of rows of 128 bytes.  So K (K-major) and V (MN-major) tiles are copied by plain TMA
+// boxes of 16 rows x 128 bytes, one per page and 64 dimensions.  A page that is missing or bad is copied from
+// beyond the tensor's end, which TMA fills with zeros: no traffic, and no stale shared memory in the product.
+//
+// The running maximum is only raised when a row's new maximum exceeds it by 2^8: P stays below 2^8, exact in the same
+// relative sense, and O is rescaled a few times per row instead of once per tile.
+#pragma once
+
+#include <cuda.h>
+
+#include "opw_tree_kernels.cuh"
+
+namespace opw_tree {
+
+constexpr int kMmaThreads = 384;              // two softmax warpgroups; of the third, one warp produces and one issues
+constexpr int kMmaKeys = 128;                 // keys per tile
+constexpr int kMmaRows = 256;                 // rows per block
+constexpr float kRaise = 8.f;                 // log2 of how far a row's maximum may run ahead of the one in use
+
+template <int D>
+struct MmaTree {
+  static constexpr int kHalves = D / 64;
+  static constexpr uint32_t kHalfBytes = 128 * 128;           // 128 rows x 64 dimensions
+  static constexpr uint32_t kPiece = kHalves * kHalfBytes;    // a K or V tile, and a query tile
+  static constexpr int kPieces = D == 128 ? 4 : 8;
+  static size_t smem(int batch) { return 1024 + (size_t)(kPieces + 2) * kPiece + (size_t)(batch + 1) * 8; }
+};
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int c1, int c3, int c4, uint32_t bar, uint64_t pol) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], "
+      "[%7], %8;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(c1), "r"(0), "r"(c3), "r"(c4), "r"(bar), "l"(pol)
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// D[tmem] (+)= A * B, M = 128, K = 16; A in shared memory or in TMEM
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+      "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.eq.b32 p, 0, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
+      "l"(b), "r"(idesc)
+      : "memory");
+}
+#define OPW_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define OPW_I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 (16) consecutive 32-bit columns of this thread's TMEM lane
+__device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+      "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : OPW_R8(r, 0), OPW_R8(r, 8), OPW_R8(r, 16), OPW_R8(r, 24)
+      : "r"(addr));
+}
+__device__ __forceinline__ void tm_ld16(uint32_t addr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : OPW_R8(r, 0), OPW_R8(r, 8)
+               : "r"(addr));
+}
+__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+      "%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::OPW_I8(r, 0),
+      OPW_I8(r, 8), OPW_I8(r, 16), OPW_I8(r, 24), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::OPW_I8(r, 0), OPW_I8(r, 8),
+      "r"(addr)
+      : "memory");
+}
+#undef OPW_R8
+#undef OPW_I8
+__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// Shared-memory matrix descriptor, 128-byte swizzle (layout type 2, version 1); offsets in 16-byte units.  K-major (Q, K): 8-row groups
+// 1024 bytes apart, leading offset unused.  MN-major (V): 64-element blocks along the dimensions kHalfBytes apart
+// (leading), groups of eight keys 1024 bytes apart (stride).
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t block_bytes) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block_bytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// kind::f16: fp32 accumulator, A and B bf16, A K-major, B K-major or MN-major (bit 16), N, M = 128
+__device__ __forceinline__ uint32_t idesc_of(int n, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
+// The row blocks of a worker's share, one after the other; every role walks the same list.
+struct Segment {
+  int b, g, rb, rows;          // rows of the block that exist
+  int32_t t0, n;               // first key tile and number of tiles
+  bool first, last;            // the block's first / last tile is among them
+  bool shared;                 // both slots on every tile (more than 128 rows), or alternate tiles
+  Span sp;
+};
+__device__ __forceinline__ Segment segment_at(const TreeParams& p, const int64_t* cum, int64_t u, int64_t u1) {
+  Segment s;
+  s.b = find_sequence(cum, p.batch, u);
+  s.sp = span_of(p, s.b, kMmaRows);
+  const int32_t cnt = tiles_of(s.sp, kMmaKeys);
+  const int64_t rem = u - cum[s.b];
+  const int32_t ri = (int32_t)(rem / cnt);
+  s.t0 = (int32_t)(rem - (int64_t)ri * cnt);
+  s.g = ri / s.sp.blocks;
+  s.rb = ri - s.g * s.sp.blocks;
+  s.rows = min(s.sp.tree * p.G - s.rb * kMmaRows, kMmaRows);
+  s.n = (int32_t)min((int64_t)(cnt - s.t0), u1 - u);
+  s.first = s.t0 == 0;
+  s.last = s.t0 + s.n == cnt;
+  s.shared = s.rows > 128;
+  return s;
+}
+// The ring takes K 0, then K t + 1 and V t for every tile t: the order in which the products need them.
+__device__ __forceinline__ int64_t piece_k(int t) { return t == 0 ? 0 : 2 * (int64_t)t - 1; }
+__device__ __forceinline__ int64_t piece_v(int t, int n) { return t + 1 < n ? 2 * (int64_t)t + 2 : 2 * (int64_t)n - 1; }
+
+template <int D>
+__global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_constant__ CUtensorMap map, const TreeParams p) {
+  using C = MmaTree<D>;
+  constexpr int NP = C::kPieces;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t full_bar[NP], empty_bar[NP], s_bar[2], p_bar[2], o_bar[2], seg_bar, end_bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int piece_bad[NP], slot_bad[2];          // pages of a K tile that are bad: bit per page
+  __shared__ uint32_t odd_s[2][4];                    // keys of a tile with values that are not finite
+  __shared__ float ml_s[2][2][128];                   // m, l of the two slots, to be joined
+  __shared__ volatile int dead_s;                     // a wait ran out: nobody waits any more
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const uint32_t q_smem = base, ring = base + 2 * C::kPiece;
+  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)(NP + 2) * C::kPiece);
+
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
+    for (int i = 0; i < NP; ++i) { mbar_init(smem_u32(&full_bar[i]), 1); mbar_init(smem_u32(&empty_bar[i]), 1); }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&s_bar[s]), 2);              // the products' commit, and the issuer once slot_bad is set
+      mbar_init(smem_u32(&p_bar[s]), 128);
+      mbar_init(smem_u32(&o_bar[s]), 1);
+    }
+    mbar_init(smem_u32(&seg_bar), 256);
+    mbar_init(smem_u32(&end_bar), 1);
+    dead_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_before();
+  scan_units(p, cum, kMmaRows, kMmaKeys);             // begins and ends with a barrier of the block
+  tc_after();
+  const uint32_t tmem = tmem_slot;
+  const int64_t U = cum[p.batch];
+  const int64_t u0 = worker_begin(U, blockIdx.x, gridDim.x), u1 = worker_begin(U, blockIdx.x + 1, gridDim.x);
+  pdl_wait();                                         // up to here only this step's lengths were read
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i <= p.batch; i += kMmaThreads) p.cum[i] = cum[i];
+
+  // Bounded wait; after the first that ran out, every wait of the block returns at once and the roles walk on through the
+  // same control flow (which depends on lengths only), so that no named barrier is left short.
+  auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+    const uint32_t a = smem_u32(bar);
+    if (mbar_try_wait(a, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    while (!dead_s) {
+      for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(a, parity)) return true;
+      if (global_timer_ns() - t0 > kWaitLimitNs) {
+        dead_s = 1;
+        atomicOr(p.status, kErrTimeout);
+      }
+    }
+    return false;
+  };
+
+  // Registers: 384 threads are launched with 168 each (64512); a softmax thread holds a row of 128 scores and wants
+  // more, the third warpgroup needs little: 256 x 200 + 128 x 104 = 64512.
+  if (warp >= 8) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+  if (warp == 8) {
+    // ---- producer ----
+    const uint64_t policy = l2_evict_first_policy();
+    const int32_t nowhere = (int32_t)(p.num_pages * p.Hkv);   // one past the tensor's last tile: zeros
+    int64_t issued = 0;
+    bool ok = true;
+    for (int64_t u = u0; u < u1 && ok;) {
+      const Segment s = segment_at(p, cum, u, u1);
+      const int32_t page0 = s.sp.lo / kPage + s.t0 * (kMmaKeys / kPage) + (lane & 7);
+      auto fetch = [&](int t) -> int32_t {            // this lane's page of tile t: raw id, or -2 where there is none
+        const int32_t lp = page0 + t * (kMmaKeys / kPage);
+        return t < s.n && (int64_t)lp * kPage < s.sp.n ? __ldg(p.page_table + (int64_t)s.b * p.max_pages + lp) : -2;
+      };
+      auto load = [&](int32_t id, int kv) {
+        const int st = (int)(issued % NP);
+        const int64_t round = issued / NP;
+        if (round > 0) ok = ok && wait(&empty_bar[st], (uint32_t)(round - 1) & 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
+        const bool good = id >= 0 && id < p.num_pages;
+        const uint32_t bad = __ballot_sync(0xffffffffu, !good && id != -2) & 0xffu;
+        if (lane == 0) {
+          if (kv == 0) {
+            piece_bad[st] = (int)bad;
+            if (bad) atomicOr(p.status, kErrBadPage);
+          }
+          mbar_expect_tx(smem_u32(&full_bar[st]), C::kPiece);
+        }
+        __syncwarp();
+        if (lane < 8 * C::kHalves) {
+          const int half = lane >> 3;
+          tma_load_5d(ring + (uint32_t)st * C::kPiece + (uint32_t)half * C::kHalfBytes + (uint32_t)(lane & 7) * 2048u, &map, half, kv,
+                      good ? (int32_t)((int64_t)id * p.Hkv + s.g) : nowhere, smem_u32(&full_bar[st]), policy);
+        }
+        ++issued;
+      };
+      int32_t id = fetch(0), next = fetch(1);
+      load(id, 0);
+      for (int t = 0; t < s.n && ok; ++t) {
+        const int32_t after = fetch(t + 2);
+        if (t + 1 < s.n) load(next, 0);
+        if (ok) load(id, 1);
+        id = next;
+        next = after;
+      }
+      u += s.n;
+    }
+    // every copy lands before the block's shared memory is given up
+    const int64_t from = issued > NP ? issued - NP : 0;
+    for (int64_t i = from; i < issued; ++i) {
+      for (int k = 0; k < 1 << 16; ++k)
+        if (mbar_try_wait(smem_u32(&full_bar[i % NP]), (uint32_t)(i / NP) & 1u)) break;
+    }
+  } else if (warp == 9) {
+    // ---- MMA issuer ----
+    if (lane == 0) {
+      const uint32_t id_s = idesc_of(kMmaKeys, false), id_o = idesc_of(D, true);
+      int64_t done = 0;                                // pieces of the segments before
+      uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_seg = 0;
+      bool ok = true;
+      for (int64_t u = u0; u < u1 && ok;) {
+        const Segment s = segment_at(p, cum, u, u1);
+        const int shift = s.shared ? 1 : 0, items = s.n << shift;
+        ok = ok && wait(&seg_bar, n_seg++ & 1u);
+        tc_after();
+        auto scores = [&](int i) {
+          const int t = i >> shift, x = i & 1;
+          const int64_t pc = done + piece_k(t);
+          const int st = (int)(pc % NP);
+          ok = ok && wait(&full_bar[st], (uint32_t)(pc / NP) & 1u);
+          if (!ok) return;
+          slot_bad[x] = piece_bad[st];
+          mbar_arrive(smem_u32(&s_bar[x]));
+          tc_after();
+          const uint32_t a = q_smem + (uint32_t)x * C::kPiece, b = ring + (uint32_t)st * C::kPiece;
+#pragma unroll
+          for (int h = 0; h < C::kHalves; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_ss(tmem + x * 128, desc_k(a + h * C::kHalfBytes) + 2u * k, desc_k(b + h * C::kHalfBytes) + 2u * k, id_s,
+                     (uint32_t)((h | k) != 0));
+          tc_commit(smem_u32(&s_bar[x]));
+          if (!s.shared || x == 1) tc_commit(smem_u32(&empty_bar[st]));
+        };
+        scores(0);
+        if (items > 1) scores(1);
+        for (int i = 0; i < items && ok; ++i) {
+          const int t = i >> shift, x = i & 1;
+          const int64_t pc = done + piece_v(t, s.n);
+          const int st = (int)(pc % NP);
+          ok = ok && wait(&p_bar[x], n_p[x]++ & 1u);
+          ok = ok && wait(&full_bar[st], (uint32_t)(pc / NP) & 1u);
+          if (!ok) break;
+          tc_after();
+          const uint64_t b = desc_mn(ring + (uint32_t)st * C::kPiece, C::kHalfBytes);
+#pragma unroll
+          for (int k = 0; k < kMmaKeys / 16; ++k) mma_ts(tmem + 256 + x * 128, tmem + x * 128 + 8 * k, b + 128u * k, id_o);
+          tc_commit(smem_u32(&o_bar[x]));
+          if (!s.shared || x == 1) tc_commit(smem_u32(&empty_bar[st]));
+          if (i + 2 < items) {
+            ok = ok && wait(&o_bar[x], n_o[x] & 1u);   // P, in the same columns as the next S, has been read
+            if (ok) scores(i + 2);
+          }
+          ++n_o[x];
+        }
+        done += 2 * (int64_t)s.n;
+        u += s.n;
+      }
+      tc_commit(smem_u32(&end_bar));                   // nothing is in flight when the TMEM is given back
+      for (int k = 0; k < 1 << 16; ++k)
+        if (mbar_try_wait(smem_u32(&end_bar), 0)) break;
+    }
+    __syncwarp();
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    // ---- softmax: thread = one row of slot x ----
+    const int x = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t s_addr = lane_addr + x * 128, o_addr = lane_addr + 256 + x * 128;
+    uint32_t mine_done = 0;                            // tiles of this slot: phases of s_bar and o_bar
+    int64_t done = 0;
+    bool on_first = true;
+    for (int64_t u = u0; u < u1;) {
+      const Segment s = segment_at(p, cum, u, u1);
+      const Span& sp = s.sp;
+      const int r = s.shared ? x * 128 + row : row;    // row of the block
+      const bool live = r < s.rows;
+      const int R = s.rb * kMmaRows + r, node = R / p.G;
+      auto global_row = [&](int rr) {
+        const int RR = s.rb * kMmaRows + rr, nn = RR / p.G;
+        return ((int64_t)s.b * p.nodes + nn) * p.Hq + (int64_t)s.g * p.G + (RR - nn * p.G);
+      };
+      // queries to shared memory, in the layout of a K-major swizzled operand; rows that are not there: zeros
+      const uint32_t qs = q_smem + (uint32_t)x * C::kPiece;
+#pragma unroll 4
+      for (int i = row; i < 128 * (D / 8); i += 128) {
+        const int qr = i / (D / 8), c = i % (D / 8), rr = s.shared ? x * 128 + qr : qr;
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (rr < s.rows) w = *(reinterpret_cast<const uint4*>(p.q + global_row(rr) * D) + c);
+        const uint32_t a = qs + (uint32_t)(c >> 3) * C::kHalfBytes + (uint32_t)qr * 128u + (uint32_t)(((c & 7) ^ (qr & 7)) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+      }
+      fence_proxy_async();
+      {
+        uint32_t z[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) z[i] = 0u;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) tm_st32(o_addr + c, z);
+        tm_wait_st();
+      }
+      tc_before();
+      mbar_arrive(smem_u32(&seg_bar));
+
+      RowView view = {0ull, 0};
+      if (live) view = row_view(p, s.b, sp, node);
+      const int32_t border = window_border(p, s.b, sp, lane);
+      float m = -INFINITY, l = 0.f;
+      const int shift = s.shared ? 1 : 0, items = s.n << shift;
+      for (int i = x; i < items; i += 2) {
+        const int t = i >> shift;
+        const int32_t key0 = sp.lo / kPage * kPage + (s.t0 + t) * kMmaKeys;
+        const bool edge = key0 + kMmaKeys > sp.ctx || key0 < border;
+        (void)wait(&s_bar[x], mine_done & 1u);
+        tc_after();
+        if (edge) {
+          // Values of keys that some row may not see.  The tile's warpgroup (slot 0's where they share it) clears the rows nobody
+          // may read and looks for values that are not finite, a thread per key.  The V tile's barrier may only be asked
+          // once the scores are there: they were issued after the piece that had its place in the ring before was read,
+          // so its phase is the one meant and not the one before, of the same parity as the one before that.
+          const int64_t pc = done + piece_v(t, s.n);
+          const int st = (int)(pc % NP), id = s.shared ? 1 : 2 + x, threads = s.shared ? 256 : 128;
+          const uint32_t v = ring + (uint32_t)st * C::kPiece + (uint32_t)row * 128u;
+          const bool mine = !s.shared || x == 0;
+          const int ox = s.shared ? 0 : x;
+          (void)wait(&full_bar[st], (uint32_t)(pc / NP) & 1u);
+          named_sync(id, threads);
+          if (mine) {
+            const int32_t key = key0 + row;
+            const bool gone = key >= sp.n || key < sp.lo;
+            bool found = false;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+              const uint32_t a = v + (uint32_t)(c >> 3) * C::kHalfBytes + (uint32_t)(((c + lane) & 7) << 4);
+              if (gone) {
+                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+              } else {
+                uint4 w;
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a));
+                found |= any_not_finite(w);
+              }
+            }
+            const uint32_t bal = __ballot_sync(0xffffffffu, found);
+            if (lane == 0) odd_s[ox][warp & 3] = bal;
+            fence_proxy_async();
+          }
+          named_sync(id, threads);
+          const volatile uint32_t* odd = odd_s[ox];
+          if (odd[0] | odd[1] | odd[2] | odd[3]) {     // rare: they leave the tile and are added to the rows that see them
+            if (mine_done > 0) (void)wait(&o_bar[x], (mine_done - 1u) & 1u);
+            tc_after();
+            const uint32_t tile = ring + (uint32_t)st * C::kPiece;
+            for (int c0 = 0; c0 < D; c0 += 16) {
+              uint32_t o[16];
+              tm_ld16(o_addr + c0, o);
+              tm_wait_ld();
+              for (int j = 0; j < 128; ++j) {
+                if (!((odd[j >> 5] >> (j & 31)) & 1u)) continue;
+                if (!live || key0 + j >= sp.n || !sees(view, sp.ctx, key0 + j)) continue;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const int d = c0 + e;
+                  const float val = bf16_at(tile + (uint32_t)(d >> 6) * C::kHalfBytes + (uint32_t)j * 128u +
+                                            (uint32_t)((((d & 63) >> 3) ^ (j & 7)) << 4) + (uint32_t)(d & 7) * 2u);
+                  if (!isfinite(val)) o[e] = __float_as_uint(__uint_as_float(o[e]) + val);
+                }
+              }
+              __syncwarp();
+              tm_st16(o_addr + c0, o);
+            }
+            tm_wait_st();
+            named_sync(id, threads);                   // everybody has read them
+            if (mine && ((odd[warp & 3] >> lane) & 1u)) {
+              for (int d = 0; d < D; ++d) {
+                const uint32_t a = v + (uint32_t)(d >> 6) * C::kHalfBytes + (uint32_t)((d & 63) * 2);
+                if (!isfinite(bf16_at(a))) asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)0) : "memory");
+              }
+            }
+            fence_proxy_async();
+            named_sync(id, threads);
+          }
+        }
+        uint32_t sv[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tm_ld32(s_addr + c, sv + c);
+        const int bad = *(volatile int*)&slot_bad[x];
+        tm_wait_ld();
+        if (edge || bad) {
+#pragma unroll
+          for (int j = 0; j < 128; ++j) {
+            const int32_t key = key0 + j;
+            const bool hide = key >= sp.n || !sees(view, sp.ctx, key) || ((bad >> (j >> 4)) & 1);
+            if (hide) sv[j] = 0xff800000u;             // -inf
+          }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 128; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(sv[j]), __uint_as_float(sv[j + 1])));
+        top *= p.scale_log2e;
+        const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xffffffffu, raise)) {
+          const bool shrink = raise && m != -INFINITY; // (with m = -inf, O and l are 0 or not finite: they stay)
+          const float a = shrink ? fast_exp2(m - top) : 1.f;
+          if (__any_sync(0xffffffffu, shrink)) {
+            (void)wait(&o_bar[x], (mine_done - 1u) & 1u);   // the products so far are in O
+            tc_after();
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tm_ld16(o_addr + c, o);
+              tm_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+              tm_st16(o_addr + c, o);
+            }
+            tm_wait_st();
+          }
+          l *= a;
+          if (raise) m = top;
+        }
+        const float off = m == -INFINITY ? 0.f : -m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float e0 = fast_exp2(fmaf(__uint_as_float(sv[c + j]), p.scale_log2e, off));
+            const float e1 = fast_exp2(fmaf(__uint_as_float(sv[c + j + 1]), p.scale_log2e, off));
+            sum[(j >> 1) & 3] += e0 + e1;
+            pk[j >> 1] = pack_bf16(e0, e1);            // rounded for the product only, the sum keeps 32 bits
+          }
+          tm_st16(s_addr + c / 2, pk);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tm_wait_st();
+        tc_before();
+        mbar_arrive(smem_u32(&p_bar[x]));
+        ++mine_done;
+      }
+      done += 2 * (int64_t)s.n;
+
+      // ---- the block, or this worker's part of it, is done ----
+      if (mine_done > 0) (void)wait(&o_bar[x], (mine_done - 1u) & 1u);
+      float scale0 = 1.f, scale1 = 0.f;                // of this slot's and the other's accumulator
+      int c0 = 0, c1 = D;
+      if (!s.shared) {
+        ml_s[x][0][row] = m;
+        ml_s[x][1][row] = l;
+        tc_before();
+        named_sync(1, 256);                            // either slot has waited for its own products
+        const float mo = ml_s[x ^ 1][0][row], lo = ml_s[x ^ 1][1][row], top = fmaxf(m, mo);
+        scale0 = m == -INFINITY ? (l == l ? 0.f : l) : fast_exp2(m - top);
+        scale1 = mo == -INFINITY ? (lo == lo ? 0.f : lo) : fast_exp2(mo - top);
+        l = (m == -INFINITY ? l : l * scale0) + (mo == -INFINITY ? lo : lo * scale1);
+        m = top;
+        c0 = x * (D / 2);
+        c1 = c0 + D / 2;
+      }
+      tc_after();
+      const bool complete = s.first && s.last;
+      const float inv = !complete ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+      float* pb = p.partials + (2 * (int64_t)blockIdx.x + (on_first ? 0 : 1)) * (int64_t)(kMmaRows * (D + 2));
+      const int64_t grow = live ? global_row(r) : 0;
+      for (int c = c0; c < c1; c += 32) {
+        uint32_t o[32];
+        tm_ld32(o_addr + c, o);
+        tm_wait_ld();
+        if (!s.shared) {
+          uint32_t o2[32];
+          tm_ld32(lane_addr + 256 + (x ^ 1) * 128 + c, o2);
+          tm_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            o[e] = __float_as_uint(__uint_as_float(o[e]) * scale0 + __uint_as_float(o2[e]) * scale1);
+        }
+        if (live && complete) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint4 w;
+            w.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+            w.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+            w.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+            w.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+            *reinterpret_cast<uint4*>(p.out + grow * D + c + e) = w;
+          }
+        } else if (live) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<uint4*>(pb + r * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+        __syncwarp();
+      }
+      if (live && (s.shared || x == 0)) {
+        if (!complete) {
+          pb[kMmaRows * D + r] = m;
+          pb[kMmaRows * (D + 1) + r] = l;
+        } else if (p.lse) {
+          p.lse[grow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
+        }
+      }
+      if (!s.shared) {
+        tc_before();
+        named_sync(1, 256);                            // the other slot has read this one's accumulator
+        tc_after();
+      }
+      on_first = false;
+      u += s.n;
+    }
+  }
+  pdl_launch_dependents();
+  tc_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+}  // namespace opw_tree

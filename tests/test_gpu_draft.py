@@ -241,6 +241,61 @@ def test_long_context_splits_over_workers(Hq, Hkv, D, T):
     assert torch.equal(out2, outs[0][0])
 
 
+@pytest.mark.parametrize("window", [0, 700, 4096])
+@pytest.mark.parametrize("Hq,Hkv,D,T", [(32, 8, 128, 26), (64, 8, 128, 33), (8, 2, 64, 40), (32, 8, 128, 6), (16, 2, 256, 11)])
+def test_many_ragged_sequences_each_of_many_tiles(Hq, Hkv, D, T, window):
+    """Workers whose shares span several sequences of many key tiles, with masked tiles at both ends (window and tree)."""
+    rng = np.random.default_rng(1600 + D + T + window)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(78)
+    n = 24
+    ctx = rng.integers(500, 9000, size=n)
+    size = rng.integers(T // 2, T + 1, size=n)
+    first = np.maximum(0, ctx + 1 - window) // 16 if window else np.zeros(n, np.int64)
+    pages = (ctx + size + 15) // 16
+    total = int((pages - first).sum())
+    perm = rng.permutation(total).astype(np.int32)
+    tab, at = np.full((n, int(pages.max())), -1, np.int32), 0
+    mask, pos = np.zeros((n, T), np.uint64), np.zeros((n, T), np.int32)
+    for b in range(n):
+        c = int(pages[b] - first[b])
+        tab[b, first[b]:pages[b]] = perm[at:at + c]
+        at += c
+        m, d = B.opw_tree_mask(random_tree(rng, int(size[b])))
+        mask[b, :size[b]], pos[b, :size[b]] = m, ctx[b] + np.array(d)
+    pool = torch.randn(total * Hkv * 2 * 16 * D, generator=g, device="cuda", dtype=torch.bfloat16)
+    q = torch.randn(n, T, Hq, D, generator=g, device="cuda", dtype=torch.bfloat16)
+    st = make_stage([pool], Hq, Hkv, D, n, tab.shape[1], window)
+    tree = B.TreeAttention(st, T)
+    out, lse = torch.empty_like(q), torch.empty(n, T, Hq, device="cuda")
+    args = (q, dev(mask), dev(pos), dev(ctx.astype(np.int32)), dev(size.astype(np.int32)), dev(tab))
+    tree.attention(0, *args, out, lse)
+    assert st.poll_error() == B.OPW_OK
+    idx = torch.arange(16 * D, device="cuda").view(16, D // 8, 8)
+    order = torch.stack([idx[t][torch.arange(D // 8, device="cuda") ^ (t & 7)].reshape(-1) for t in range(16)]).reshape(-1)
+    for b in range(n):
+        c, t, lo = int(ctx[b]), int(size[b]), int(first[b]) * 16
+        ids = dev(tab[b, first[b]:pages[b]]).long()
+        kv = pool.view(total, Hkv, 2, 16 * D)[ids][..., order].view(len(ids), Hkv, 2, 16, D)
+        kv = kv.permute(2, 1, 0, 3, 4).reshape(2, Hkv, len(ids) * 16, D)[:, :, :c + t - lo].double()
+        where = np.concatenate([np.arange(lo, c), pos[b, :t]])
+        see = np.ones((t, c + t - lo), bool)
+        for i in range(t):
+            see[i, c - lo:] = [(int(mask[b, i]) >> j) & 1 for j in range(t)]
+            if window:
+                see[i] &= where > pos[b, i] - window
+        x = torch.einsum("thgd,hkd->hgtk", q[b, :t].double().view(t, Hkv, -1, D), kv[0]) / math.sqrt(D)
+        x = x.masked_fill(~dev(see), -math.inf)
+        p = torch.softmax(x, -1)
+        want = torch.einsum("hgtk,hkd->thgd", p, kv[1]).reshape(t, Hq, D)
+        spread = torch.einsum("hgtk,hkd->thgd", p, kv[1].abs()).reshape(t, Hq, D)
+        big = torch.einsum("thgd,hkd->hgtk", q[b, :t].double().abs().view(t, Hkv, -1, D), kv[0].abs()).amax(-1) / math.sqrt(D)
+        ref = [a.cpu().numpy() for a in (want, torch.logsumexp(x, -1).permute(2, 0, 1).reshape(t, Hq), spread,
+                                         big.permute(2, 0, 1).reshape(t, Hq))]
+        check_tree(out[b, :t], lse[b, :t], ref, c + t)
+        assert (out[b, t:] == 0).all() and torch.isneginf(lse[b, t:]).all()
+
+
 def test_a_chain_of_one_is_a_decode_step():
     rng = np.random.default_rng(1300)
     Hq, Hkv, D, lens = 32, 8, 128, [0, 15, 16, 100, 999]
