@@ -109,26 +109,54 @@ __device__ __forceinline__ int find_sequence(const int64_t* cum, int batch, int6
   return lo;
 }
 
-// Which keys row r sees, apart from the end of the sequence.
+// Which keys a row sees.
 struct RowView {
-  uint64_t bits;         // drafted keys, those outside the window taken out
-  int32_t lo;            // first context key
+  uint64_t bits;         // drafted keys that exist, those outside the window taken out
+  int32_t lo, end, ctx;  // context keys [lo, end) (lo may be negative); drafted key m is key ctx + m
 };
-__device__ __forceinline__ RowView row_view(const TreeParams& p, int b, const Span& s, int node) {
+// (Called, not inlined, as all of the rare paths here: the kernels' loops have to stay in the instruction cache.  With everything
+// inlined the tensor-core kernel had 180 KB of code and spent most of its time fetching it.)
+__device__ __noinline__ RowView row_view(const uint64_t* mask, const int32_t* pos, int32_t window, int32_t ctx, int32_t n, int32_t tree,
+                                         int node) {
   RowView v;
-  v.bits = p.mask[(int64_t)b * p.nodes + node];
+  v.bits = mask[node];
   v.lo = 0;
-  if (s.tree < 64) v.bits &= (1ull << s.tree) - 1ull;
-  if (p.window > 0) {
-    const int32_t* pos = p.positions + (int64_t)b * p.nodes;
-    const int32_t own = pos[node] > s.ctx ? pos[node] : s.ctx;
-    v.lo = own - p.window + 1;               // may be negative
-    for (int m = 0; m < s.tree; ++m) {
-      const int32_t at = pos[m] > s.ctx ? pos[m] : s.ctx;
-      if (at < v.lo) v.bits &= ~(1ull << m);
-    }
+  v.ctx = ctx;
+  v.end = min(ctx, n);
+  const int32_t drafted = n - ctx;
+  if (drafted < 64) v.bits &= drafted > 0 ? (1ull << drafted) - 1ull : 0ull;
+  if (window > 0) {
+    v.lo = max(pos[node], ctx) - window + 1;
+#pragma unroll 1
+    for (int m = 0; m < tree; ++m)
+      if (max(pos[m], ctx) < v.lo) v.bits &= ~(1ull << m);
   }
   return v;
+}
+__device__ __forceinline__ RowView row_view(const TreeParams& p, int b, const Span& s, int node) {
+  return row_view(p.mask + (int64_t)b * p.nodes, p.positions + (int64_t)b * p.nodes, p.window, s.ctx, s.n, s.tree, node);
+}
+// The bounded wait with its loop out of line.
+__device__ __noinline__ bool mbar_wait_loop(uint32_t bar, uint32_t parity) {
+  const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (global_timer_ns() - t0 > kWaitLimitNs) return false;
+  }
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+  return mbar_try_wait(bar, parity) || mbar_wait_loop(bar, parity);
+}
+// Bit i: the row sees key base + i, i < 32.
+__device__ __forceinline__ uint32_t visible_word(const RowView& v, int32_t base) {
+  auto ones = [](int32_t k) { return k >= 32 ? ~0u : (1u << max(k, 0)) - 1u; };
+  uint32_t w = ones(v.end - base) & ~ones(v.lo - base);
+  const int32_t o = v.ctx - base;
+  if (o < 32 && o > -64) w |= o >= 0 ? (uint32_t)v.bits << o : (uint32_t)(v.bits >> -o);
+  return w;
 }
 // The first context key that the window hides from no node (a whole warp asks).
 __device__ __forceinline__ int32_t window_border(const TreeParams& p, int b, const Span& s, int lane) {
@@ -137,11 +165,6 @@ __device__ __forceinline__ int32_t window_border(const TreeParams& p, int b, con
   const int32_t* pos = p.positions + (int64_t)b * p.nodes;
   for (int i = lane; i < s.tree; i += 32) border = max(border, pos[i] - p.window + 1);
   return __reduce_max_sync(0xffffffffu, border);
-}
-__device__ __forceinline__ bool sees(const RowView& v, int32_t ctx, int32_t key) {
-  if (key < ctx) return key >= v.lo;
-  const uint32_t m = (uint32_t)(key - ctx);
-  return m < 64u && ((v.bits >> m) & 1ull);
 }
 __device__ __forceinline__ bool any_not_finite(const uint4& w) {   // of eight bf16
   auto bad = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
@@ -281,7 +304,7 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
         for (int nt = 0; nt < NT; ++nt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
       }
     }
-    if (!mbar_wait_bounded(bar0 + 8 * slot, phase)) { failed = true; break; }
+    if (!mbar_wait(bar0 + 8 * slot, phase)) { failed = true; break; }
     --inflight;
     const uint32_t tile = ring + slot * TILE;
     const int32_t key0 = (int32_t)(page & kPageBits) * kPage;
@@ -336,14 +359,12 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
         for (int h = 0; h < 2; ++h) {
           const int r = mt * 16 + h * 8 + qrow;
           if (r < rows && !(page & kBad)) {
-            const RowView v = row_view(p, b, sp, (rb * C::kRows + r) / p.G);
+            const uint32_t seen = visible_word(row_view(p, b, sp, (rb * C::kRows + r) / p.G), key0);
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int32_t key = key0 + nt * 8 + qcol + e;
-                if (key >= sp.n || !sees(v, sp.ctx, key)) x[mt][nt][2 * h + e] = -INFINITY;
-              }
+              for (int e = 0; e < 2; ++e)
+                if (!((seen >> (nt * 8 + qcol + e)) & 1u)) x[mt][nt][2 * h + e] = -INFINITY;
           } else {
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) x[mt][nt][2 * h] = x[mt][nt][2 * h + 1] = -INFINITY;
@@ -398,7 +419,7 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int r = mt * 16 + h * 8 + qrow;
-            if (r >= rows || !sees(row_view(p, b, sp, (rb * C::kRows + r) / p.G), sp.ctx, key0 + t)) continue;
+            if (r >= rows || !((visible_word(row_view(p, b, sp, (rb * C::kRows + r) / p.G), key0) >> t) & 1u)) continue;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -478,7 +499,7 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
     // A copy did not arrive in time: record it, then give every copy still in flight a bounded chance to land.
     if (lane == 0) atomicOr(p.status, kErrTimeout);
     for (int i = 0; i < inflight; ++i) {
-      (void)mbar_wait_bounded(bar0 + 8 * slot, phase);
+      (void)mbar_wait(bar0 + 8 * slot, phase);
       if (++slot == stages) { slot = 0; phase ^= 1u; }
     }
   }

@@ -1,6 +1,6 @@
 // Tree attention on the 5th-generation tensor cores, for trees whose rows (nodes x group) fill matrix tiles.
 //
-// One CTA per SM: two softmax warpgroups ("slots"), a TMA producer and an MMA issuer.  Slot s owns a query tile of
+// One CTA per SM: two softmax warpgroups ("slots"), two TMA producers (K, V) and an MMA issuer per slot.  Slot s owns a query tile of
 // 128 rows in shared memory and, in TMEM, a score tile S_s (128 x 128 fp32, its first 64 columns reused for P in bf16)
 // and an accumulator O_s (128 x D fp32).  Per key tile of 128 keys (eight pages):
 //     S_s = Q_s K^T      tcgen05.mma, both operands in shared memory
@@ -25,7 +25,7 @@
 
 namespace opw_tree {
 
-constexpr int kMmaThreads = 384;              // two softmax warpgroups; of the third, one warp produces and one issues
+constexpr int kMmaThreads = 384;              // two softmax warpgroups; in the third two producers and two MMA issuers
 constexpr int kMmaKeys = 128;                 // keys per tile
 constexpr int kMmaRows = 256;                 // rows per block
 constexpr float kRaise = 8.f;                 // log2 of how far a row's maximum may run ahead of the one in use
@@ -35,7 +35,7 @@ struct MmaTree {
   static constexpr int kHalves = D / 64;
   static constexpr uint32_t kHalfBytes = 128 * 128;           // 128 rows x 64 dimensions
   static constexpr uint32_t kPiece = kHalves * kHalfBytes;    // a K or V tile, and a query tile
-  static constexpr int kPieces = D == 128 ? 4 : 8;
+  static constexpr int kPieces = D == 128 ? 4 : 8;            // half of them for K, half for V
   static size_t smem(int batch) { return 1024 + (size_t)(kPieces + 2) * kPiece + (size_t)(batch + 1) * 8; }
 };
 
@@ -48,6 +48,28 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map
 }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
+// two fp32 at a time
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -99,6 +121,9 @@ __device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t* r) {
 #undef OPW_I8
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void named_arrive(int id, int threads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
@@ -115,6 +140,21 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t block_bytes)
 // kind::f16: fp32 accumulator, A and B bf16, A K-major, B K-major or MN-major (bit 16), N, M = 128
 __device__ __forceinline__ uint32_t idesc_of(int n, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
+__device__ __forceinline__ bool mbar_wait_or_dead(uint32_t bar, uint32_t parity, volatile int* dead, uint32_t* status) {
+  const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+  while (!*dead) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (global_timer_ns() - t0 > kWaitLimitNs) {
+      *dead = 1;
+      atomicOr(status, kErrTimeout);
+    }
+  }
+  return false;
 }
 
 // The row blocks of a worker's share, one after the other; every role walks the same list.
@@ -142,38 +182,41 @@ __device__ __forceinline__ Segment segment_at(const TreeParams& p, const int64_t
   s.shared = s.rows > 128;
   return s;
 }
-// The ring takes K 0, then K t + 1 and V t for every tile t: the order in which the products need them.
-__device__ __forceinline__ int64_t piece_k(int t) { return t == 0 ? 0 : 2 * (int64_t)t - 1; }
-__device__ __forceinline__ int64_t piece_v(int t, int n) { return t + 1 < n ? 2 * (int64_t)t + 2 : 2 * (int64_t)n - 1; }
-
 template <int D>
 __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_constant__ CUtensorMap map, const TreeParams p) {
   using C = MmaTree<D>;
-  constexpr int NP = C::kPieces;
+  constexpr int NS = C::kPieces / 2;                  // ring depth of K, and of V
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[NP], empty_bar[NP], s_bar[2], p_bar[2], o_bar[2], seg_bar, end_bar;
+  __shared__ __align__(8) uint64_t full_bar[2][NS], empty_bar[2][NS], s_bar[2], p_bar[2][2], o_bar[2], seg_bar, end_bar[2];
   __shared__ uint32_t tmem_slot;
-  __shared__ int piece_bad[NP], slot_bad[2];          // pages of a K tile that are bad: bit per page
+  __shared__ int piece_bad[NS], slot_bad[2];          // pages of a K tile that are bad: bit per page
   __shared__ uint32_t odd_s[2][4];                    // keys of a tile with values that are not finite
   __shared__ float ml_s[2][2][128];                   // m, l of the two slots, to be joined
+  __shared__ float zero_s;
   __shared__ volatile int dead_s;                     // a wait ran out: nobody waits any more
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t q_smem = base, ring = base + 2 * C::kPiece;
-  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)(NP + 2) * C::kPiece);
+  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)(C::kPieces + 2) * C::kPiece);
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
-    for (int i = 0; i < NP; ++i) { mbar_init(smem_u32(&full_bar[i]), 1); mbar_init(smem_u32(&empty_bar[i]), 1); }
+    for (int i = 0; i < 2 * NS; ++i) {
+      mbar_init(smem_u32(&full_bar[0][0] + i), 1);
+      mbar_init(smem_u32(&empty_bar[0][0] + i), 2);   // an arrival from each slot, or two from the one that has the tile
+    }
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&s_bar[s]), 2);              // the products' commit, and the issuer once slot_bad is set
-      mbar_init(smem_u32(&p_bar[s]), 128);
+      mbar_init(smem_u32(&p_bar[s][0]), 128);         // P of the tile's first and second 64 keys
+      mbar_init(smem_u32(&p_bar[s][1]), 128);
       mbar_init(smem_u32(&o_bar[s]), 1);
     }
     mbar_init(smem_u32(&seg_bar), 256);
-    mbar_init(smem_u32(&end_bar), 1);
+    mbar_init(smem_u32(&end_bar[0]), 1);
+    mbar_init(smem_u32(&end_bar[1]), 1);
     dead_s = 0;
+    zero_s = 0.f;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
@@ -184,7 +227,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   tc_before();
   scan_units(p, cum, kMmaRows, kMmaKeys);             // begins and ends with a barrier of the block
   tc_after();
-  const uint32_t tmem = tmem_slot;
+  constexpr uint32_t tmem = 0;                        // all 512 columns are this block's: they begin at column 0
   const int64_t U = cum[p.batch];
   const int64_t u0 = worker_begin(U, blockIdx.x, gridDim.x), u1 = worker_begin(U, blockIdx.x + 1, gridDim.x);
   pdl_wait();                                         // up to here only this step's lengths were read
@@ -195,28 +238,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   // same control flow (which depends on lengths only), so that no named barrier is left short.
   auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
     const uint32_t a = smem_u32(bar);
-    if (mbar_try_wait(a, parity)) return true;
-    const uint64_t t0 = global_timer_ns();
-    while (!dead_s) {
-      for (int i = 0; i < 64; ++i)
-        if (mbar_try_wait(a, parity)) return true;
-      if (global_timer_ns() - t0 > kWaitLimitNs) {
-        dead_s = 1;
-        atomicOr(p.status, kErrTimeout);
-      }
-    }
-    return false;
+    return mbar_try_wait(a, parity) || mbar_wait_or_dead(a, parity, &dead_s, p.status);
   };
 
   // Registers: 384 threads are launched with 168 each (64512); a softmax thread holds a row of 128 scores and wants
   // more, the third warpgroup needs little: 256 x 200 + 128 x 104 = 64512.
   if (warp >= 8) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-  if (warp == 8) {
-    // ---- producer ----
+  if (warp == 8 || warp == 11) {
+    // ---- producers: warp 8 copies the K tiles, warp 11 the V tiles ----
+    const int kv = warp == 8 ? 0 : 1;
     const uint64_t policy = l2_evict_first_policy();
     const int32_t nowhere = (int32_t)(p.num_pages * p.Hkv);   // one past the tensor's last tile: zeros
-    int64_t issued = 0;
+    uint32_t issued = 0;
     bool ok = true;
     for (int64_t u = u0; u < u1 && ok;) {
       const Segment s = segment_at(p, cum, u, u1);
@@ -225,106 +259,123 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         const int32_t lp = page0 + t * (kMmaKeys / kPage);
         return t < s.n && (int64_t)lp * kPage < s.sp.n ? __ldg(p.page_table + (int64_t)s.b * p.max_pages + lp) : -2;
       };
-      auto load = [&](int32_t id, int kv) {
-        const int st = (int)(issued % NP);
-        const int64_t round = issued / NP;
-        if (round > 0) ok = ok && wait(&empty_bar[st], (uint32_t)(round - 1) & 1u);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return;
+      int32_t id = fetch(0), next = fetch(1);
+      for (int t = 0; t < s.n; ++t) {
+        const int32_t after = fetch(t + 2);
         const bool good = id >= 0 && id < p.num_pages;
         const uint32_t bad = __ballot_sync(0xffffffffu, !good && id != -2) & 0xffu;
-        if (lane == 0) {
+        const int32_t tile = good ? (int32_t)((int64_t)id * p.Hkv + s.g) : nowhere;
+        int32_t tiles8[8];                             // one thread issues: a lane each would be eight divergent issues
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tiles8[i] = __shfl_sync(0xffffffffu, tile, i);
+        const uint32_t st = issued % NS, round = issued / NS;
+        if (round > 0) ok = ok && wait(&empty_bar[kv][st], (round - 1) & 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t bar = smem_u32(&full_bar[kv][st]), dst = ring + (uint32_t)(kv * NS + st) * C::kPiece;
           if (kv == 0) {
             piece_bad[st] = (int)bad;
             if (bad) atomicOr(p.status, kErrBadPage);
           }
-          mbar_expect_tx(smem_u32(&full_bar[st]), C::kPiece);
+          mbar_expect_tx(bar, C::kPiece);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int h = 0; h < C::kHalves; ++h)
+              tma_load_5d(dst + (uint32_t)h * C::kHalfBytes + (uint32_t)i * 2048u, &map, h, kv, tiles8[i], bar, policy);
         }
         __syncwarp();
-        if (lane < 8 * C::kHalves) {
-          const int half = lane >> 3;
-          tma_load_5d(ring + (uint32_t)st * C::kPiece + (uint32_t)half * C::kHalfBytes + (uint32_t)(lane & 7) * 2048u, &map, half, kv,
-                      good ? (int32_t)((int64_t)id * p.Hkv + s.g) : nowhere, smem_u32(&full_bar[st]), policy);
-        }
         ++issued;
-      };
-      int32_t id = fetch(0), next = fetch(1);
-      load(id, 0);
-      for (int t = 0; t < s.n && ok; ++t) {
-        const int32_t after = fetch(t + 2);
-        if (t + 1 < s.n) load(next, 0);
-        if (ok) load(id, 1);
         id = next;
         next = after;
       }
       u += s.n;
     }
     // every copy lands before the block's shared memory is given up
-    const int64_t from = issued > NP ? issued - NP : 0;
-    for (int64_t i = from; i < issued; ++i) {
+    for (uint32_t i = issued > NS ? issued - NS : 0; i < issued; ++i)
       for (int k = 0; k < 1 << 16; ++k)
-        if (mbar_try_wait(smem_u32(&full_bar[i % NP]), (uint32_t)(i / NP) & 1u)) break;
-    }
-  } else if (warp == 9) {
-    // ---- MMA issuer ----
-    if (lane == 0) {
+        if (mbar_try_wait(smem_u32(&full_bar[kv][i % NS]), (i / NS) & 1u)) break;
+  } else {
+    // ---- MMA issuers, a warp per slot: one's waits and bookkeeping hide under the other's products ----
+    const int x = __shfl_sync(0xffffffffu, warp, 0) - 9;
+    {
+      const uint32_t s_tm = x * 128, o_tm = 256 + x * 128;
+      constexpr uint32_t half = C::kHalfBytes >> 4;
       const uint32_t id_s = idesc_of(kMmaKeys, false), id_o = idesc_of(D, true);
-      int64_t done = 0;                                // pieces of the segments before
-      uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_seg = 0;
+      const uint32_t sb = smem_u32(&s_bar[x]), ob = smem_u32(&o_bar[x]);
+      uint32_t tiles = 0, mine = 0, n_seg = 0;         // tiles of all segments before; of this slot's; segments
+      const bool el = elect_one();
       bool ok = true;
       for (int64_t u = u0; u < u1 && ok;) {
         const Segment s = segment_at(p, cum, u, u1);
-        const int shift = s.shared ? 1 : 0, items = s.n << shift;
-        ok = ok && wait(&seg_bar, n_seg++ & 1u);
-        tc_after();
-        auto scores = [&](int i) {
-          const int t = i >> shift, x = i & 1;
-          const int64_t pc = done + piece_k(t);
-          const int st = (int)(pc % NP);
-          ok = ok && wait(&full_bar[st], (uint32_t)(pc / NP) & 1u);
-          if (!ok) return;
-          slot_bad[x] = piece_bad[st];
-          mbar_arrive(smem_u32(&s_bar[x]));
-          tc_after();
-          const uint32_t a = q_smem + (uint32_t)x * C::kPiece, b = ring + (uint32_t)st * C::kPiece;
-#pragma unroll
-          for (int h = 0; h < C::kHalves; ++h)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_ss(tmem + x * 128, desc_k(a + h * C::kHalfBytes) + 2u * k, desc_k(b + h * C::kHalfBytes) + 2u * k, id_s,
-                     (uint32_t)((h | k) != 0));
-          tc_commit(smem_u32(&s_bar[x]));
-          if (!s.shared || x == 1) tc_commit(smem_u32(&empty_bar[st]));
+        const int step = s.shared ? 1 : 2;
+        int bad = 0;
+        auto ready = [&](int t) {                      // K tile t has arrived
+          const uint32_t st = (tiles + t) % NS;
+          ok = ok && wait(&full_bar[0][st], ((tiles + t) / NS) & 1u);
+          bad = piece_bad[st];
         };
-        scores(0);
-        if (items > 1) scores(1);
-        for (int i = 0; i < items && ok; ++i) {
-          const int t = i >> shift, x = i & 1;
-          const int64_t pc = done + piece_v(t, s.n);
-          const int st = (int)(pc % NP);
-          ok = ok && wait(&p_bar[x], n_p[x]++ & 1u);
-          ok = ok && wait(&full_bar[st], (uint32_t)(pc / NP) & 1u);
-          if (!ok) break;
-          tc_after();
-          const uint64_t b = desc_mn(ring + (uint32_t)st * C::kPiece, C::kHalfBytes);
+        auto scores = [&](int t) {
+          const uint32_t st = (tiles + t) % NS;
+          if (el && ok) {
+            slot_bad[x] = bad;
+            mbar_arrive(sb);
+            const uint64_t q = desc_k(q_smem + x * C::kPiece), k = desc_k(ring + st * C::kPiece);
 #pragma unroll
-          for (int k = 0; k < kMmaKeys / 16; ++k) mma_ts(tmem + 256 + x * 128, tmem + x * 128 + 8 * k, b + 128u * k, id_o);
-          tc_commit(smem_u32(&o_bar[x]));
-          if (!s.shared || x == 1) tc_commit(smem_u32(&empty_bar[st]));
-          if (i + 2 < items) {
-            ok = ok && wait(&o_bar[x], n_o[x] & 1u);   // P, in the same columns as the next S, has been read
-            if (ok) scores(i + 2);
+            for (int j = 0; j < D / 16; ++j) {
+              const uint64_t at = (uint64_t)((j >> 2) * half + 2 * (j & 3));
+              mma_ss(s_tm, q + at, k + at, id_s, (uint32_t)(j != 0));
+            }
+            tc_commit(sb);
           }
-          ++n_o[x];
+        };
+        auto values = [&](uint32_t st, const int h) {  // half h of the tile's keys
+          if (el && ok) {
+            const uint64_t v = desc_mn(ring + (NS + st) * C::kPiece, C::kHalfBytes) + (uint64_t)(512 * h);
+            const uint32_t pt = s_tm + 32 * h;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_ts(o_tm, pt + 8 * k, v + (uint64_t)(128 * k), id_o);
+            if (h == 1) tc_commit(ob);
+          }
+        };
+        int t = s.shared ? 0 : x;
+        if (t < s.n) ready(t);
+        ok = ok && wait(&seg_bar, n_seg++ & 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_after();
+        if (t < s.n) scores(t);
+        for (; t < s.n && ok; t += step) {
+          // What does not depend on the softmax is waited for before it; from P's arrival on, every step is on the slot's
+          // critical path: PV, its end (P lies where the next scores go), QK.
+          const uint32_t st = (tiles + t) % NS;
+          ok = ok && wait(&full_bar[1][st], ((tiles + t) / NS) & 1u);
+          if (t + step < s.n) ready(t + step);
+          ok = ok && wait(&p_bar[x][0], mine & 1u);
+          tc_after();
+          values(st, 0);
+          ok = ok && wait(&p_bar[x][1], mine & 1u);
+          tc_after();
+          values(st, 1);
+          ok = ok && wait(&o_bar[x], mine++ & 1u);
+          tc_after();
+          if (t + step < s.n) scores(t + step);
+          if (el) {
+            mbar_arrive(smem_u32(&empty_bar[1][st]));
+            if (!s.shared) mbar_arrive(smem_u32(&empty_bar[1][st]));
+          }
+          ok = __all_sync(0xffffffffu, ok);
         }
-        done += 2 * (int64_t)s.n;
+        tiles += (uint32_t)s.n;
         u += s.n;
       }
-      tc_commit(smem_u32(&end_bar));                   // nothing is in flight when the TMEM is given back
-      for (int k = 0; k < 1 << 16; ++k)
-        if (mbar_try_wait(smem_u32(&end_bar), 0)) break;
+      if (el) {                                        // nothing is in flight when the TMEM is given back
+        tc_commit(smem_u32(&end_bar[x]));
+        for (int k = 0; k < 1 << 16; ++k)
+          if (mbar_try_wait(smem_u32(&end_bar[x]), 0)) break;
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -333,7 +384,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_addr + x * 128, o_addr = lane_addr + 256 + x * 128;
     uint32_t mine_done = 0;                            // tiles of this slot: phases of s_bar and o_bar
-    int64_t done = 0;
+    uint32_t tiles = 0;                                // of all segments before
     bool on_first = true;
     for (int64_t u = u0; u < u1;) {
       const Segment s = segment_at(p, cum, u, u1);
@@ -367,34 +418,51 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       tc_before();
       mbar_arrive(smem_u32(&seg_bar));
 
-      RowView view = {0ull, 0};
-      if (live) view = row_view(p, s.b, sp, node);
+      auto view_of_row = [&]() -> RowView {            // asked for at masked tiles only
+        if (!live) return {0ull, 0, 0, 0};
+        return row_view(p, s.b, sp, node);
+      };
       const int32_t border = window_border(p, s.b, sp, lane);
       float m = -INFINITY, l = 0.f;
-      const int shift = s.shared ? 1 : 0, items = s.n << shift;
-      for (int i = x; i < items; i += 2) {
-        const int t = i >> shift;
+      const uint64_t scale2 = pack2(p.scale_log2e, p.scale_log2e);
+      const bool idle = (warp & 3) * 32 + (s.shared ? x * 128 : 0) >= s.rows;   // none of the warp's rows exists
+      // The slots take turns at the exponentials (barriers 4 and 5: slot 0's, slot 1's turn).  Left alone they fall into
+      // step, both wait for the MUFU together and then both for the tensor core.
+      const int tiles0 = s.shared ? s.n : (s.n + 1) / 2, tiles1 = s.shared ? s.n : s.n / 2;
+      int turn = 0;
+      auto my_turn = [&]() { named_sync(4 + x, 256); };
+      auto next_turn = [&]() {
+        ++turn;
+        if (x == 0 ? turn <= tiles1 : turn < tiles0) named_arrive(5 - x, 256);
+      };
+      if (x == 1) named_arrive(4, 256);                // slot 0 begins
+      for (int t = s.shared ? 0 : x; t < s.n; t += s.shared ? 1 : 2) {
         const int32_t key0 = sp.lo / kPage * kPage + (s.t0 + t) * kMmaKeys;
         const bool edge = key0 + kMmaKeys > sp.ctx || key0 < border;
         (void)wait(&s_bar[x], mine_done & 1u);
         tc_after();
+        if (row == 0) {                                // K has been read
+          const uint32_t e = smem_u32(&empty_bar[0][(tiles + t) % NS]);
+          mbar_arrive(e);
+          if (!s.shared) mbar_arrive(e);
+        }
         if (edge) {
           // Values of keys that some row may not see.  The tile's warpgroup (slot 0's where they share it) clears the rows nobody
           // may read and looks for values that are not finite, a thread per key.  The V tile's barrier may only be asked
-          // once the scores are there: they were issued after the piece that had its place in the ring before was read,
-          // so its phase is the one meant and not the one before, of the same parity as the one before that.
-          const int64_t pc = done + piece_v(t, s.n);
-          const int st = (int)(pc % NP), id = s.shared ? 1 : 2 + x, threads = s.shared ? 256 : 128;
-          const uint32_t v = ring + (uint32_t)st * C::kPiece + (uint32_t)row * 128u;
+          // once the scores are there: they are issued after the tile that had its place in the ring before was read, so
+          // that a completed phase of this parity is the one meant.
+          const uint32_t st = (tiles + t) % NS;
+          const int id = s.shared ? 1 : 2 + x, threads = s.shared ? 256 : 128;
+          const uint32_t tile = ring + (NS + st) * C::kPiece, v = tile + (uint32_t)row * 128u;
           const bool mine = !s.shared || x == 0;
           const int ox = s.shared ? 0 : x;
-          (void)wait(&full_bar[st], (uint32_t)(pc / NP) & 1u);
+          (void)wait(&full_bar[1][st], ((tiles + t) / NS) & 1u);
           named_sync(id, threads);
           if (mine) {
             const int32_t key = key0 + row;
             const bool gone = key >= sp.n || key < sp.lo;
             bool found = false;
-#pragma unroll
+#pragma unroll 4
             for (int c = 0; c < D / 8; ++c) {
               const uint32_t a = v + (uint32_t)(c >> 3) * C::kHalfBytes + (uint32_t)(((c + lane) & 7) << 4);
               if (gone) {
@@ -412,16 +480,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
           named_sync(id, threads);
           const volatile uint32_t* odd = odd_s[ox];
           if (odd[0] | odd[1] | odd[2] | odd[3]) {     // rare: they leave the tile and are added to the rows that see them
-            if (mine_done > 0) (void)wait(&o_bar[x], (mine_done - 1u) & 1u);
-            tc_after();
-            const uint32_t tile = ring + (uint32_t)st * C::kPiece;
+            const RowView view = view_of_row();
+#pragma unroll 1
             for (int c0 = 0; c0 < D; c0 += 16) {
               uint32_t o[16];
               tm_ld16(o_addr + c0, o);
               tm_wait_ld();
+#pragma unroll 1
               for (int j = 0; j < 128; ++j) {
-                if (!((odd[j >> 5] >> (j & 31)) & 1u)) continue;
-                if (!live || key0 + j >= sp.n || !sees(view, sp.ctx, key0 + j)) continue;
+                if (!((odd[j >> 5] >> (j & 31)) & 1u) || !((visible_word(view, key0 + (j & ~31)) >> (j & 31)) & 1u)) continue;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                   const int d = c0 + e;
@@ -436,6 +503,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
             tm_wait_st();
             named_sync(id, threads);                   // everybody has read them
             if (mine && ((odd[warp & 3] >> lane) & 1u)) {
+#pragma unroll 1
               for (int d = 0; d < D; ++d) {
                 const uint32_t a = v + (uint32_t)(d >> 6) * C::kHalfBytes + (uint32_t)((d & 63) * 2);
                 if (!isfinite(bf16_at(a))) asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)0) : "memory");
@@ -445,31 +513,51 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
             named_sync(id, threads);
           }
         }
+        if (idle) {                                    // P stays what it is: these rows of O are never read
+          tc_before();
+          mbar_arrive(smem_u32(&p_bar[x][0]));
+          mbar_arrive(smem_u32(&p_bar[x][1]));
+          my_turn();
+          next_turn();
+          ++mine_done;
+          continue;
+        }
+        const int bad = *(volatile int*)&slot_bad[x];
+        uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
+        if (edge || bad) {
+          const RowView view = view_of_row();
+#pragma unroll 1
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t gone = ((bad >> (2 * w)) & 1 ? 0xffffu : 0u) | ((bad >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
+            const uint32_t word = visible_word(view, key0 + 32 * w) & ~gone;
+            if (w == 0) seen[0] = word;
+            else if (w == 1) seen[1] = word;
+            else if (w == 2) seen[2] = word;
+            else seen[3] = word;
+          }
+        }
         uint32_t sv[128];
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int c = 0; c < 128; c += 32) tm_ld32(s_addr + c, sv + c);
-        const int bad = *(volatile int*)&slot_bad[x];
         tm_wait_ld();
         if (edge || bad) {
 #pragma unroll
-          for (int j = 0; j < 128; ++j) {
-            const int32_t key = key0 + j;
-            const bool hide = key >= sp.n || !sees(view, sp.ctx, key) || ((bad >> (j >> 4)) & 1);
-            if (hide) sv[j] = 0xff800000u;             // -inf
-          }
+          for (int j = 0; j < 128; ++j)
+            if (!((seen[j >> 5] >> (j & 31)) & 1u)) sv[j] = 0xff800000u;   // -inf
         }
-        float top = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 128; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(sv[j]), __uint_as_float(sv[j + 1])));
-        top *= p.scale_log2e;
+        for (int j = 0; j < 128; j += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tops[e] = fmaxf(tops[e], fmaxf(__uint_as_float(sv[j + e]), __uint_as_float(sv[j + 4 + e])));
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2e;
         const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, raise)) {
+          // The scores were issued after the products before them had ended: O is complete.
           const bool shrink = raise && m != -INFINITY; // (with m = -inf, O and l are 0 or not finite: they stay)
           const float a = shrink ? fast_exp2(m - top) : 1.f;
           if (__any_sync(0xffffffffu, shrink)) {
-            (void)wait(&o_bar[x], (mine_done - 1u) & 1u);   // the products so far are in O
-            tc_after();
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < D; c += 16) {
               uint32_t o[16];
               tm_ld16(o_addr + c, o);
@@ -478,32 +566,47 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
               for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
               tm_st16(o_addr + c, o);
             }
-            tm_wait_st();
           }
           l *= a;
           if (raise) m = top;
         }
-        const float off = m == -INFINITY ? 0.f : -m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) {
+        my_turn();
+        // (the zero, from shared memory behind the barrier, keeps the exponentials from moving above it)
+        const float off1 = (m == -INFINITY ? 0.f : -m) + *(volatile float*)&zero_s;
+        const uint64_t off = pack2(off1, off1);
+        uint64_t sum[2] = {0ull, 0ull};
+        auto exps = [&](const int from) {              // 32 columns: P to TMEM, their sum
           uint32_t pk[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            const float e0 = fast_exp2(fmaf(__uint_as_float(sv[c + j]), p.scale_log2e, off));
-            const float e1 = fast_exp2(fmaf(__uint_as_float(sv[c + j + 1]), p.scale_log2e, off));
-            sum[(j >> 1) & 3] += e0 + e1;
+            float e0, e1;
+            unpack2(fma2(pack2(__uint_as_float(sv[from + j]), __uint_as_float(sv[from + j + 1])), scale2, off), e0, e1);
+            e0 = fast_exp2(e0);
+            e1 = fast_exp2(e1);
+            sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pack2(e0, e1));
             pk[j >> 1] = pack_bf16(e0, e1);            // rounded for the product only, the sum keeps 32 bits
           }
-          tm_st16(s_addr + c / 2, pk);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tm_st16(s_addr + from / 2, pk);
+        };
+        exps(0);
+        exps(32);
         tm_wait_st();
         tc_before();
-        mbar_arrive(smem_u32(&p_bar[x]));
+        mbar_arrive(smem_u32(&p_bar[x][0]));
+        exps(64);
+        exps(96);
+        next_turn();
+        tm_wait_st();
+        tc_before();
+        mbar_arrive(smem_u32(&p_bar[x][1]));
+        {
+          float a0, a1;
+          unpack2(add2(sum[0], sum[1]), a0, a1);
+          l += a0 + a1;
+        }
         ++mine_done;
       }
-      done += 2 * (int64_t)s.n;
+      tiles += (uint32_t)s.n;
 
       // ---- the block, or this worker's part of it, is done ----
       if (mine_done > 0) (void)wait(&o_bar[x], (mine_done - 1u) & 1u);
@@ -527,6 +630,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       const float inv = !complete ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
       float* pb = p.partials + (2 * (int64_t)blockIdx.x + (on_first ? 0 : 1)) * (int64_t)(kMmaRows * (D + 2));
       const int64_t grow = live ? global_row(r) : 0;
+#pragma unroll 1
       for (int c = c0; c < c1; c += 32) {
         uint32_t o[32];
         tm_ld32(o_addr + c, o);
