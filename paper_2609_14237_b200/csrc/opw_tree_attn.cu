@@ -68,6 +68,15 @@ cudaError_t launch_warp(const opw_stage_view& v, const opw_tree::TreeParams& p, 
 }
 
 template <int D>
+cudaError_t launch_combine(const opw_stage_view& v, const opw_tree::TreeCombineParams& c, int64_t blocks, bool deal,
+                           cudaStream_t stream) {
+  const int all = c.t.nodes * c.t.G, rows = all < c.row_block ? all : c.row_block, per = deal ? 8 : 32;
+  const dim3 grid((unsigned)blocks, (rows + per - 1) / per), block(opw_tree::kTreeCombineThreads);
+  return deal ? opw_launch(opw_tree::tree_combine_kernel<D, 4>, grid, block, 0, stream, v.pdl, 1, c)
+              : opw_launch(opw_tree::tree_combine_kernel<D, 1>, grid, block, 0, stream, v.pdl, 1, c);
+}
+
+template <int D>
 cudaError_t launch_mma(const opw_stage_view& v, const CUtensorMap& map, const opw_tree::TreeParams& p, cudaStream_t stream) {
   return opw_launch(opw_tree::tree_mma_kernel<D>, dim3(v.sms), dim3(opw_tree::kMmaThreads), opw_tree::MmaTree<D>::smem(p.batch), stream,
                     v.pdl, 1, map, p);
@@ -224,8 +233,11 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   else e = launch_warp<256, 1>(v, p, stream);
   if (e == cudaSuccess) {
     *v.launches += 1;
-    e = opw_launch(opw_tree::tree_combine_kernel, dim3((unsigned)batch * v.Hkv * c.max_blocks, v.D / opw_tree::kTreeCombineCols),
-                   dim3(opw_tree::kTreeCombineThreads), 0, stream, v.pdl, 1, c);
+    // Partials per row block, about: workers / blocks.  Above four the partials are dealt out to four groups of threads.
+    const int64_t blocks = (int64_t)batch * v.Hkv * c.max_blocks;
+    const bool deal = k.workers > 4 * blocks;
+    e = v.D == 64 ? launch_combine<64>(v, c, blocks, deal, stream)
+        : v.D == 128 ? launch_combine<128>(v, c, blocks, deal, stream) : launch_combine<256>(v, c, blocks, deal, stream);
   }
   if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   *v.launches += 1;

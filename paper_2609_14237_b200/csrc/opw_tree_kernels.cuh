@@ -99,6 +99,13 @@ __device__ __forceinline__ void scan_units(const TreeParams& p, int64_t* cum, in
   if (threadIdx.x == 0) cum[p.batch] = carry;
   __syncthreads();
 }
+// How many of the launched workers share U units: never more than there are units, and with single pages as units (a warp each) at least
+// four of them per worker -- a short step would otherwise leave a partial per page (63 of them at 1000 keys: the
+// combine took 110 us).
+__device__ __forceinline__ int64_t workers_for(int64_t U, int64_t launched, int keys) {
+  const int64_t most = keys == kPage ? U / 4 : U;
+  return most < 1 ? 1 : most < launched ? most : launched;
+}
 // the sequence that holds unit u < cum[batch]
 __device__ __forceinline__ int find_sequence(const int64_t* cum, int batch, int64_t u) {
   int lo = 0, hi = batch;                    // cum[lo] <= u < cum[hi]
@@ -205,7 +212,7 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
 
   scan_units(p, cum, C::kRows, kPage);
   const int64_t U = cum[p.batch];
-  const int64_t workers = (int64_t)gridDim.x * warps, worker = (int64_t)blockIdx.x * warps + warp;
+  const int64_t workers = workers_for(U, (int64_t)gridDim.x * warps, kPage), worker = (int64_t)warp * gridDim.x + blockIdx.x;
   const uint32_t ring = smem_u32(smem + (size_t)warp * stages * TILE);
   const uint32_t bar0 = smem_u32(bars + warp * stages);
   if (lane == 0) {
@@ -215,7 +222,8 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
   }
   __syncwarp();
 
-  const int64_t u0 = worker_begin(U, worker, workers), u1 = worker_begin(U, worker + 1, workers);
+  const bool idle = worker >= workers;         // (few units: the first workers are on different SMs)
+  const int64_t u0 = idle ? U : worker_begin(U, worker, workers), u1 = idle ? U : worker_begin(U, worker + 1, workers);
   struct Desc { int32_t tile; uint32_t page; };
   auto describe = [&](int64_t u) -> Desc {
     Desc d = {0, 0u};
@@ -514,79 +522,107 @@ struct TreeCombineParams {
   int64_t workers;
 };
 constexpr int kTreeCombineThreads = 256;
-constexpr int kTreeCombineCols = 32;         // columns of a block's slice
 
-// grid (batch * Hkv * max_blocks, D / 32).  Each block merges 32 columns of one row block: first every row's maximum and sum over
-// the partials, then the weighted sums, a thread per four columns of a row.
+// grid (batch * Hkv * max_blocks, rows of a block / (32 / kGroups)).  Eight threads own a row, every eighth float4 each, and walk the row's
+// partials once, carrying (O, m, l) like an online softmax; with kGroups > 1 (few rows of many partials each: the walk is a
+// chain of L2 round trips) the partials are dealt out to that many groups of threads, which meet in shared memory.
+template <int D, int kGroups>
 __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const TreeCombineParams c) {
+  constexpr int kRows = 32 / kGroups, V = D / 32, kDeep = V >= 4 ? 2 : 4;      // float4s a thread; partials in flight
   const TreeParams& p = c.t;
-  __shared__ float top_s[256], sum_s[256];
+  __shared__ int32_t slot_s[kTreeCombineThreads];
+  __shared__ float4 acc_s[kGroups > 1 ? kTreeCombineThreads : 1][kGroups > 1 ? V : 1];
+  __shared__ float2 ml_s[kGroups > 1 ? kTreeCombineThreads : 1];
   pdl_launch_dependents();
   pdl_wait();
   const int rb = blockIdx.x % c.max_blocks, bg = blockIdx.x / c.max_blocks, g = bg % p.Hkv, b = bg / p.Hkv;
+  const int64_t U = p.cum[p.batch], before = p.cum[b];           // asked for together with the lengths
   const Span s = span_of(p, b, c.row_block);
-  const int live = s.tree * p.G, r0 = rb * c.row_block;
-  const int r1 = min(r0 + c.row_block, p.nodes * p.G);           // rows [r0, r1) of this block exist in the output
-  const int D = c.D, col0 = blockIdx.y * kTreeCombineCols;
+  const int live = s.tree * p.G;
+  const int lane8 = threadIdx.x & 7, group = threadIdx.x / (8 * kRows);
+  const int r = blockIdx.y * kRows + (threadIdx.x >> 3) % kRows, R = rb * c.row_block + r;   // row of the block, of (b, g)
   const int32_t cnt = tiles_of(s, c.keys);
-  auto out_row = [&](int R) {
-    const int node = R / p.G;
-    return ((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
-  };
-  // rows of nodes that are not there (or of a sequence with no key to see): zeros
-  for (int i = threadIdx.x; i < (r1 - r0) * (kTreeCombineCols / 8); i += kTreeCombineThreads) {
-    const int R = r0 + i / (kTreeCombineCols / 8);
-    if (R < live && cnt > 0) continue;
-    *reinterpret_cast<uint4*>(p.out + out_row(R) * D + col0 + i % (kTreeCombineCols / 8) * 8) = make_uint4(0u, 0u, 0u, 0u);
-    if (p.lse && blockIdx.y == 0 && i % (kTreeCombineCols / 8) == 0) p.lse[out_row(R)] = -INFINITY;
+  const int node = R / p.G;
+  const int64_t row = ((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
+  if ((cnt == 0 || R >= live) && R < p.nodes * p.G && group == 0) {
+    // a node that is not there (or a sequence without a key): zeros
+#pragma unroll
+    for (int j = 0; j < V; ++j) *reinterpret_cast<uint2*>(p.out + row * D + (lane8 + 8 * j) * 4) = make_uint2(0u, 0u);
+    if (p.lse && lane8 == 0) p.lse[row] = -INFINITY;
   }
-  if (cnt == 0 || rb >= s.blocks) return;
-  const int64_t U = p.cum[p.batch];
-  const int64_t first = p.cum[b] + ((int64_t)g * s.blocks + rb) * cnt, end = first + cnt;
-  const int64_t wf = worker_of(U, first, c.workers), wl = worker_of(U, end - 1, c.workers);
+  if (cnt == 0 || rb * c.row_block + (int)blockIdx.y * kRows >= live) return;   // (the same for the whole block)
+  const int64_t workers = workers_for(U, c.workers, c.keys);
+  const int64_t first = before + ((int64_t)g * s.blocks + rb) * cnt, end = first + cnt;
+  const int64_t wf = worker_of(U, first, workers), wl = worker_of(U, end - 1, workers);
   if (wf == wl) return;                                          // finished by its worker
   const int64_t slot_floats = (int64_t)c.row_block * (D + 2);
-  auto part = [&](int64_t w) -> const float* {                   // worker w's partial of this row block, or null
-    const int64_t a = worker_begin(U, w, c.workers);
-    if (a == worker_begin(U, w + 1, c.workers)) return nullptr;
-    return p.partials + (2 * w + (a >= first ? 0 : 1)) * slot_floats;
+  float4 acc[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float m = -INFINITY, l = 0.f;
+  // A part that saw nothing has the maximum -inf, O = 0 and the sum 0 (or NaN, from a NaN score): weight 1.
+  auto merge = [&](float mw, float lw, const float4* v) {
+    const float top = fmaxf(m, mw), a = m == -INFINITY ? 1.f : fast_exp2(m - top), f = mw == -INFINITY ? 1.f : fast_exp2(mw - top);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      acc[j].x = acc[j].x * a + v[j].x * f; acc[j].y = acc[j].y * a + v[j].y * f;
+      acc[j].z = acc[j].z * a + v[j].z * f; acc[j].w = acc[j].w * a + v[j].w * f;
+    }
+    l = l * a + lw * f;
+    m = top;
   };
-  const int rows = min(live - r0, c.row_block);
-  for (int r = threadIdx.x; r < rows; r += kTreeCombineThreads) {
-    float m = -INFINITY, l = 0.f;
-    for (int64_t w = wf; w <= wl; ++w) {
-      const float* q = part(w);
-      if (!q) continue;
-      const float mw = __ldcg(q + c.row_block * D + r), lw = __ldcg(q + c.row_block * (D + 1) + r);
-      const float t = fmaxf(m, mw);
-      // a part that saw nothing has the maximum -inf and the sum 0 (or NaN, from a NaN score): weight 1
-      l = (m == -INFINITY ? l : l * exp2f(m - t)) + (mw == -INFINITY ? lw : lw * exp2f(mw - t));
-      m = t;
+  const bool merges = R < live && r < c.row_block;
+#pragma unroll 1
+  for (int64_t w0 = wf; w0 <= wl; w0 += kTreeCombineThreads) {
+    const int n = (int)min(wl - w0 + 1, (int64_t)kTreeCombineThreads);
+    if ((int)threadIdx.x < n) {                                  // the partial slot of worker w for this block
+      const int64_t w = w0 + threadIdx.x;                        // (no share is empty: there are at least as many units as workers)
+      slot_s[threadIdx.x] = (int32_t)(2 * w + (worker_begin(U, w, workers) >= first ? 0 : 1));
     }
-    top_s[r] = m;
-    sum_s[r] = l;
+    __syncthreads();
+    if (merges) {
+#pragma unroll 1
+      for (int i = group; i < n; i += kDeep * kGroups) {
+        float4 v[kDeep][V];
+        float mw[kDeep], lw[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+          const int k = i + u * kGroups;
+          const float* q = p.partials + (int64_t)slot_s[k < n ? k : i] * slot_floats;
+#pragma unroll
+          for (int j = 0; j < V; ++j) v[u][j] = __ldcg(reinterpret_cast<const float4*>(q + r * D) + lane8 + 8 * j);
+          mw[u] = __ldcg(q + c.row_block * D + r);
+          lw[u] = __ldcg(q + c.row_block * (D + 1) + r);
+        }
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+          if (i + u * kGroups < n) merge(mw[u], lw[u], v[u]);
+      }
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < rows * (kTreeCombineCols / 4); i += kTreeCombineThreads) {
-    const int r = i / (kTreeCombineCols / 4), col = col0 + i % (kTreeCombineCols / 4) * 4;
-    const float m = top_s[r], l = sum_s[r];
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int64_t w = wf; w <= wl; ++w) {
-      const float* q = part(w);
-      if (!q) continue;
-      const float mw = __ldcg(q + c.row_block * D + r);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(q + r * D + col));
-      const float f = mw == -INFINITY ? 1.f : exp2f(mw - m);     // -inf: this part of the row saw nothing, O is 0
-      acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+  if (kGroups > 1) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc_s[threadIdx.x][j] = acc[j];
+    ml_s[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll 1
+    for (int k = 1; k < kGroups; ++k) {                          // in group order: deterministic
+      const int other = threadIdx.x + k * 8 * kRows;
+      merge(ml_s[other].x, ml_s[other].y, acc_s[other]);
     }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  }
+  if (!merges) return;
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
     uint2 w2;
-    w2.x = pack_bf16(acc.x * inv, acc.y * inv);
-    w2.y = pack_bf16(acc.z * inv, acc.w * inv);
-    const int64_t row = out_row(r0 + r);
-    *reinterpret_cast<uint2*>(p.out + row * D + col) = w2;
-    if (p.lse && col == 0) p.lse[row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
+    w2.x = pack_bf16(acc[j].x * inv, acc[j].y * inv);
+    w2.y = pack_bf16(acc[j].z * inv, acc[j].w * inv);
+    *reinterpret_cast<uint2*>(p.out + row * D + (lane8 + 8 * j) * 4) = w2;
   }
+  if (p.lse && lane8 == 0) p.lse[row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
 }
 
 }  // namespace opw_tree

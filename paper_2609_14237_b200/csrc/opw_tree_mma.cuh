@@ -229,7 +229,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   tc_after();
   constexpr uint32_t tmem = 0;                        // all 512 columns are this block's: they begin at column 0
   const int64_t U = cum[p.batch];
-  const int64_t u0 = worker_begin(U, blockIdx.x, gridDim.x), u1 = worker_begin(U, blockIdx.x + 1, gridDim.x);
+  const int64_t workers = workers_for(U, gridDim.x, kMmaKeys);
+  const bool spare = blockIdx.x >= workers;           // fewer units than blocks
+  const int64_t u0 = spare ? U : worker_begin(U, blockIdx.x, workers), u1 = spare ? U : worker_begin(U, blockIdx.x + 1, workers);
   pdl_wait();                                         // up to here only this step's lengths were read
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i <= p.batch; i += kMmaThreads) p.cum[i] = cum[i];
