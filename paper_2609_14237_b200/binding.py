@@ -549,8 +549,18 @@ def opw_tree_attention(tree: int, layer: int, batch: int, nodes: int, q: int, tr
                                     stream), "opw_tree_attention")
 
 
+_layer_arrays: dict = {}
+
+
 def _layer_array(layers: Sequence[int]):
-    return (ctypes.c_int32 * len(layers))(*layers)
+    """The C array of a list of layers; the few lists a program uses are made once each."""
+    key = tuple(layers)
+    arr = _layer_arrays.get(key)
+    if arr is None:
+        arr = (ctypes.c_int32 * len(key))(*key)
+        if len(_layer_arrays) < 256:
+            _layer_arrays[key] = arr
+    return arr
 
 
 def opw_kv_commit(stage: int, layers: Sequence[int], batch: int, nodes: int, accepted: int, accepted_lens: int, ctx_lens: int,
@@ -575,18 +585,13 @@ def opw_kv_free_pages(stage: int, refcounts: int, num_pages: int, free_list: Opt
     _check(lib().opw_kv_free_pages(stage, refcounts, num_pages, free_list, max_list, count, stream), "opw_kv_free_pages")
 
 
-def _need(where: str, device, dtype, *tensors) -> None:
-    """The kernels see addresses only: a tensor of another type, device or memory order would be read wrongly."""
+def _need(where: str, index: int, dtype, count: int, *tensors) -> None:
+    """The kernels see addresses only: a tensor of another type, device, size or memory order would be read wrongly.
+    count: elements each must have (-1: any)."""
     for t in tensors:
-        if t.dtype is not dtype or t.device != device or not t.is_contiguous():
-            raise ValueError(f"{where}: expected contiguous {dtype} tensors on {device}, got {t.dtype} on {t.device}"
-                             f"{'' if t.is_contiguous() else ' (not contiguous)'}")
-
-
-def _shapes(where: str, *pairs) -> None:
-    for t, shape in pairs:
-        if t.shape != shape:
-            raise ValueError(f"{where}: expected a tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+        if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or (count >= 0 and t.numel() != count):
+            raise ValueError(f"{where}: expected contiguous {dtype} tensors{f' of {count} elements' if count >= 0 else ''} on cuda:{index}, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (not contiguous)'}")
 
 
 class Rope:
@@ -636,7 +641,10 @@ class Stage:
         cfg.workspace = base
         cfg.workspace_bytes = nbytes
         self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
-        self.max_pages_per_seq = max_pages_per_seq
+        self.max_pages_per_seq, self.layer_num_pages = max_pages_per_seq, [int(n) for n in layer_num_pages]
+        # what the short calls look up every time
+        self.index, self._i32, self._bf16 = dev.index or 0, torch.int32, torch.bfloat16
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self.handle = opw_attn_stage_create(cfg)
 
     @staticmethod
@@ -682,88 +690,78 @@ class Stage:
 
     def _own_stream(self):
         """The current stream of the stage's device, whichever device is current."""
-        import torch
-
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self.index)
 
     def _table_ok(self, where, page_table, rows):
-        import torch
-
-        _need(where, self.device, torch.int32, page_table)
+        _need(where, self.index, self._i32, -1, page_table)
         if page_table.dim() != 2 or page_table.shape[0] < rows or page_table.shape[1] != self.max_pages_per_seq:
             raise ValueError(f"{where}: page_table must be [at least {rows}, {self.max_pages_per_seq}]")
 
     def rope_append(self, layer, rope, q, k, v, seq, slots, positions, page_table, q_out):
         """Rotate q into q_out, append rotated k and v to the cache; q, k, v: [rows, heads, head_dim], rows may be strided
         (views into one projection).  q = q_out = None: keys and values only."""
-        import torch
-
-        where, D, rows = "rope_append", self.head_dim, seq.shape[0]
-        _need(where, self.device, torch.int32, seq, slots, positions)
-        _shapes(where, (slots, seq.shape), (positions, seq.shape), (k, (rows, self.num_kv_heads, D)), (v, (rows, self.num_kv_heads, D)))
+        where, D, rows, dev = "rope_append", self.head_dim, seq.shape[0], self.index
+        _need(where, dev, self._i32, rows, seq, slots, positions)
         self._table_ok(where, page_table, 1)
-        for t in (k, v) if q is None else (q, k, v):
-            if t.dtype is not torch.bfloat16 or t.device != self.device or t.stride(2) != 1 or t.stride(1) != D:
-                raise ValueError(f"{where}: q, k, v must be bfloat16 on {self.device} with contiguous heads")
+        for t, heads in ((k, self.num_kv_heads), (v, self.num_kv_heads)) if q is None else (
+                (q, self.num_q_heads), (k, self.num_kv_heads), (v, self.num_kv_heads)):
+            if t.dtype is not self._bf16 or t.get_device() != dev or t.shape != (rows, heads, D) or t.stride()[1:] != (D, 1):
+                raise ValueError(f"{where}: q, k, v must be bfloat16 [{rows}, heads, {D}] on {self.device} with contiguous heads")
         if q is not None:
-            _need(where, self.device, torch.bfloat16, q_out)
-            _shapes(where, (q, (rows, self.num_q_heads, D)), (q_out, q.shape))
-        if rope.table.device != self.device:
+            _need(where, dev, self._bf16, rows * self.num_q_heads * D, q_out)
+        if rope.table.get_device() != dev:
             raise ValueError(f"{where}: the rotary table is on {rope.table.device}")
         opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(),
                         None if q is None else q.data_ptr(), 0 if q is None else q.stride(0), k.data_ptr(), k.stride(0),
                         v.data_ptr(), v.stride(0), seq.data_ptr(), slots.data_ptr(), positions.data_ptr(), page_table.data_ptr(),
-                        None if q is None else q_out.data_ptr(), self._own_stream())
+                        None if q is None else q_out.data_ptr(), self._raw_stream(dev))
 
     def kv_commit(self, layers, accepted, accepted_lens, ctx_lens, page_table, new_lens=None):
-        """Move the rows of the accepted nodes together behind each sequence's context, in all of `layers`."""
-        import torch
-
-        where, batch = "kv_commit", ctx_lens.shape[0]
-        _need(where, self.device, torch.int32, accepted, accepted_lens, ctx_lens)
-        _shapes(where, (accepted_lens, ctx_lens.shape), (accepted, (batch, accepted.shape[1])))
+        """Move the rows of the accepted nodes together behind each sequence's context, in all of `layers`.  accepted: int32
+        [batch, nodes]; the lengths: int32 [batch]."""
+        where, batch, dev = "kv_commit", ctx_lens.shape[0], self.index
+        nodes = accepted.shape[1]
+        _need(where, dev, self._i32, batch, ctx_lens, accepted_lens)
+        _need(where, dev, self._i32, batch * nodes, accepted)
         self._table_ok(where, page_table, batch)
+        new = None
         if new_lens is not None:
-            _need(where, self.device, torch.int32, new_lens)
-            _shapes(where, (new_lens, ctx_lens.shape))
-        opw_kv_commit(self.handle, layers, batch, accepted.shape[1], accepted.data_ptr(), accepted_lens.data_ptr(),
-                      ctx_lens.data_ptr(), page_table.data_ptr(), None if new_lens is None else new_lens.data_ptr(),
-                      self._own_stream())
+            _need(where, dev, self._i32, batch, new_lens)
+            new = new_lens.data_ptr()
+        opw_kv_commit(self.handle, layers, batch, nodes, accepted.data_ptr(), accepted_lens.data_ptr(), ctx_lens.data_ptr(),
+                      page_table.data_ptr(), new, self._raw_stream(dev))
 
     def kv_fork(self, layers, src_rows, dst_rows, lens, new_pages, page_table, refcounts):
         """Let table rows dst_rows share the first lens tokens of src_rows; a last partial page is copied to new_pages."""
-        import torch
-
-        where, n = "kv_fork", src_rows.shape[0]
-        _need(where, self.device, torch.int32, src_rows, dst_rows, lens, new_pages, refcounts)
-        _shapes(where, (dst_rows, (n,)), (lens, (n,)), (new_pages, (n,)))
+        where, n, dev = "kv_fork", src_rows.shape[0], self.index
+        _need(where, dev, self._i32, n, src_rows, dst_rows, lens, new_pages)
+        _need(where, dev, self._i32, -1, refcounts)
         self._table_ok(where, page_table, 1)
-        page = self.num_kv_heads * 2 * 16 * self.head_dim
-        if refcounts.numel() < min(self.pools[i].numel() // page for i in layers):
+        if refcounts.numel() < min(self.layer_num_pages[i] for i in layers):
             raise ValueError(f"{where}: refcounts must have an entry per page")
         opw_kv_fork(self.handle, layers, n, src_rows.data_ptr(), dst_rows.data_ptr(), lens.data_ptr(), new_pages.data_ptr(),
-                    page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(), self._own_stream())
+                    page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(), self._raw_stream(dev))
 
     def kv_release(self, rows, keep_lens, page_table, refcounts):
         """Drop the pages of table rows behind their first keep_lens tokens (None: all)."""
-        import torch
-
-        where = "kv_release"
-        _need(where, self.device, torch.int32, rows, refcounts)
+        where, n, dev = "kv_release", rows.shape[0], self.index
+        _need(where, dev, self._i32, n, rows)
+        _need(where, dev, self._i32, -1, refcounts)
         self._table_ok(where, page_table, 1)
+        keep = None
         if keep_lens is not None:
-            _need(where, self.device, torch.int32, keep_lens)
-            _shapes(where, (keep_lens, rows.shape))
-        opw_kv_release(self.handle, rows.shape[0], rows.data_ptr(), None if keep_lens is None else keep_lens.data_ptr(),
-                       page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(), refcounts.numel(), self._own_stream())
+            _need(where, dev, self._i32, n, keep_lens)
+            keep = keep_lens.data_ptr()
+        opw_kv_release(self.handle, n, rows.data_ptr(), keep, page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(),
+                       refcounts.numel(), self._raw_stream(dev))
 
     def kv_free_pages(self, refcounts, free_list, count):
         """List the pages nobody holds, ascending, in free_list; their number in count."""
-        import torch
-
-        _need("kv_free_pages", self.device, torch.int32, refcounts, free_list, count)
+        dev = self.index
+        _need("kv_free_pages", dev, self._i32, -1, refcounts, free_list)
+        _need("kv_free_pages", dev, self._i32, 1, count)
         opw_kv_free_pages(self.handle, refcounts.data_ptr(), refcounts.numel(), free_list.data_ptr(), free_list.numel(),
-                          count.data_ptr(), self._own_stream())
+                          count.data_ptr(), self._raw_stream(dev))
 
     def packed_host_buffers(self, batch):
         """One pinned host buffer holding q, k_new, v_new, positions at the packed offsets;
@@ -803,7 +801,7 @@ class TreeAttention:
     def __init__(self, stage: Stage, max_nodes: int = OPW_TREE_MAX_NODES):
         import torch
 
-        self.stage, self.max_nodes = stage, max_nodes
+        self.stage, self.max_nodes, self._i64, self._f32 = stage, max_nodes, torch.int64, torch.float32
         nbytes = opw_tree_attn_workspace_bytes(stage.handle, max_nodes)
         if nbytes == 0:
             raise OpwError(OPW_ERR_INVALID_ARG, "opw_tree_attn_workspace_bytes")
@@ -814,22 +812,22 @@ class TreeAttention:
     def attention(self, layer, q, tree_mask, positions, ctx_lens, tree_lens, page_table, out, lse=None):
         """q, out: bf16 [batch, nodes, Hq, D]; tree_mask: int64 [batch, nodes] (the bits of a uint64); positions: int32
         [batch, nodes]; lse: fp32 [batch, nodes, Hq] or None."""
-        import torch
-
         where, st = "tree attention", self.stage
-        batch, nodes = q.shape[0], q.shape[1]
-        _need(where, st.device, torch.bfloat16, q, out)
-        _need(where, st.device, torch.int32, positions, ctx_lens, tree_lens)
-        _need(where, st.device, torch.int64, tree_mask)
-        _shapes(where, (q, (batch, nodes, st.num_q_heads, st.head_dim)), (out, q.shape), (tree_mask, (batch, nodes)),
-                (positions, (batch, nodes)), (ctx_lens, (batch,)), (tree_lens, (batch,)))
+        batch, nodes, dev = q.shape[0], q.shape[1], st.index
+        if q.shape != (batch, nodes, st.num_q_heads, st.head_dim):
+            raise ValueError(f"{where}: q must be [batch, nodes, {st.num_q_heads}, {st.head_dim}], got {tuple(q.shape)}")
+        _need(where, dev, st._bf16, batch * nodes * st.num_q_heads * st.head_dim, q, out)
+        _need(where, dev, st._i32, batch, ctx_lens, tree_lens)
+        _need(where, dev, st._i32, batch * nodes, positions)
+        _need(where, dev, self._i64, batch * nodes, tree_mask)
         st._table_ok(where, page_table, batch)
+        lse_ptr = None
         if lse is not None:
-            _need(where, st.device, torch.float32, lse)
-            _shapes(where, (lse, (batch, nodes, st.num_q_heads)))
+            _need(where, dev, self._f32, batch * nodes * st.num_q_heads, lse)
+            lse_ptr = lse.data_ptr()
         opw_tree_attention(self.handle, layer, batch, nodes, q.data_ptr(), tree_mask.data_ptr(), positions.data_ptr(),
-                           ctx_lens.data_ptr(), tree_lens.data_ptr(), page_table.data_ptr(), out.data_ptr(),
-                           None if lse is None else lse.data_ptr(), st._own_stream())
+                           ctx_lens.data_ptr(), tree_lens.data_ptr(), page_table.data_ptr(), out.data_ptr(), lse_ptr,
+                           st._raw_stream(dev))
 
     def close(self):
         if getattr(self, "handle", None):
