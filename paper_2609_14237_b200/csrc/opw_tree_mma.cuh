@@ -1,14 +1,15 @@
 // Tree attention on the 5th-generation tensor cores, for trees whose rows (nodes x group) fill matrix tiles.
 //
-// One CTA per SM: two softmax warpgroups ("slots"), two TMA producers (K, V) and an MMA issuer per slot.  Slot s owns a query tile of
-// 128 rows in shared memory and, in TMEM, a score tile S_s (128 x 128 fp32, its first 64 columns reused for P in bf16)
-// and an accumulator O_s (128 x D fp32).  Per key tile of 128 keys (eight pages):
-//     S_s = Q_s K^T      tcgen05.mma, both operands in shared memory
-//     P_s = 2^(S - m)    a thread per row: S from TMEM to registers, P back to TMEM
-//     O_s += P_s V       tcgen05.mma, P from TMEM, V from shared memory
+// One CTA per SM: two softmax warpgroups ("slots"), two TMA producers (K, V) and an MMA issuer per slot.  Slot s owns a query
+// tile of 128 rows in shared memory and, in TMEM, two score buffers S (128 x 64 fp32, their first 32 columns reused for P in
+// bf16) and an accumulator O (128 x D fp32).  Per key tile of 64 keys (four pages):
+//     S = Q K^T      tcgen05.mma, both operands in shared memory
+//     P = 2^(S - m)  a thread per row: S from TMEM to registers, P back to TMEM
+//     O += P V       tcgen05.mma, P from TMEM, V from shared memory
+// With two buffers the products of one tile run under the softmax of the next.  (With one buffer of 128 keys a slot's tile was
+// a chain of softmax, PV and QK of 4000 cycles in which every unit idled half the time.)
 // A row block of up to 256 rows shares every key tile between the slots (slot s = rows 128 s ...).  One of up to 128
-// rows gives each slot every other key tile, and the two (O, m, l) are joined at the end.  Either way one slot's
-// softmax runs under the other's products.
+// rows gives each slot every other key tile, and the two (O, m, l) are joined at the end.
 //
 // The cache needs no re-layout: a cached row's 16-byte words are permuted by XOR with slot mod 8, which is what the
 // 128-byte swizzle of the tensor core expects of rows of 128 bytes.  So K (K-major) and V (MN-major) tiles are copied by plain TMA
@@ -26,17 +27,20 @@
 namespace opw_tree {
 
 constexpr int kMmaThreads = 384;              // two softmax warpgroups; in the third two producers and two MMA issuers
-constexpr int kMmaKeys = 128;                 // keys per tile
+constexpr int kMmaKeys = 64;                  // keys per tile
+constexpr int kTilePages = kMmaKeys / 16;
+constexpr int kBadRing = 32;
 constexpr int kMmaRows = 256;                 // rows per block
 constexpr float kRaise = 8.f;                 // log2 of how far a row's maximum may run ahead of the one in use
 
 template <int D>
 struct MmaTree {
   static constexpr int kHalves = D / 64;
-  static constexpr uint32_t kHalfBytes = 128 * 128;           // 128 rows x 64 dimensions
-  static constexpr uint32_t kPiece = kHalves * kHalfBytes;    // a K or V tile, and a query tile
-  static constexpr int kPieces = D == 128 ? 4 : 8;            // half of them for K, half for V
-  static size_t smem(int batch) { return 1024 + (size_t)(kPieces + 2) * kPiece + (size_t)(batch + 1) * 8; }
+  static constexpr uint32_t kHalfBytes = kMmaKeys * 128;      // 64 dimensions of a K or V tile
+  static constexpr uint32_t kPiece = kHalves * kHalfBytes;    // a K or V tile
+  static constexpr uint32_t kQHalf = 128 * 128, kQTile = kHalves * kQHalf;   // a query tile: 128 rows
+  static constexpr int kPieces = D == 128 ? 8 : 16;           // half of them for K, half for V
+  static size_t smem(int batch) { return 1024 + (size_t)kPieces * kPiece + 2 * kQTile + (size_t)(batch + 1) * 8; }
 };
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int c1, int c3, int c4, uint32_t bar, uint64_t pol) {
@@ -70,6 +74,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -187,18 +194,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   using C = MmaTree<D>;
   constexpr int NS = C::kPieces / 2;                  // ring depth of K, and of V
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[2][NS], empty_bar[2][NS], s_bar[2], p_bar[2][2], o_bar[2], seg_bar, end_bar[2];
+  __shared__ __align__(8) uint64_t full_bar[2][NS], empty_bar[2][NS], s_bar[2][2], p_bar[2][2], o_bar[2][2], seg_bar, end_bar[2];
   __shared__ uint32_t tmem_slot;
-  __shared__ int piece_bad[NS], slot_bad[2];          // pages of a K tile that are bad: bit per page
-  __shared__ uint32_t odd_s[2][4];                    // keys of a tile with values that are not finite
+  __shared__ int bad_s[kBadRing];                     // pages of a tile that are bad: bit per page; by tile, the last few
+  __shared__ uint32_t odd_s[2][4];                    // keys of a tile with values that are not finite, by warp
   __shared__ float ml_s[2][2][128];                   // m, l of the two slots, to be joined
   __shared__ float zero_s;
   __shared__ volatile int dead_s;                     // a wait ran out: nobody waits any more
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t q_smem = base, ring = base + 2 * C::kPiece;
-  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)(C::kPieces + 2) * C::kPiece);
+  const uint32_t q_smem = base, ring = base + 2 * C::kQTile;
+  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)C::kPieces * C::kPiece + 2 * C::kQTile);
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
@@ -206,11 +213,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       mbar_init(smem_u32(&full_bar[0][0] + i), 1);
       mbar_init(smem_u32(&empty_bar[0][0] + i), 2);   // an arrival from each slot, or two from the one that has the tile
     }
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(smem_u32(&s_bar[s]), 2);              // the products' commit, and the issuer once slot_bad is set
-      mbar_init(smem_u32(&p_bar[s][0]), 128);         // P of the tile's first and second 64 keys
-      mbar_init(smem_u32(&p_bar[s][1]), 128);
-      mbar_init(smem_u32(&o_bar[s]), 1);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&s_bar[0][0] + i), 1);
+      mbar_init(smem_u32(&p_bar[0][0] + i), 4);       // a lane of each warp
+      mbar_init(smem_u32(&o_bar[0][0] + i), 1);
     }
     mbar_init(smem_u32(&seg_bar), 256);
     mbar_init(smem_u32(&end_bar[0]), 1);
@@ -256,20 +262,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     bool ok = true;
     for (int64_t u = u0; u < u1 && ok;) {
       const Segment s = segment_at(p, cum, u, u1);
-      const int32_t page0 = s.sp.lo / kPage + s.t0 * (kMmaKeys / kPage) + (lane & 7);
+      const int32_t page0 = s.sp.lo / kPage + s.t0 * kTilePages + (lane & (kTilePages - 1));
       auto fetch = [&](int t) -> int32_t {            // this lane's page of tile t: raw id, or -2 where there is none
-        const int32_t lp = page0 + t * (kMmaKeys / kPage);
+        const int32_t lp = page0 + t * kTilePages;
         return t < s.n && (int64_t)lp * kPage < s.sp.n ? __ldg(p.page_table + (int64_t)s.b * p.max_pages + lp) : -2;
       };
       int32_t id = fetch(0), next = fetch(1);
       for (int t = 0; t < s.n; ++t) {
         const int32_t after = fetch(t + 2);
         const bool good = id >= 0 && id < p.num_pages;
-        const uint32_t bad = __ballot_sync(0xffffffffu, !good && id != -2) & 0xffu;
+        const uint32_t bad = __ballot_sync(0xffffffffu, !good && id != -2) & ((1u << kTilePages) - 1u);
         const int32_t tile = good ? (int32_t)((int64_t)id * p.Hkv + s.g) : nowhere;
-        int32_t tiles8[8];                             // one thread issues: a lane each would be eight divergent issues
+        int32_t pages[kTilePages];                     // one thread issues: a lane each would issue one after the other, slowly
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tiles8[i] = __shfl_sync(0xffffffffu, tile, i);
+        for (int i = 0; i < kTilePages; ++i) pages[i] = __shfl_sync(0xffffffffu, tile, i);
         const uint32_t st = issued % NS, round = issued / NS;
         if (round > 0) ok = ok && wait(&empty_bar[kv][st], (round - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
@@ -277,15 +283,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         if (elect_one()) {
           const uint32_t bar = smem_u32(&full_bar[kv][st]), dst = ring + (uint32_t)(kv * NS + st) * C::kPiece;
           if (kv == 0) {
-            piece_bad[st] = (int)bad;
+            bad_s[issued % kBadRing] = (int)bad;       // (rewritten long after every row has looked: the ring of K is shorter)
             if (bad) atomicOr(p.status, kErrBadPage);
           }
           mbar_expect_tx(bar, C::kPiece);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kTilePages; ++i)
 #pragma unroll
             for (int h = 0; h < C::kHalves; ++h)
-              tma_load_5d(dst + (uint32_t)h * C::kHalfBytes + (uint32_t)i * 2048u, &map, h, kv, tiles8[i], bar, policy);
+              tma_load_5d(dst + (uint32_t)h * C::kHalfBytes + (uint32_t)i * 2048u, &map, h, kv, pages[i], bar, policy);
         }
         __syncwarp();
         ++issued;
@@ -303,74 +309,66 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     const int x = __shfl_sync(0xffffffffu, warp, 0) - 9;
     {
       const uint32_t s_tm = x * 128, o_tm = 256 + x * 128;
-      constexpr uint32_t half = C::kHalfBytes >> 4;
+      constexpr uint32_t q_half = C::kQHalf >> 4, k_half = C::kHalfBytes >> 4;
       const uint32_t id_s = idesc_of(kMmaKeys, false), id_o = idesc_of(D, true);
-      const uint32_t sb = smem_u32(&s_bar[x]), ob = smem_u32(&o_bar[x]);
       uint32_t tiles = 0, mine = 0, n_seg = 0;         // tiles of all segments before; of this slot's; segments
+      // The slot's n-th tile uses buffer n % 2, and phase n / 2 of that buffer's barriers.  This loop is the kernel's
+      // pulse: a wait costs about 100 cycles here even when it need not wait, so there are four per tile and nothing else.
       const bool el = elect_one();
-      bool ok = true;
-      for (int64_t u = u0; u < u1 && ok;) {
-        const Segment s = segment_at(p, cum, u, u1);
-        const int step = s.shared ? 1 : 2;
-        int bad = 0;
-        auto ready = [&](int t) {                      // K tile t has arrived
-          const uint32_t st = (tiles + t) % NS;
-          ok = ok && wait(&full_bar[0][st], ((tiles + t) / NS) & 1u);
-          bad = piece_bad[st];
-        };
-        auto scores = [&](int t) {
-          const uint32_t st = (tiles + t) % NS;
-          if (el && ok) {
-            slot_bad[x] = bad;
-            mbar_arrive(sb);
-            const uint64_t q = desc_k(q_smem + x * C::kPiece), k = desc_k(ring + st * C::kPiece);
+      const uint64_t q = desc_k(q_smem + x * C::kQTile), k0 = desc_k(ring), v0 = desc_mn(ring + NS * C::kPiece, C::kHalfBytes);
+      const uint32_t sb = smem_u32(&s_bar[x][0]), ob = smem_u32(&o_bar[x][0]), pb = smem_u32(&p_bar[x][0]);
+      const uint32_t kf = smem_u32(&full_bar[0][0]), vf = smem_u32(&full_bar[1][0]), ve = smem_u32(&empty_bar[1][0]);
+      auto wait_at = [&](uint32_t bar, uint32_t parity) {
+        return mbar_try_wait(bar, parity) || mbar_wait_or_dead(bar, parity, &dead_s, p.status);
+      };
+      auto scores = [&](uint32_t tile, uint32_t n) -> bool {   // the slot's n-th tile, number `tile` of the worker
+        const uint32_t st = tile % NS;
+        if (!wait_at(kf + 8 * st, (tile / NS) & 1u)) return false;
+        const uint64_t k = k0 + (uint64_t)(st * (C::kPiece >> 4));
+        const uint32_t d = s_tm + 64 * (n & 1u);
+        if (el) {
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-              const uint64_t at = (uint64_t)((j >> 2) * half + 2 * (j & 3));
-              mma_ss(s_tm, q + at, k + at, id_s, (uint32_t)(j != 0));
-            }
-            tc_commit(sb);
-          }
-        };
-        auto values = [&](uint32_t st, const int h) {  // half h of the tile's keys
-          if (el && ok) {
-            const uint64_t v = desc_mn(ring + (NS + st) * C::kPiece, C::kHalfBytes) + (uint64_t)(512 * h);
-            const uint32_t pt = s_tm + 32 * h;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mma_ts(o_tm, pt + 8 * k, v + (uint64_t)(128 * k), id_o);
-            if (h == 1) tc_commit(ob);
-          }
-        };
-        int t = s.shared ? 0 : x;
-        if (t < s.n) ready(t);
-        ok = ok && wait(&seg_bar, n_seg++ & 1u);
-        ok = __all_sync(0xffffffffu, ok);
-        tc_after();
-        if (t < s.n) scores(t);
-        for (; t < s.n && ok; t += step) {
-          // What does not depend on the softmax is waited for before it; from P's arrival on, every step is on the slot's
-          // critical path: PV, its end (P lies where the next scores go), QK.
-          const uint32_t st = (tiles + t) % NS;
-          ok = ok && wait(&full_bar[1][st], ((tiles + t) / NS) & 1u);
-          if (t + step < s.n) ready(t + step);
-          ok = ok && wait(&p_bar[x][0], mine & 1u);
-          tc_after();
-          values(st, 0);
-          ok = ok && wait(&p_bar[x][1], mine & 1u);
-          tc_after();
-          values(st, 1);
-          ok = ok && wait(&o_bar[x], mine++ & 1u);
-          tc_after();
-          if (t + step < s.n) scores(t + step);
-          if (el) {
-            mbar_arrive(smem_u32(&empty_bar[1][st]));
-            if (!s.shared) mbar_arrive(smem_u32(&empty_bar[1][st]));
-          }
-          ok = __all_sync(0xffffffffu, ok);
+          for (int j = 0; j < D / 16; ++j)
+            mma_ss(d, q + (uint64_t)((j >> 2) * q_half + 2 * (j & 3)), k + (uint64_t)((j >> 2) * k_half + 2 * (j & 3)), id_s,
+                   (uint32_t)(j != 0));
+          tc_commit(sb + 8 * (n & 1u));
         }
-        tiles += (uint32_t)s.n;
+        return true;
+      };
+      for (int64_t u = u0; u < u1;) {
+        const Segment s = segment_at(p, cum, u, u1);
+        const uint32_t step = s.shared ? 1u : 2u, end = tiles + (uint32_t)s.n;
+        uint32_t t = s.shared ? tiles : tiles + x;
+        if (!wait(&seg_bar, n_seg++ & 1u)) break;
+        tc_after();
+        if (t < end && !scores(t, mine)) break;
+        if (t + step < end && !scores(t + step, mine + 1)) break;
+        bool ok = true;
+        for (; t < end; t += step, ++mine) {
+          const uint32_t st = t % NS, buf = mine & 1u, phase = (mine >> 1) & 1u;
+          ok = wait_at(vf + 8 * st, (t / NS) & 1u) && wait_at(pb + 8 * buf, phase);
+          if (!ok) break;
+          tc_after();
+          if (el) {
+            const uint64_t v = v0 + (uint64_t)(st * (C::kPiece >> 4));
+            const uint32_t pt = s_tm + 64 * buf;
+#pragma unroll
+            for (int k = 0; k < kMmaKeys / 16; ++k) mma_ts(o_tm, pt + 8 * k, v + (uint64_t)(128 * k), id_o);
+            tc_commit(ob + 8 * buf);
+          }
+          ok = wait_at(ob + 8 * buf, phase);           // P lies where the next scores of this buffer go
+          if (!ok) break;
+          if (el) mbar_arrive_n(ve + 8 * st, step);   // (two arrivals free a tile: one slot's of each, or both of one)
+          if (t + 2 * step < end) {
+            ok = scores(t + 2 * step, mine + 2);
+            if (!ok) break;
+          }
+        }
+        if (!ok) break;
+        tiles = end;
         u += s.n;
       }
+      __syncwarp();
       if (el) {                                        // nothing is in flight when the TMEM is given back
         tc_commit(smem_u32(&end_bar[x]));
         for (int k = 0; k < 1 << 16; ++k)
@@ -384,8 +382,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     // ---- softmax: thread = one row of slot x ----
     const int x = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t s_addr = lane_addr + x * 128, o_addr = lane_addr + 256 + x * 128;
-    uint32_t mine_done = 0;                            // tiles of this slot: phases of s_bar and o_bar
+    const uint32_t o_addr = lane_addr + 256 + x * 128;
+    uint32_t mine = 0;                                 // tiles of this slot so far
+    // (the products of the slot's n-th tile are in O)
+    auto wait_products = [&](uint32_t n) { (void)wait(&o_bar[x][n & 1u], (n >> 1) & 1u); };
     uint32_t tiles = 0;                                // of all segments before
     bool on_first = true;
     for (int64_t u = u0; u < u1;) {
@@ -399,13 +399,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         return ((int64_t)s.b * p.nodes + nn) * p.Hq + (int64_t)s.g * p.G + (RR - nn * p.G);
       };
       // queries to shared memory, in the layout of a K-major swizzled operand; rows that are not there: zeros
-      const uint32_t qs = q_smem + (uint32_t)x * C::kPiece;
+      const uint32_t qs = q_smem + (uint32_t)x * C::kQTile;
 #pragma unroll 4
       for (int i = row; i < 128 * (D / 8); i += 128) {
         const int qr = i / (D / 8), c = i % (D / 8), rr = s.shared ? x * 128 + qr : qr;
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
         if (rr < s.rows) w = *(reinterpret_cast<const uint4*>(p.q + global_row(rr) * D) + c);
-        const uint32_t a = qs + (uint32_t)(c >> 3) * C::kHalfBytes + (uint32_t)qr * 128u + (uint32_t)(((c & 7) ^ (qr & 7)) << 4);
+        const uint32_t a = qs + (uint32_t)(c >> 3) * C::kQHalf + (uint32_t)qr * 128u + (uint32_t)(((c & 7) ^ (qr & 7)) << 4);
         asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
       }
       fence_proxy_async();
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       const uint64_t scale2 = pack2(p.scale_log2e, p.scale_log2e);
       const bool idle = (warp & 3) * 32 + (s.shared ? x * 128 : 0) >= s.rows;   // none of the warp's rows exists
       // The slots take turns at the exponentials (barriers 4 and 5: slot 0's, slot 1's turn).  Left alone they fall into
-      // step, both wait for the MUFU together and then both for the tensor core.
+      // step, wait for the MUFU together and then leave it idle together.
       const int tiles0 = s.shared ? s.n : (s.n + 1) / 2, tiles1 = s.shared ? s.n : s.n / 2;
       int turn = 0;
       auto my_turn = [&]() { named_sync(4 + x, 256); };
@@ -441,12 +441,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       for (int t = s.shared ? 0 : x; t < s.n; t += s.shared ? 1 : 2) {
         const int32_t key0 = sp.lo / kPage * kPage + (s.t0 + t) * kMmaKeys;
         const bool edge = key0 + kMmaKeys > sp.ctx || key0 < border;
-        (void)wait(&s_bar[x], mine_done & 1u);
+        const uint32_t buf = mine & 1u, s_addr = lane_addr + x * 128 + 64 * buf;
+        (void)wait(&s_bar[x][buf], (mine >> 1) & 1u);
         tc_after();
         if (row == 0) {                                // K has been read
-          const uint32_t e = smem_u32(&empty_bar[0][(tiles + t) % NS]);
-          mbar_arrive(e);
-          if (!s.shared) mbar_arrive(e);
+          mbar_arrive_n(smem_u32(&empty_bar[0][(tiles + t) % NS]), s.shared ? 1u : 2u);
         }
         if (edge) {
           // Values of keys that some row may not see.  The tile's warpgroup (slot 0's where they share it) clears the rows nobody
@@ -455,24 +454,29 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
           // that a completed phase of this parity is the one meant.
           const uint32_t st = (tiles + t) % NS;
           const int id = s.shared ? 1 : 2 + x, threads = s.shared ? 256 : 128;
-          const uint32_t tile = ring + (NS + st) * C::kPiece, v = tile + (uint32_t)row * 128u;
-          const bool mine = !s.shared || x == 0;
+          const uint32_t tile = ring + (NS + st) * C::kPiece;
+          const bool mine_v = !s.shared || x == 0;
           const int ox = s.shared ? 0 : x;
+          // thread = 64 dimensions of a key: warps 0 and 1 the first, 2 and 3 the second (head_dim 128)
+          const int vk = row & 63, vh = row >> 6;
+          const uint32_t v = tile + (uint32_t)vh * C::kHalfBytes + (uint32_t)vk * 128u;
           (void)wait(&full_bar[1][st], ((tiles + t) / NS) & 1u);
           named_sync(id, threads);
-          if (mine) {
-            const int32_t key = key0 + row;
+          if (mine_v) {
+            const int32_t key = key0 + vk;
             const bool gone = key >= sp.n || key < sp.lo;
             bool found = false;
-#pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-              const uint32_t a = v + (uint32_t)(c >> 3) * C::kHalfBytes + (uint32_t)(((c + lane) & 7) << 4);
-              if (gone) {
-                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
-              } else {
-                uint4 w;
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a));
-                found |= any_not_finite(w);
+            if (vh < C::kHalves) {
+#pragma unroll 2
+              for (int c = 0; c < 8; ++c) {
+                const uint32_t a = v + (uint32_t)(((c + lane) & 7) << 4);
+                if (gone) {
+                  asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+                } else {
+                  uint4 w;
+                  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a));
+                  found |= any_not_finite(w);
+                }
               }
             }
             const uint32_t bal = __ballot_sync(0xffffffffu, found);
@@ -481,16 +485,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
           }
           named_sync(id, threads);
           const volatile uint32_t* odd = odd_s[ox];
-          if (odd[0] | odd[1] | odd[2] | odd[3]) {     // rare: they leave the tile and are added to the rows that see them
+          const uint32_t odd0 = odd[0] | odd[2], odd1 = odd[1] | odd[3];   // keys 0..31, 32..63
+          if (odd0 | odd1) {                           // rare: they leave the tile and are added to the rows that see them
+            if (mine > 0) wait_products(mine - 1);
+            tc_after();
             const RowView view = view_of_row();
+            const uint32_t add0 = odd0 & visible_word(view, key0), add1 = odd1 & visible_word(view, key0 + 32);
 #pragma unroll 1
             for (int c0 = 0; c0 < D; c0 += 16) {
               uint32_t o[16];
               tm_ld16(o_addr + c0, o);
               tm_wait_ld();
 #pragma unroll 1
-              for (int j = 0; j < 128; ++j) {
-                if (!((odd[j >> 5] >> (j & 31)) & 1u) || !((visible_word(view, key0 + (j & ~31)) >> (j & 31)) & 1u)) continue;
+              for (int j = 0; j < kMmaKeys; ++j) {
+                if (!(((j < 32 ? add0 : add1) >> (j & 31)) & 1u)) continue;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                   const int d = c0 + e;
@@ -504,10 +512,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
             }
             tm_wait_st();
             named_sync(id, threads);                   // everybody has read them
-            if (mine && ((odd[warp & 3] >> lane) & 1u)) {
+            if (mine_v && vh < C::kHalves && (((vk < 32 ? odd0 : odd1) >> (vk & 31)) & 1u)) {
 #pragma unroll 1
-              for (int d = 0; d < D; ++d) {
-                const uint32_t a = v + (uint32_t)(d >> 6) * C::kHalfBytes + (uint32_t)((d & 63) * 2);
+              for (int d = 0; d < 64; ++d) {
+                const uint32_t a = v + (uint32_t)(d * 2);
                 if (!isfinite(bf16_at(a))) asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)0) : "memory");
               }
             }
@@ -517,48 +525,47 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         }
         if (idle) {                                    // P stays what it is: these rows of O are never read
           tc_before();
-          mbar_arrive(smem_u32(&p_bar[x][0]));
-          mbar_arrive(smem_u32(&p_bar[x][1]));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][buf]));
           my_turn();
           next_turn();
-          ++mine_done;
+          ++mine;
           continue;
         }
-        const int bad = *(volatile int*)&slot_bad[x];
-        uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
+        const int bad = *(volatile int*)&bad_s[(tiles + t) % kBadRing];
+        uint32_t seen0 = ~0u, seen1 = ~0u;
         if (edge || bad) {
           const RowView view = view_of_row();
-#pragma unroll 1
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t gone = ((bad >> (2 * w)) & 1 ? 0xffffu : 0u) | ((bad >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
-            const uint32_t word = visible_word(view, key0 + 32 * w) & ~gone;
-            if (w == 0) seen[0] = word;
-            else if (w == 1) seen[1] = word;
-            else if (w == 2) seen[2] = word;
-            else seen[3] = word;
-          }
+          auto gone = [&](int page) { return ((bad >> page) & 1 ? 0xffffu : 0u) | ((bad >> (page + 1)) & 1 ? 0xffff0000u : 0u); };
+          seen0 = visible_word(view, key0) & ~gone(0);
+          seen1 = visible_word(view, key0 + 32) & ~gone(2);
         }
-        uint32_t sv[128];
-        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) tm_ld32(s_addr + c, sv + c);
+        uint32_t sv[kMmaKeys];
+        tm_ld32(s_addr, sv);
+        tm_ld32(s_addr + 32, sv + 32);
         tm_wait_ld();
         if (edge || bad) {
 #pragma unroll
-          for (int j = 0; j < 128; ++j)
-            if (!((seen[j >> 5] >> (j & 31)) & 1u)) sv[j] = 0xff800000u;   // -inf
+          for (int j = 0; j < 32; ++j) {
+            if (!((seen0 >> j) & 1u)) sv[j] = 0xff800000u;             // -inf
+            if (!((seen1 >> j) & 1u)) sv[32 + j] = 0xff800000u;
+          }
         }
+        float tops[4];
 #pragma unroll
-        for (int j = 0; j < 128; j += 8)
+        for (int e = 0; e < 4; ++e) tops[e] = fmaxf(__uint_as_float(sv[e]), __uint_as_float(sv[4 + e]));
+#pragma unroll
+        for (int j = 8; j < kMmaKeys; j += 8)
 #pragma unroll
           for (int e = 0; e < 4; ++e) tops[e] = fmaxf(tops[e], fmaxf(__uint_as_float(sv[j + e]), __uint_as_float(sv[j + 4 + e])));
         const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale_log2e;
         const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, raise)) {
-          // The scores were issued after the products before them had ended: O is complete.
           const bool shrink = raise && m != -INFINITY; // (with m = -inf, O and l are 0 or not finite: they stay)
           const float a = shrink ? fast_exp2(m - top) : 1.f;
           if (__any_sync(0xffffffffu, shrink)) {
+            wait_products(mine - 1);
+            tc_after();
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
               uint32_t o[16];
@@ -577,41 +584,35 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         const float off1 = (m == -INFINITY ? 0.f : -m) + *(volatile float*)&zero_s;
         const uint64_t off = pack2(off1, off1);
         uint64_t sum[2] = {0ull, 0ull};
-        auto exps = [&](const int from) {              // 32 columns: P to TMEM, their sum
+#pragma unroll
+        for (int c = 0; c < kMmaKeys; c += 32) {
           uint32_t pk[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
             float e0, e1;
-            unpack2(fma2(pack2(__uint_as_float(sv[from + j]), __uint_as_float(sv[from + j + 1])), scale2, off), e0, e1);
+            unpack2(fma2(pack2(__uint_as_float(sv[c + j]), __uint_as_float(sv[c + j + 1])), scale2, off), e0, e1);
             e0 = fast_exp2(e0);
             e1 = fast_exp2(e1);
             sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pack2(e0, e1));
             pk[j >> 1] = pack_bf16(e0, e1);            // rounded for the product only, the sum keeps 32 bits
           }
-          tm_st16(s_addr + from / 2, pk);
-        };
-        exps(0);
-        exps(32);
-        tm_wait_st();
-        tc_before();
-        mbar_arrive(smem_u32(&p_bar[x][0]));
-        exps(64);
-        exps(96);
+          tm_st16(s_addr + c / 2, pk);
+        }
         next_turn();
         tm_wait_st();
         tc_before();
-        mbar_arrive(smem_u32(&p_bar[x][1]));
-        {
-          float a0, a1;
-          unpack2(add2(sum[0], sum[1]), a0, a1);
-          l += a0 + a1;
-        }
-        ++mine_done;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&p_bar[x][buf]));
+        float a0, a1;
+        unpack2(add2(sum[0], sum[1]), a0, a1);
+        l += a0 + a1;
+        ++mine;
       }
       tiles += (uint32_t)s.n;
 
       // ---- the block, or this worker's part of it, is done ----
-      if (mine_done > 0) (void)wait(&o_bar[x], (mine_done - 1u) & 1u);
+      if (mine > 1) wait_products(mine - 2);
+      if (mine > 0) wait_products(mine - 1);
       float scale0 = 1.f, scale1 = 0.f;                // of this slot's and the other's accumulator
       int c0 = 0, c1 = D;
       if (!s.shared) {
