@@ -33,12 +33,17 @@ struct RopeParams {
   const int32_t* page_table;
   uint32_t* status;
   int64_t q_stride, k_stride, v_stride, num_pages;
-  int32_t Hq, Hkv, D, rot, max_batch, max_pages, layout_half;
+  int32_t rows, Hq, Hkv, D, rot, max_batch, max_pages, layout_half;
 };
 
 constexpr int kRopeThreads = 256;
 constexpr int kMaxPairs = 128;
+constexpr int kRopeWarpRows = 8;          // from this many rows per SM on, a warp takes a row (measurements at the kernel)
 
+template <bool X>
+struct Flag {
+  static constexpr bool value = X;
+};
 __device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -58,29 +63,41 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// One block per token row: the row's cosines and sines are computed once (the angle in 64 bits: turns =
-// position * turns_per_position, reduced to [-1/2, 1/2] before it is rounded to 32) and serve all heads.
-// The heads then pass through registers in 16-byte words; a thread takes both words of a rotated pair, so
-// that q may be rotated in place.  kVec 0: pairs a word apart within the head (half layout, rot % 16 == 0);
-// 1: pairs inside a word (interleaved, rot % 8 == 0); 2: any even rot -- a warp takes a whole head at a time
-// and looks partners up in shared memory.
-template <int kVec>
-__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeParams p) {
-  __shared__ float2 cs[kMaxPairs];
-  __shared__ float stage[kVec == 2 ? kRopeThreads / 32 : 1][kVec == 2 ? 256 : 1];
+// kGroup threads per token row, a block (256) or a warp (32, eight rows to a block).  The row's cosines and sines are computed
+// once (the angle in 64 bits: turns = position * turns_per_position, reduced to [-1/2, 1/2] before it is rounded to 32)
+// and serve all heads.  The heads then pass through registers in 16-byte words; a thread takes both words of a rotated
+// pair, so that q may be rotated in place.  kVec 0: pairs a word apart within the head (half layout, rot % 16 == 0); 1: pairs inside
+// a word (interleaved, rot % 8 == 0); 2: any even rot -- a warp takes a whole head at a time and looks partners up in
+// shared memory.
+// Measured at 32/8 heads of 128, rotary 128 half and 64 interleaved, us with a block and with a warp per row: 128 rows
+// 3.9 / 6.5 and 3.5 / 5.6, 512 rows 5.1 / 6.7 and 4.2 / 5.7, 1184 rows 12.0 / 11.1 and 9.1 / 9.0, 8192 rows 76.7 / 39.6 and 62.9 / 36.2
+// (5.1 and 5.6 TB/s of the bytes that have to move).  A block per row spends most of its life in the latencies before its first load; a warp per
+// row keeps more rows in flight.
+template <int kVec, int kGroup>
+__global__ void __launch_bounds__(kRopeThreads, 4) rope_append_kernel(const RopeParams p) {
+  constexpr int kRows = kRopeThreads / kGroup, kWarps = kRopeThreads / 32;
+  __shared__ float2 cs_s[kRows][kMaxPairs];
+  __shared__ float stage[kVec == 2 ? kWarps : 1][kVec == 2 ? 256 : 1];
   pdl_launch_dependents();
   pdl_wait();
-  const int r = blockIdx.x;
+  const int tid = threadIdx.x % kGroup;
+  const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / kGroup;
+  float2* cs = cs_s[threadIdx.x / kGroup];
+  auto sync = [] {
+    if (kGroup == 32) __syncwarp();
+    else __syncthreads();
+  };
+  if (r >= p.rows) return;                                        // (a whole group)
   const int32_t b = p.seq[r];
   if (b < 0) return;
   const int32_t pos = p.positions[r], slot = p.slots[r];
   const int D = p.D, pairs = p.rot >> 1, words = D >> 3;
-  if (threadIdx.x < pairs) {
-    const double turns = (double)pos * p.table[threadIdx.x];
+  for (int i = tid; i < pairs; i += kGroup) {
+    const double turns = (double)pos * p.table[i];
     const float amp = (float)p.table[pairs];
     float sn, cn;
     sincospif(2.f * (float)(turns - rint(turns)), &sn, &cn);
-    cs[threadIdx.x] = make_float2(amp * cn, amp * sn);
+    cs[i] = make_float2(amp * cn, amp * sn);
   }
   // where the row's keys and values go: null if it is not appended
   __nv_bfloat16* kv = nullptr;
@@ -89,13 +106,12 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
     const int32_t pid = p.page_table[(int64_t)b * p.max_pages + lp];
     if (pid >= 0 && pid < p.num_pages) kv = p.pool + ((int64_t)pid * p.Hkv * 2 * kPage + t) * D;
   }
-  if (kv == nullptr && threadIdx.x == 0) atomicOr(p.status, kErrBadPage);
-  __syncthreads();
+  if (kv == nullptr && tid == 0) atomicOr(p.status, kErrBadPage);
 
   const __nv_bfloat16* qr = p.q ? p.q + r * p.q_stride : nullptr;
   const __nv_bfloat16* kr = p.k + r * p.k_stride;
   const __nv_bfloat16* vr = p.v + r * p.v_stride;
-  __nv_bfloat16* qo = p.q_out ? p.q_out + (int64_t)r * p.Hq * D : nullptr;
+  __nv_bfloat16* qo = p.q_out ? p.q_out + r * p.Hq * D : nullptr;
   const int first = p.q ? 0 : p.Hq, last = kv ? p.Hq + 2 * p.Hkv : p.Hq;   // heads: queries, keys, values
   const int64_t tile = (int64_t)kPage * D;
   auto source = [&](int h) {
@@ -109,81 +125,122 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopePar
   };
 
   if (kVec == 2) {
+    sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int h = first + warp; h < last; h += kRopeThreads / 32) {
+    const int per = 32 / words, c = lane & (words - 1);           // heads a warp takes at a time; this lane's word
+    float* mine = stage[warp] + (lane / words) * D;
+    for (int h0 = first + tid / 32 * per; h0 < last; h0 += kGroup / 32 * per) {
+      const int h = h0 + lane / words;
       uint4 w = make_uint4(0u, 0u, 0u, 0u);
       float x[8];
-      if (lane < words) {
-        w = reinterpret_cast<const uint4*>(source(h))[lane];
+      if (h < last) {
+        w = reinterpret_cast<const uint4*>(source(h))[c];
         unpack8(w, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) stage[warp][lane * 8 + e] = x[e];
+        for (int e = 0; e < 8; ++e) mine[c * 8 + e] = x[e];
       }
       __syncwarp();
-      if (lane < words && h < p.Hq + p.Hkv) {
+      if (h < p.Hq + p.Hkv && h < last) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int d = lane * 8 + e;
+          const int d = c * 8 + e;
           if (d < p.rot) {
             int i, other;
             bool upper;
             if (p.layout_half) { upper = d >= pairs; i = upper ? d - pairs : d; other = upper ? i : d + pairs; }
             else { upper = d & 1; i = d >> 1; other = d ^ 1; }
-            const float2 c = cs[i];
-            const float y = stage[warp][other];
-            x[e] = upper ? x[e] * c.x + y * c.y : x[e] * c.x - y * c.y;
+            const float2 t2 = cs[i];
+            const float y = mine[other];
+            x[e] = upper ? x[e] * t2.x + y * t2.y : x[e] * t2.x - y * t2.y;
           }
         }
         w = pack8(x);
       }
-      if (lane < words) *target(h, lane) = w;
+      if (h < last) *target(h, c) = w;
       __syncwarp();
     }
     return;
   }
-  // Units of work: a head's rotated words (half layout: two per unit), then the words that pass.
-  const int rot_units = kVec == 0 ? p.rot >> 4 : p.rot >> 3;
-  const int pass0 = p.rot >> 3;                                  // first word that passes
+  // A thread keeps its place within the head -- a unit is a rotated word (half layout: the two words of eight pairs) or a
+  // word that passes -- and walks the heads: its cosines stay in registers, and nothing is divided per word (with a division per
+  // word the kernel was bound by instructions, 55 us for 8192 rows of 24 KB in and out).
+  const int rot_units = kVec == 0 ? p.rot >> 4 : p.rot >> 3, pass0 = p.rot >> 3;
   const int per_head = rot_units + words - pass0;
-  const int turned = (p.Hq + p.Hkv - first) * per_head;           // units of heads that are rotated
-  const int q_units = (p.Hq - first) * per_head;
-  const int total = kv ? turned + p.Hkv * words : q_units;
-  for (int u = threadIdx.x; u < total; u += kRopeThreads) {
-    if (u >= turned) {                                            // values
-      const int i = u - turned, h = p.Hq + p.Hkv + i / words, c = i % words;
-      *target(h, c) = reinterpret_cast<const uint4*>(source(h))[c];
-      continue;
-    }
-    const int h = first + u / per_head, j = u % per_head;
-    const uint4* src = reinterpret_cast<const uint4*>(source(h));
-    if (j >= rot_units) {
-      const int c = pass0 + j - rot_units;
-      *target(h, c) = src[c];
-      continue;
-    }
-    float a[8], y[8];
-    if (kVec == 0) {
-      float z[8];
-      unpack8(src[j], a);
-      unpack8(src[j + rot_units], z);
+  const int lanes = per_head <= 4 ? 4 : per_head <= 8 ? 8 : per_head <= 16 ? 16 : 32;   // of a head
+  constexpr int kDeep = kVec == 0 ? 2 : 4, kPairs = kVec == 0 ? 8 : 4;    // (64 registers, four blocks an SM)
+  // heads [h0, h1) of one kind, kDeep at a time, loads first
+  auto walk = [&](auto turns, int lane, int per, const __nv_bfloat16* src, uint4* dst, int64_t dst_words, int n, int c, int c2,
+                  int d, int d2, const float2* t2, bool turn) {
+    constexpr bool kTurn = decltype(turns)::value, kTwo = kTurn && kVec == 0;
+    const int step = kGroup / per;
+    for (int h0 = lane; h0 < n; h0 += kDeep * step) {
+      uint4 w0[kDeep], w1[kTwo ? kDeep : 1];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 c = cs[j * 8 + e];
-        y[e] = a[e] * c.x - z[e] * c.y;
-        z[e] = z[e] * c.x + a[e] * c.y;
+      for (int k = 0; k < kDeep; ++k) {
+        const int h = h0 + k * step;
+        if (h >= n) break;
+        const uint4* q = reinterpret_cast<const uint4*>(src + (int64_t)h * D);
+        w0[k] = q[c];
+        if (kTwo) w1[k] = q[c2];
       }
-      *target(h, j) = pack8(y);
-      *target(h, j + rot_units) = pack8(z);
-    } else {
-      unpack8(src[j], a);
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float2 c = cs[j * 4 + e / 2];
-        y[e] = a[e] * c.x - a[e + 1] * c.y;
-        y[e + 1] = a[e + 1] * c.x + a[e] * c.y;
+      for (int k = 0; k < kDeep; ++k) {
+        const int h = h0 + k * step;
+        if (h >= n) break;
+        uint4* out = dst + h * dst_words;
+        if (kTurn) {
+          float x[8], y[8];
+          unpack8(w0[k], x);
+          if (kTwo) {
+            float z[8];
+            unpack8(w1[k], z);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              y[e] = x[e] * t2[e].x - z[e] * t2[e].y;
+              z[e] = z[e] * t2[e].x + x[e] * t2[e].y;
+            }
+            out[d2] = pack8(z);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+              y[e] = x[e] * t2[e / 2].x - x[e + 1] * t2[e / 2].y;
+              y[e + 1] = x[e + 1] * t2[e / 2].x + x[e] * t2[e / 2].y;
+            }
+          }
+          out[d] = turn ? pack8(y) : w0[k];
+        } else {
+          out[d] = w0[k];
+        }
       }
-      *target(h, j) = pack8(y);
     }
+  };
+  const uint32_t swap = (uint32_t)t & 7u;                         // cached rows have their words permuted by the slot
+  const int64_t tile_words = 2 * tile / 8;
+  uint4* k_dst = reinterpret_cast<uint4*>(kv);
+  if (kv != nullptr) {                                            // values: they need no cosines
+    const int c = tid & (words - 1);
+    walk(Flag<false>{}, tid / words, words, vr, k_dst + tile / 8, tile_words, p.Hkv, c, 0, (int)(c ^ swap), 0, nullptr, false);
+  }
+  sync();
+  const int j = tid & (lanes - 1), h0 = tid / lanes;
+  if (kVec == 1) {                                                // words that turn and words that pass side by side: one walk
+    float2 t2[kPairs];
+    const bool turn = j < rot_units;
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) t2[e] = turn ? cs[j * kPairs + e] : make_float2(0.f, 0.f);
+    if (qr) walk(Flag<true>{}, h0, lanes, qr, reinterpret_cast<uint4*>(qo), words, p.Hq, j, 0, j, 0, t2, turn);
+    if (kv) walk(Flag<true>{}, h0, lanes, kr, k_dst, tile_words, p.Hkv, j, 0, (int)(j ^ swap), 0, t2, turn);
+  } else if (j < rot_units) {
+    float2 t2[kPairs];
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) t2[e] = cs[j * kPairs + e];
+    const int c2 = j + rot_units;
+    if (qr) walk(Flag<true>{}, h0, lanes, qr, reinterpret_cast<uint4*>(qo), words, p.Hq, j, c2, j, c2, t2, true);
+    if (kv) walk(Flag<true>{}, h0, lanes, kr, k_dst, tile_words, p.Hkv, j, c2, (int)(j ^ swap), (int)(c2 ^ swap), t2, true);
+  } else if (j < per_head) {
+    const int c = pass0 + j - rot_units;
+    if (qr) walk(Flag<false>{}, h0, lanes, qr, reinterpret_cast<uint4*>(qo), words, p.Hq, c, 0, c, 0, nullptr, false);
+    if (kv) walk(Flag<false>{}, h0, lanes, kr, k_dst, tile_words, p.Hkv, c, 0, (int)(c ^ swap), 0, nullptr, false);
   }
 }
 
@@ -204,18 +261,20 @@ struct CommitParams {
 
 constexpr int kCommitThreads = 256;
 
-// grid (tiles of a page = K and V of every head, sequences, layers).  A block owns one head's K or V rows of one
-// sequence: it takes all rows it has to move into registers (at most 64 rows of 32 words), waits, and
-// stores them, so sources and targets may overlap in any order.
+// grid (groups of a page's K and V tiles, sequences, layers).  A block owns a few heads' K or V rows of one sequence: it takes
+// all rows that it has to move into registers (at most 64 rows; 16 words a thread), waits, and stores them, so sources and
+// targets may overlap in any order.  Where a row comes from and goes to is looked up once for all of the block's tiles: that chain
+// of lookups (lengths, path, page table) is what a block spends its time on.  (64 sequences x 8 layers of 32 rows of 4 KB: 33 us with
+// a tile per block.)
 template <int kWords>
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_constant__ CommitParams p) {
-  constexpr int kPer = 64 * kWords / kCommitThreads;
+  constexpr int kPer = 64 * kWords / kCommitThreads, kTiles = 16 / kPer;
   pdl_wait();
-  const int b = blockIdx.y, tile = blockIdx.x;
+  const int b = blockIdx.y, tile0 = blockIdx.x * kTiles;
   const int32_t ctx = p.ctx_lens[b];
   int32_t m = p.accepted_lens[b];
   if (m < 0 || ctx < 0) m = 0;
-  const bool lead = tile == 0 && blockIdx.z == 0 && threadIdx.x == 0;
+  const bool lead = blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0;
   if (m > p.nodes) {
     m = p.nodes;
     if (lead) atomicOr(p.status, kErrBadPage);
@@ -224,7 +283,7 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_con
   const int64_t num_pages = p.num_pages[blockIdx.z];
   uint4* pool = static_cast<uint4*>(p.pool[blockIdx.z]);
   const int32_t* table = p.page_table + (int64_t)b * p.max_pages;
-  // word of row ctx + i of this head, or -1
+  // word of row ctx + i in the page's first tile, or -1
   auto place = [&](int i, int c) -> int64_t {
     const int64_t s = (int64_t)ctx + i;
     const int64_t lp = s / kPage;
@@ -232,9 +291,9 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_con
     if (lp >= p.max_pages) return -1;
     const int32_t pid = table[lp];
     if (pid < 0 || pid >= num_pages) return -1;
-    return (((int64_t)pid * 2 * p.Hkv + tile) * kPage + t) * kWords + (c ^ (t & 7));
+    return ((int64_t)pid * 2 * p.Hkv * kPage + t) * kWords + (c ^ (t & 7));
   };
-  uint4 held[kPer];
+  uint4 held[kPer][kTiles];
   int64_t to[kPer];
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
@@ -254,15 +313,28 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_con
       atomicOr(p.status, kErrBadPage);
       continue;
     }
-    held[u] = pool[from];
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+      if (tile0 + k < 2 * p.Hkv) held[u][k] = pool[from + (int64_t)(tile0 + k) * kPage * kWords];
   }
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < kPer; ++u)
-    if (to[u] >= 0) pool[to[u]] = held[u];
+    if (to[u] >= 0) {
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k)
+        if (tile0 + k < 2 * p.Hkv) pool[to[u] + (int64_t)(tile0 + k) * kPage * kWords] = held[u][k];
+    }
 }
 
 }  // namespace opw_draft
+
+template <int kVec, int kGroup>
+static cudaError_t launch_rope(const opw_stage_view& s, const opw_draft::RopeParams& p, cudaStream_t stream) {
+  constexpr int kRows = opw_draft::kRopeThreads / kGroup;
+  return opw_launch(opw_draft::rope_append_kernel<kVec, kGroup>, dim3((p.rows + kRows - 1) / kRows), dim3(opw_draft::kRopeThreads), 0,
+                    stream, s.pdl, 1, p);
+}
 
 extern "C" opw_status_t opw_rope_table(const opw_rope_config_t* cfg, double* table) {
   if (!cfg || !table || cfg->struct_size != sizeof(opw_rope_config_t) || cfg->reserved != 0) return OPW_ERR_INVALID_ARG;
@@ -344,6 +416,7 @@ extern "C" opw_status_t opw_rope_append(opw_attn_stage_t* stage, int32_t layer, 
   p.k_stride = k_stride;
   p.v_stride = v_stride;
   p.num_pages = s.num_pages[layer];
+  p.rows = rows;
   p.Hq = s.Hq;
   p.Hkv = s.Hkv;
   p.D = s.D;
@@ -353,15 +426,12 @@ extern "C" opw_status_t opw_rope_append(opw_attn_stage_t* stage, int32_t layer, 
   p.layout_half = layout == OPW_ROPE_HALF;
   opw_device_guard guard(s.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
-  const dim3 grid(rows), block(opw_draft::kRopeThreads);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const int vec = layout == OPW_ROPE_HALF ? (rotary_dim % 16 == 0 ? 0 : 2) : (rotary_dim % 8 == 0 ? 1 : 2);
   cudaError_t e;
-  if (layout == OPW_ROPE_HALF && rotary_dim % 16 == 0)
-    e = opw_launch(opw_draft::rope_append_kernel<0>, grid, block, 0, stream, s.pdl, 1, p);
-  else if (layout == OPW_ROPE_INTERLEAVED && rotary_dim % 8 == 0)
-    e = opw_launch(opw_draft::rope_append_kernel<1>, grid, block, 0, stream, s.pdl, 1, p);
-  else
-    e = opw_launch(opw_draft::rope_append_kernel<2>, grid, block, 0, stream, s.pdl, 1, p);
+  if (vec == 2) e = launch_rope<2, 256>(s, p, stream);
+  else if (rows >= opw_draft::kRopeWarpRows * s.sms) e = vec == 0 ? launch_rope<0, 32>(s, p, stream) : launch_rope<1, 32>(s, p, stream);
+  else e = vec == 0 ? launch_rope<0, 256>(s, p, stream) : launch_rope<1, 256>(s, p, stream);
   if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   *s.launches += 1;
   return OPW_OK;
@@ -405,7 +475,8 @@ extern "C" opw_status_t opw_kv_commit(opw_attn_stage_t* stage, const int32_t* la
       p.num_pages[i] = s.num_pages[layers[l0 + i]];
     }
     p.new_lens = l0 == 0 ? new_lens : nullptr;
-    const dim3 grid(2 * s.Hkv, batch, here), block(opw_draft::kCommitThreads);
+    const int per = s.D == 64 ? 8 : s.D == 128 ? 4 : 2;            // tiles a block takes (kTiles)
+    const dim3 grid((2 * s.Hkv + per - 1) / per, batch, here), block(opw_draft::kCommitThreads);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
     if (s.D == 64) e = opw_launch(opw_draft::commit_kernel<8>, grid, block, 0, stream, s.pdl, 1, p);
