@@ -18,7 +18,7 @@ struct TreeLayout {
 
 struct Variant {              // a kernel, and how it cuts rows and keys
   int row_block, keys, workers;
-  bool mma;
+  bool mma, wide;
 };
 
 constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the shared memory beside the tiles
@@ -26,16 +26,11 @@ constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the sha
 Variant pick(const opw_stage_view& v, int nodes, int batch) {
   const int rows = nodes * (v.Hq / v.Hkv);
   Variant k;
-  k.mma = rows > 32 && v.D != 256 && batch <= kMmaMaxBatch;
-  if (k.mma) {
-    k.keys = opw_tree::kMmaKeys;
-    k.row_block = opw_tree::kMmaRows;
-    k.workers = v.sms;
-    return k;
-  }
-  k.keys = 16;
-  k.row_block = rows <= 16 || v.D == 256 ? 16 : 32;
-  k.workers = v.sms * (v.D == 64 ? 12 : v.D == 128 ? 8 : 6);
+  k.wide = rows > 128;
+  k.mma = rows > 16 && v.D != 256 && batch <= kMmaMaxBatch;
+  k.keys = k.mma ? opw_tree::kMmaKeys : 16;
+  k.row_block = k.mma ? (k.wide ? 256 : 128) : 16;
+  k.workers = k.mma ? v.sms : v.sms * (v.D == 64 ? 12 : v.D == 128 ? 8 : 6);
   return k;
 }
 
@@ -55,16 +50,21 @@ TreeLayout carve(const opw_stage_view& v, int max_nodes) {
   return L;
 }
 
-template <int D, int MT>
+template <int D>
 cudaError_t raise_smem() {
-  return cudaFuncSetAttribute(opw_tree::tree_warp_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)opw_tree::WarpTree<D, MT>::smem(opw_tree::kMaxTreeBatch));
+  return cudaFuncSetAttribute(opw_tree::tree_warp_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)opw_tree::WarpTree<D>::smem(opw_tree::kMaxTreeBatch));
+}
+template <int D, bool kWide>
+cudaError_t raise_smem_mma() {
+  return cudaFuncSetAttribute(opw_tree::tree_mma_kernel<D, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)opw_tree::MmaTree<D, kWide>::smem(kMmaMaxBatch));
 }
 
-template <int D, int MT>
+template <int D>
 cudaError_t launch_warp(const opw_stage_view& v, const opw_tree::TreeParams& p, cudaStream_t stream) {
-  using C = opw_tree::WarpTree<D, MT>;
-  return opw_launch(opw_tree::tree_warp_kernel<D, MT>, dim3(v.sms), dim3(C::kWarps * 32), C::smem(p.batch), stream, v.pdl, 1, p);
+  using C = opw_tree::WarpTree<D>;
+  return opw_launch(opw_tree::tree_warp_kernel<D>, dim3(v.sms), dim3(C::kWarps * 32), C::smem(p.batch), stream, v.pdl, 1, p);
 }
 
 template <int D>
@@ -76,10 +76,10 @@ cudaError_t launch_combine(const opw_stage_view& v, const opw_tree::TreeCombineP
               : opw_launch(opw_tree::tree_combine_kernel<D, 1>, grid, block, 0, stream, v.pdl, 1, c);
 }
 
-template <int D>
+template <int D, bool kWide>
 cudaError_t launch_mma(const opw_stage_view& v, const CUtensorMap& map, const opw_tree::TreeParams& p, cudaStream_t stream) {
-  return opw_launch(opw_tree::tree_mma_kernel<D>, dim3(v.sms), dim3(opw_tree::kMmaThreads), opw_tree::MmaTree<D>::smem(p.batch), stream,
-                    v.pdl, 1, map, p);
+  return opw_launch(opw_tree::tree_mma_kernel<D, kWide>, dim3(v.sms), dim3(opw_tree::kMmaThreads),
+                    opw_tree::MmaTree<D, kWide>::smem(p.batch), stream, v.pdl, 1, map, p);
 }
 
 typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -135,20 +135,16 @@ extern "C" opw_status_t opw_tree_attn_create(opw_attn_stage_t* stage, int32_t ma
   if (!guard.ok()) return OPW_ERR_CUDA;
   cudaError_t e;
   if (v.D == 64) {
-    e = raise_smem<64, 1>();
-    if (e == cudaSuccess) e = raise_smem<64, 2>();
+    e = raise_smem<64>();
+    if (e == cudaSuccess) e = raise_smem_mma<64, false>();
+    if (e == cudaSuccess) e = raise_smem_mma<64, true>();
   } else if (v.D == 128) {
-    e = raise_smem<128, 1>();
-    if (e == cudaSuccess) e = raise_smem<128, 2>();
+    e = raise_smem<128>();
+    if (e == cudaSuccess) e = raise_smem_mma<128, false>();
+    if (e == cudaSuccess) e = raise_smem_mma<128, true>();
   } else {
-    e = raise_smem<256, 1>();
+    e = raise_smem<256>();
   }
-  if (e == cudaSuccess && v.D == 64)
-    e = cudaFuncSetAttribute(opw_tree::tree_mma_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)opw_tree::MmaTree<64>::smem(kMmaMaxBatch));
-  if (e == cudaSuccess && v.D == 128)
-    e = cudaFuncSetAttribute(opw_tree::tree_mma_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)opw_tree::MmaTree<128>::smem(kMmaMaxBatch));
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult found;
   if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
@@ -227,10 +223,13 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   if (!guard.ok()) return OPW_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (k.mma) e = v.D == 64 ? launch_mma<64>(v, tree->maps[layer], p, stream) : launch_mma<128>(v, tree->maps[layer], p, stream);
-  else if (v.D == 64) e = k.row_block == 16 ? launch_warp<64, 1>(v, p, stream) : launch_warp<64, 2>(v, p, stream);
-  else if (v.D == 128) e = k.row_block == 16 ? launch_warp<128, 1>(v, p, stream) : launch_warp<128, 2>(v, p, stream);
-  else e = launch_warp<256, 1>(v, p, stream);
+  if (k.mma) {
+    const CUtensorMap& map = tree->maps[layer];
+    if (v.D == 64) e = k.wide ? launch_mma<64, true>(v, map, p, stream) : launch_mma<64, false>(v, map, p, stream);
+    else e = k.wide ? launch_mma<128, true>(v, map, p, stream) : launch_mma<128, false>(v, map, p, stream);
+  } else {
+    e = v.D == 64 ? launch_warp<64>(v, p, stream) : v.D == 128 ? launch_warp<128>(v, p, stream) : launch_warp<256>(v, p, stream);
+  }
   if (e == cudaSuccess) {
     *v.launches += 1;
     // Partials per row block, about: workers / blocks.  Above four the partials are dealt out to four groups of threads.

@@ -186,12 +186,11 @@ __device__ __forceinline__ float bf16_at(uint32_t addr) {
 // ---------------------------------------------------------------------------------
 // few rows: every warp streams its own units, as the stage's decode kernel does
 // ---------------------------------------------------------------------------------
-// A unit is one page; a row block is MT * 16 rows, the accumulators of MT matrix tiles in registers.  While the rows of
-// one (b, g) fit the block the cache is read once and HBM bounds the kernel.
-template <int D, int MT>
+// A unit is one page; a row block is 16 rows, the accumulators of one matrix tile in registers.
+template <int D>
 struct WarpTree {
   static constexpr int kTile = 2 * kPage * D * 2;
-  static constexpr int kRows = 16 * MT;
+  static constexpr int kRows = 16;
   static constexpr int kWarps = D == 64 ? 12 : D == 128 ? 8 : 6;
   static constexpr int kStages = 2;
   static size_t smem(int batch) {
@@ -199,9 +198,9 @@ struct WarpTree {
   }
 };
 
-template <int D, int MT>
-__global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_kernel(TreeParams p) {
-  using C = WarpTree<D, MT>;
+template <int D>
+__global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(TreeParams p) {
+  using C = WarpTree<D>;
   constexpr int KS = D / 16, NT = D / 8, ROWB = D * 2, TILE = C::kTile;
   constexpr uint32_t kFirst = 1u << 28, kLast = 1u << 29, kBad = 1u << 30, kPageBits = kFirst - 1;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -266,8 +265,8 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
 
   const int mi = lane >> 3, rr = lane & 7, qrow = lane >> 2, qcol = (lane & 3) * 2;
   const uint32_t k_off = (uint32_t)((rr + 8 * (mi >> 1)) * ROWB), v_off = (uint32_t)(kPage * ROWB + (rr + 8 * (mi & 1)) * ROWB);
-  uint32_t qa[MT][KS][4];
-  float o[MT][NT][4], mx[MT][2], l[MT][2];
+  uint32_t qa[KS][4];
+  float o[NT][4], mx[2], l[2];
   int b = 0, g = 0, rb = 0, rows = 0;
   int32_t border = 0;
   Span sp = {0, 0, 0, 0, 1, false};
@@ -293,24 +292,21 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
       rows = sp.tree * p.G - rb * C::kRows;   // of this block; may exceed it
       border = window_border(p, b, sp, lane);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int r = mt * 16 + h * 8 + qrow;
+          const int r = h * 8 + qrow;
           const bool live = r < rows;
           const int R = rb * C::kRows + r, node = R / p.G;
           const __nv_bfloat16* qb = p.q + (((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G)) * D + qcol;
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            qa[mt][ks][h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16) : 0u;
-            qa[mt][ks][2 + h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16 + 8) : 0u;
+            qa[ks][h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16) : 0u;
+            qa[ks][2 + h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16 + 8) : 0u;
           }
-          mx[mt][h] = -INFINITY;
-          l[mt][h] = 0.f;
+          mx[h] = -INFINITY;
+          l[h] = 0.f;
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
-      }
+        for (int nt = 0; nt < NT; ++nt) o[nt][0] = o[nt][1] = o[nt][2] = o[nt][3] = 0.f;
     }
     if (!mbar_wait(bar0 + 8 * slot, phase)) { failed = true; break; }
     --inflight;
@@ -318,27 +314,20 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
     const int32_t key0 = (int32_t)(page & kPageBits) * kPage;
 
     // ---- S = Q K^T ----
-    float x[MT][2][4];
+    float x[2][4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) x[mt][nt][0] = x[mt][nt][1] = x[mt][nt][2] = x[mt][nt][3] = 0.f;
+      for (int nt = 0; nt < 2; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       uint32_t r0, r1, r2, r3;
       ldsm_x4(tile + k_off + ((((2 * ks + (mi & 1)) ^ rr)) << 4), r0, r1, r2, r3);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        mma_bf16(x[mt][0], qa[mt][ks][0], qa[mt][ks][1], qa[mt][ks][2], qa[mt][ks][3], r0, r1);
-        mma_bf16(x[mt][1], qa[mt][ks][0], qa[mt][ks][1], qa[mt][ks][2], qa[mt][ks][3], r2, r3);
-      }
+        mma_bf16(x[0], qa[ks][0], qa[ks][1], qa[ks][2], qa[ks][3], r0, r1);
+        mma_bf16(x[1], qa[ks][0], qa[ks][1], qa[ks][2], qa[ks][3], r2, r3);
     }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[mt][nt][e] *= p.scale_log2e;
+        for (int e = 0; e < 4; ++e) x[nt][e] *= p.scale_log2e;
 
     const bool masked = key0 + kPage > sp.ctx || key0 < border || (page & kBad);
     uint32_t odd = 0;                         // keys of the tile whose values are not all finite
@@ -362,71 +351,64 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
       }
       __syncwarp();
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int r = mt * 16 + h * 8 + qrow;
+          const int r = h * 8 + qrow;
           if (r < rows && !(page & kBad)) {
             const uint32_t seen = visible_word(row_view(p, b, sp, (rb * C::kRows + r) / p.G), key0);
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e)
-                if (!((seen >> (nt * 8 + qcol + e)) & 1u)) x[mt][nt][2 * h + e] = -INFINITY;
+                if (!((seen >> (nt * 8 + qcol + e)) & 1u)) x[nt][2 * h + e] = -INFINITY;
           } else {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) x[mt][nt][2 * h] = x[mt][nt][2 * h + 1] = -INFINITY;
+            for (int nt = 0; nt < 2; ++nt) x[nt][2 * h] = x[nt][2 * h + 1] = -INFINITY;
           }
         }
     }
 
     // ---- online softmax (base 2) ----
-    uint32_t pa[MT][4];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    uint32_t pa[4];
       float top[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float t = fmaxf(fmaxf(x[mt][0][2 * h], x[mt][0][2 * h + 1]), fmaxf(x[mt][1][2 * h], x[mt][1][2 * h + 1]));
+        float t = fmaxf(fmaxf(x[0][2 * h], x[0][2 * h + 1]), fmaxf(x[1][2 * h], x[1][2 * h + 1]));
         t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-        top[h] = fmaxf(mx[mt][h], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2)));
+        top[h] = fmaxf(mx[h], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2)));
       }
-      if (__any_sync(0xffffffffu, top[0] > mx[mt][0] || top[1] > mx[mt][1])) {
+      if (__any_sync(0xffffffffu, top[0] > mx[0] || top[1] > mx[1])) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float a = mx[mt][h] == -INFINITY ? 0.f : fast_exp2(mx[mt][h] - top[h]);   // nothing summed yet: all zero
-          l[mt][h] *= a;
+          const float a = mx[h] == -INFINITY ? 0.f : fast_exp2(mx[h] - top[h]);   // nothing summed yet: all zero
+          l[h] *= a;
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) { o[mt][nt][2 * h] *= a; o[mt][nt][2 * h + 1] *= a; }
-          mx[mt][h] = top[h];
+          for (int nt = 0; nt < NT; ++nt) { o[nt][2 * h] *= a; o[nt][2 * h + 1] *= a; }
+          mx[h] = top[h];
         }
       }
       float pr[2][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float m = mx[mt][h] == -INFINITY ? 0.f : mx[mt][h];
+        const float m = mx[h] == -INFINITY ? 0.f : mx[h];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            pr[nt][2 * h + e] = fast_exp2(x[mt][nt][2 * h + e] - m);
-            l[mt][h] += pr[nt][2 * h + e];
+            pr[nt][2 * h + e] = fast_exp2(x[nt][2 * h + e] - m);
+            l[h] += pr[nt][2 * h + e];
           }
       }
       // P is rounded to bf16 for the product, the sum is not: the roundings average out over the keys
-      pa[mt][0] = pack_bf16(pr[0][0], pr[0][1]);
-      pa[mt][1] = pack_bf16(pr[0][2], pr[0][3]);
-      pa[mt][2] = pack_bf16(pr[1][0], pr[1][1]);
-      pa[mt][3] = pack_bf16(pr[1][2], pr[1][3]);
-    }
+      pa[0] = pack_bf16(pr[0][0], pr[0][1]);
+      pa[1] = pack_bf16(pr[0][2], pr[0][3]);
+      pa[2] = pack_bf16(pr[1][0], pr[1][1]);
+      pa[3] = pack_bf16(pr[1][2], pr[1][3]);
     if (odd) {                                // rare: values that are not finite leave the tile
       for (uint32_t rest = odd; rest; rest &= rest - 1) {
         const int t = __ffs(rest) - 1;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int r = mt * 16 + h * 8 + qrow;
+            const int r = h * 8 + qrow;
             if (r >= rows || !((visible_word(row_view(p, b, sp, (rb * C::kRows + r) / p.G), key0) >> t) & 1u)) continue;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -434,7 +416,7 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
               for (int e = 0; e < 2; ++e) {
                 const uint32_t a = tile + (uint32_t)(kPage * ROWB + t * ROWB + ((nt ^ (t & 7)) << 4) + (qcol + e) * 2);
                 const float val = bf16_at(a);
-                if (!isfinite(val)) o[mt][nt][2 * h + e] += val;
+                if (!isfinite(val)) o[nt][2 * h + e] += val;
               }
           }
       }
@@ -453,11 +435,8 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
     for (int j = 0; j < KS; ++j) {
       uint32_t r0, r1, r2, r3;
       ldsm_x4_t(tile + v_off + ((((2 * j + (mi >> 1)) ^ rr)) << 4), r0, r1, r2, r3);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        mma_bf16(o[mt][2 * j], pa[mt][0], pa[mt][1], pa[mt][2], pa[mt][3], r0, r1);
-        mma_bf16(o[mt][2 * j + 1], pa[mt][0], pa[mt][1], pa[mt][2], pa[mt][3], r2, r3);
-      }
+        mma_bf16(o[2 * j], pa[0], pa[1], pa[2], pa[3], r0, r1);
+        mma_bf16(o[2 * j + 1], pa[0], pa[1], pa[2], pa[3], r2, r3);
     }
     __syncwarp();
     if (u + stages < u1) {
@@ -471,13 +450,11 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
       const bool complete = from_first && last;
       float* pb = p.partials + (2 * worker + (on_first_row ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float t = l[mt][h];
+          float t = l[h];
           t += __shfl_xor_sync(0xffffffffu, t, 1);
           t += __shfl_xor_sync(0xffffffffu, t, 2);
-          const int r = mt * 16 + h * 8 + qrow;
+          const int r = h * 8 + qrow;
           if (r >= rows) continue;
           if (complete) {
             const int R = rb * C::kRows + r, node = R / p.G;
@@ -486,15 +463,15 @@ __global__ void __launch_bounds__(WarpTree<D, MT>::kWarps * 32, 1) tree_warp_ker
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
               *reinterpret_cast<uint32_t*>(p.out + row * D + nt * 8 + qcol) =
-                  pack_bf16(o[mt][nt][2 * h] * inv, o[mt][nt][2 * h + 1] * inv);
+                  pack_bf16(o[nt][2 * h] * inv, o[nt][2 * h + 1] * inv);
             if (p.lse && (lane & 3) == 0)
-              p.lse[row] = t > 0.f ? (mx[mt][h] + log2f(t)) * 0.6931471805599453f : t == 0.f ? -INFINITY : t;
+              p.lse[row] = t > 0.f ? (mx[h] + log2f(t)) * 0.6931471805599453f : t == 0.f ? -INFINITY : t;
           } else {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
-              *reinterpret_cast<float2*>(pb + r * D + nt * 8 + qcol) = make_float2(o[mt][nt][2 * h], o[mt][nt][2 * h + 1]);
+              *reinterpret_cast<float2*>(pb + r * D + nt * 8 + qcol) = make_float2(o[nt][2 * h], o[nt][2 * h + 1]);
             if ((lane & 3) == 0) {
-              pb[C::kRows * D + r] = mx[mt][h];
+              pb[C::kRows * D + r] = mx[h];
               pb[C::kRows * (D + 1) + r] = t;
             }
           }

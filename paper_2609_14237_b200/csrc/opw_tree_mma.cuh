@@ -30,17 +30,22 @@ constexpr int kMmaThreads = 384;              // two softmax warpgroups; in the 
 constexpr int kMmaKeys = 64;                  // keys per tile
 constexpr int kTilePages = kMmaKeys / 16;
 constexpr int kBadRing = 32;
-constexpr int kMmaRows = 256;                 // rows per block
 constexpr float kRaise = 8.f;                 // log2 of how far a row's maximum may run ahead of the one in use
 
-template <int D>
+// kWide: row blocks of 256 rows, for trees of more than 128.  Without it a block has 128, both slots read one query tile, and the
+// shared memory of the other goes to V: a V tile waits for its softmax where a K tile is used at once, and with
+// four tiles of either a CTA had too few bytes in flight (64 trees of 8 at 1k to 4k keys: 138 us, with six of V 130 us).
+template <int D, bool kWide>
 struct MmaTree {
   static constexpr int kHalves = D / 64;
+  static constexpr int kRows = kWide ? 256 : 128;
   static constexpr uint32_t kHalfBytes = kMmaKeys * 128;      // 64 dimensions of a K or V tile
   static constexpr uint32_t kPiece = kHalves * kHalfBytes;    // a K or V tile
   static constexpr uint32_t kQHalf = 128 * 128, kQTile = kHalves * kQHalf;   // a query tile: 128 rows
-  static constexpr int kPieces = D == 128 ? 8 : 16;           // half of them for K, half for V
-  static size_t smem(int batch) { return 1024 + (size_t)kPieces * kPiece + 2 * kQTile + (size_t)(batch + 1) * 8; }
+  // ring depths, even: in alternate mode the tile that had a place before is then the same slot's
+  static constexpr int kStagesK = D == 128 ? 4 : 8, kStagesV = D == 128 ? (kWide ? 4 : 6) : (kWide ? 8 : 12);
+  static constexpr int kPieces = kStagesK + kStagesV, kQTiles = kWide ? 2 : 1;
+  static size_t smem(int batch) { return 1024 + (size_t)kPieces * kPiece + kQTiles * kQTile + (size_t)(batch + 1) * 8; }
 };
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int c1, int c3, int c4, uint32_t bar, uint64_t pol) {
@@ -172,29 +177,30 @@ struct Segment {
   bool shared;                 // both slots on every tile (more than 128 rows), or alternate tiles
   Span sp;
 };
+template <int kRows>
 __device__ __forceinline__ Segment segment_at(const TreeParams& p, const int64_t* cum, int64_t u, int64_t u1) {
   Segment s;
   s.b = find_sequence(cum, p.batch, u);
-  s.sp = span_of(p, s.b, kMmaRows);
+  s.sp = span_of(p, s.b, kRows);
   const int32_t cnt = tiles_of(s.sp, kMmaKeys);
   const int64_t rem = u - cum[s.b];
   const int32_t ri = (int32_t)(rem / cnt);
   s.t0 = (int32_t)(rem - (int64_t)ri * cnt);
   s.g = ri / s.sp.blocks;
   s.rb = ri - s.g * s.sp.blocks;
-  s.rows = min(s.sp.tree * p.G - s.rb * kMmaRows, kMmaRows);
+  s.rows = min(s.sp.tree * p.G - s.rb * kRows, kRows);
   s.n = (int32_t)min((int64_t)(cnt - s.t0), u1 - u);
   s.first = s.t0 == 0;
   s.last = s.t0 + s.n == cnt;
-  s.shared = s.rows > 128;
+  s.shared = kRows > 128 && s.rows > 128;
   return s;
 }
-template <int D>
+template <int D, bool kWide>
 __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_constant__ CUtensorMap map, const TreeParams p) {
-  using C = MmaTree<D>;
-  constexpr int NS = C::kPieces / 2;                  // ring depth of K, and of V
+  using C = MmaTree<D, kWide>;
+  constexpr uint32_t NK = C::kStagesK, NV = C::kStagesV;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[2][NS], empty_bar[2][NS], s_bar[2][2], p_bar[2][2], o_bar[2][2], seg_bar, end_bar[2];
+  __shared__ __align__(8) uint64_t full_bar[NK + NV], empty_bar[NK + NV], s_bar[2][2], p_bar[2][2], o_bar[2][2], seg_bar, end_bar[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int bad_s[kBadRing];                     // pages of a tile that are bad: bit per page; by tile, the last few
   __shared__ uint32_t odd_s[2][4];                    // keys of a tile with values that are not finite, by warp
@@ -204,14 +210,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t q_smem = base, ring = base + 2 * C::kQTile;
-  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)C::kPieces * C::kPiece + 2 * C::kQTile);
+  const uint32_t q_smem = base, ring = base + C::kQTiles * C::kQTile, ring_v = ring + NK * C::kPiece;
+  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)C::kPieces * C::kPiece + C::kQTiles * C::kQTile);
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
-    for (int i = 0; i < 2 * NS; ++i) {
-      mbar_init(smem_u32(&full_bar[0][0] + i), 1);
-      mbar_init(smem_u32(&empty_bar[0][0] + i), 2);   // an arrival from each slot, or two from the one that has the tile
+    for (int i = 0; i < C::kPieces; ++i) {             // K's stages, then V's
+      mbar_init(smem_u32(&full_bar[i]), 1);
+      mbar_init(smem_u32(&empty_bar[i]), 2);          // an arrival from each slot, or two from the one that has the tile
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(smem_u32(&s_bar[0][0] + i), 1);
@@ -231,7 +237,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_before();
-  scan_units(p, cum, kMmaRows, kMmaKeys);             // begins and ends with a barrier of the block
+  scan_units(p, cum, C::kRows, kMmaKeys);             // begins and ends with a barrier of the block
   tc_after();
   constexpr uint32_t tmem = 0;                        // all 512 columns are this block's: they begin at column 0
   const int64_t U = cum[p.batch];
@@ -256,12 +262,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   if (warp == 8 || warp == 11) {
     // ---- producers: warp 8 copies the K tiles, warp 11 the V tiles ----
     const int kv = warp == 8 ? 0 : 1;
+    const uint32_t stages = kv == 0 ? NK : NV, stage0 = kv == 0 ? 0 : NK;
     const uint64_t policy = l2_evict_first_policy();
     const int32_t nowhere = (int32_t)(p.num_pages * p.Hkv);   // one past the tensor's last tile: zeros
     uint32_t issued = 0;
     bool ok = true;
     for (int64_t u = u0; u < u1 && ok;) {
-      const Segment s = segment_at(p, cum, u, u1);
+      const Segment s = segment_at<C::kRows>(p, cum, u, u1);
       const int32_t page0 = s.sp.lo / kPage + s.t0 * kTilePages + (lane & (kTilePages - 1));
       auto fetch = [&](int t) -> int32_t {            // this lane's page of tile t: raw id, or -2 where there is none
         const int32_t lp = page0 + t * kTilePages;
@@ -276,12 +283,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         int32_t pages[kTilePages];                     // one thread issues: a lane each would issue one after the other, slowly
 #pragma unroll
         for (int i = 0; i < kTilePages; ++i) pages[i] = __shfl_sync(0xffffffffu, tile, i);
-        const uint32_t st = issued % NS, round = issued / NS;
-        if (round > 0) ok = ok && wait(&empty_bar[kv][st], (round - 1) & 1u);
+        const uint32_t round = issued / stages, st = stage0 + issued - round * stages;
+        if (round > 0) ok = ok && wait(&empty_bar[st], (round - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (elect_one()) {
-          const uint32_t bar = smem_u32(&full_bar[kv][st]), dst = ring + (uint32_t)(kv * NS + st) * C::kPiece;
+          const uint32_t bar = smem_u32(&full_bar[st]), dst = ring + st * C::kPiece;
           if (kv == 0) {
             bad_s[issued % kBadRing] = (int)bad;       // (rewritten long after every row has looked: the ring of K is shorter)
             if (bad) atomicOr(p.status, kErrBadPage);
@@ -301,9 +308,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       u += s.n;
     }
     // every copy lands before the block's shared memory is given up
-    for (uint32_t i = issued > NS ? issued - NS : 0; i < issued; ++i)
+    for (uint32_t i = issued > stages ? issued - stages : 0; i < issued; ++i)
       for (int k = 0; k < 1 << 16; ++k)
-        if (mbar_try_wait(smem_u32(&full_bar[kv][i % NS]), (i / NS) & 1u)) break;
+        if (mbar_try_wait(smem_u32(&full_bar[stage0 + i % stages]), (i / stages) & 1u)) break;
   } else {
     // ---- MMA issuers, a warp per slot: one's waits and bookkeeping hide under the other's products ----
     const int x = __shfl_sync(0xffffffffu, warp, 0) - 9;
@@ -315,15 +322,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       // The slot's n-th tile uses buffer n % 2, and phase n / 2 of that buffer's barriers.  This loop is the kernel's
       // pulse: a wait costs about 100 cycles here even when it need not wait, so there are four per tile and nothing else.
       const bool el = elect_one();
-      const uint64_t q = desc_k(q_smem + x * C::kQTile), k0 = desc_k(ring), v0 = desc_mn(ring + NS * C::kPiece, C::kHalfBytes);
+      const uint64_t q = desc_k(q_smem + (kWide ? x * C::kQTile : 0u)), k0 = desc_k(ring), v0 = desc_mn(ring_v, C::kHalfBytes);
       const uint32_t sb = smem_u32(&s_bar[x][0]), ob = smem_u32(&o_bar[x][0]), pb = smem_u32(&p_bar[x][0]);
-      const uint32_t kf = smem_u32(&full_bar[0][0]), vf = smem_u32(&full_bar[1][0]), ve = smem_u32(&empty_bar[1][0]);
+      const uint32_t kf = smem_u32(&full_bar[0]), vf = smem_u32(&full_bar[NK]), ve = smem_u32(&empty_bar[NK]);
       auto wait_at = [&](uint32_t bar, uint32_t parity) {
         return mbar_try_wait(bar, parity) || mbar_wait_or_dead(bar, parity, &dead_s, p.status);
       };
       auto scores = [&](uint32_t tile, uint32_t n) -> bool {   // the slot's n-th tile, number `tile` of the worker
-        const uint32_t st = tile % NS;
-        if (!wait_at(kf + 8 * st, (tile / NS) & 1u)) return false;
+        const uint32_t st = tile % NK;
+        if (!wait_at(kf + 8 * st, (tile / NK) & 1u)) return false;
         const uint64_t k = k0 + (uint64_t)(st * (C::kPiece >> 4));
         const uint32_t d = s_tm + 64 * (n & 1u);
         if (el) {
@@ -336,7 +343,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         return true;
       };
       for (int64_t u = u0; u < u1;) {
-        const Segment s = segment_at(p, cum, u, u1);
+        const Segment s = segment_at<C::kRows>(p, cum, u, u1);
         const uint32_t step = s.shared ? 1u : 2u, end = tiles + (uint32_t)s.n;
         uint32_t t = s.shared ? tiles : tiles + x;
         if (!wait(&seg_bar, n_seg++ & 1u)) break;
@@ -345,8 +352,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         if (t + step < end && !scores(t + step, mine + 1)) break;
         bool ok = true;
         for (; t < end; t += step, ++mine) {
-          const uint32_t st = t % NS, buf = mine & 1u, phase = (mine >> 1) & 1u;
-          ok = wait_at(vf + 8 * st, (t / NS) & 1u) && wait_at(pb + 8 * buf, phase);
+          const uint32_t st = t % NV, buf = mine & 1u, phase = (mine >> 1) & 1u;
+          ok = wait_at(vf + 8 * st, (t / NV) & 1u) && wait_at(pb + 8 * buf, phase);
           if (!ok) break;
           tc_after();
           if (el) {
@@ -389,19 +396,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     uint32_t tiles = 0;                                // of all segments before
     bool on_first = true;
     for (int64_t u = u0; u < u1;) {
-      const Segment s = segment_at(p, cum, u, u1);
+      const Segment s = segment_at<C::kRows>(p, cum, u, u1);
       const Span& sp = s.sp;
       const int r = s.shared ? x * 128 + row : row;    // row of the block
       const bool live = r < s.rows;
-      const int R = s.rb * kMmaRows + r, node = R / p.G;
+      const int R = s.rb * C::kRows + r, node = R / p.G;
       auto global_row = [&](int rr) {
-        const int RR = s.rb * kMmaRows + rr, nn = RR / p.G;
+        const int RR = s.rb * C::kRows + rr, nn = RR / p.G;
         return ((int64_t)s.b * p.nodes + nn) * p.Hq + (int64_t)s.g * p.G + (RR - nn * p.G);
       };
       // queries to shared memory, in the layout of a K-major swizzled operand; rows that are not there: zeros
-      const uint32_t qs = q_smem + (uint32_t)x * C::kQTile;
+      const uint32_t qs = q_smem + (kWide ? (uint32_t)x * C::kQTile : 0u);
+      constexpr int kLoaders = kWide ? 128 : 256;      // of a query tile: its slot's threads, or all
 #pragma unroll 4
-      for (int i = row; i < 128 * (D / 8); i += 128) {
+      for (int i = kWide ? row : (int)threadIdx.x; i < 128 * (D / 8); i += kLoaders) {
         const int qr = i / (D / 8), c = i % (D / 8), rr = s.shared ? x * 128 + qr : qr;
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
         if (rr < s.rows) w = *(reinterpret_cast<const uint4*>(p.q + global_row(rr) * D) + c);
@@ -445,22 +453,22 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         (void)wait(&s_bar[x][buf], (mine >> 1) & 1u);
         tc_after();
         if (row == 0) {                                // K has been read
-          mbar_arrive_n(smem_u32(&empty_bar[0][(tiles + t) % NS]), s.shared ? 1u : 2u);
+          mbar_arrive_n(smem_u32(&empty_bar[(tiles + t) % NK]), s.shared ? 1u : 2u);
         }
         if (edge) {
           // Values of keys that some row may not see.  The tile's warpgroup (slot 0's where they share it) clears the rows nobody
           // may read and looks for values that are not finite, a thread per key.  The V tile's barrier may only be asked
           // once the scores are there: they are issued after the tile that had its place in the ring before was read, so
           // that a completed phase of this parity is the one meant.
-          const uint32_t st = (tiles + t) % NS;
+          const uint32_t st = (tiles + t) % NV;
           const int id = s.shared ? 1 : 2 + x, threads = s.shared ? 256 : 128;
-          const uint32_t tile = ring + (NS + st) * C::kPiece;
+          const uint32_t tile = ring_v + st * C::kPiece;
           const bool mine_v = !s.shared || x == 0;
           const int ox = s.shared ? 0 : x;
           // thread = 64 dimensions of a key: warps 0 and 1 the first, 2 and 3 the second (head_dim 128)
           const int vk = row & 63, vh = row >> 6;
           const uint32_t v = tile + (uint32_t)vh * C::kHalfBytes + (uint32_t)vk * 128u;
-          (void)wait(&full_bar[1][st], ((tiles + t) / NS) & 1u);
+          (void)wait(&full_bar[NK + st], ((tiles + t) / NV) & 1u);
           named_sync(id, threads);
           if (mine_v) {
             const int32_t key = key0 + vk;
@@ -631,7 +639,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       tc_after();
       const bool complete = s.first && s.last;
       const float inv = !complete ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-      float* pb = p.partials + (2 * (int64_t)blockIdx.x + (on_first ? 0 : 1)) * (int64_t)(kMmaRows * (D + 2));
+      float* pb = p.partials + (2 * (int64_t)blockIdx.x + (on_first ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
       const int64_t grow = live ? global_row(r) : 0;
 #pragma unroll 1
       for (int c = c0; c < c1; c += 32) {
@@ -665,8 +673,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       }
       if (live && (s.shared || x == 0)) {
         if (!complete) {
-          pb[kMmaRows * D + r] = m;
-          pb[kMmaRows * (D + 1) + r] = l;
+          pb[C::kRows * D + r] = m;
+          pb[C::kRows * (D + 1) + r] = l;
         } else if (p.lse) {
           p.lse[grow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
         }
