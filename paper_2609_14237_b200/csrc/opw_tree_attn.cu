@@ -27,7 +27,8 @@ Variant pick(const opw_stage_view& v, int nodes, int batch) {
   const int rows = nodes * (v.Hq / v.Hkv);
   Variant k;
   k.wide = rows > 128;
-  k.mma = rows > 16 && v.D != 256 && batch <= kMmaMaxBatch;
+  const bool few = batch * v.Hkv < 2 * v.sms;
+  k.mma = (rows > 16 || few) && v.D != 256 && batch <= kMmaMaxBatch;
   k.keys = k.mma ? opw_tree::kMmaKeys : 16;
   k.row_block = k.mma ? (k.wide ? 256 : 128) : 16;
   k.workers = k.mma ? v.sms : v.sms * (v.D == 64 ? 12 : v.D == 128 ? 8 : 6);
@@ -40,7 +41,7 @@ TreeLayout carve(const opw_stage_view& v, int max_nodes) {
   L.partials = align_up((size_t)(opw_tree::kMaxTreeBatch + 1) * 8);
   size_t most = 0;            // over every number of nodes a call may have
   for (int n = 1; n <= max_nodes; ++n) {
-    for (int b : {1, kMmaMaxBatch + 1}) {
+    for (int b : {1, kMmaMaxBatch, kMmaMaxBatch + 1}) {
       const Variant k = pick(v, n, b);
       const size_t need = (size_t)k.workers * 2 * k.row_block * (v.D + 2) * 4;
       if (need > most) most = need;
@@ -70,10 +71,10 @@ cudaError_t launch_warp(const opw_stage_view& v, const opw_tree::TreeParams& p, 
 template <int D>
 cudaError_t launch_combine(const opw_stage_view& v, const opw_tree::TreeCombineParams& c, int64_t blocks, bool deal,
                            cudaStream_t stream) {
-  const int all = c.t.nodes * c.t.G, rows = all < c.row_block ? all : c.row_block, per = deal ? 8 : 32;
-  const dim3 grid((unsigned)blocks, (rows + per - 1) / per), block(opw_tree::kTreeCombineThreads);
-  return deal ? opw_launch(opw_tree::tree_combine_kernel<D, 4>, grid, block, 0, stream, v.pdl, 1, c)
-              : opw_launch(opw_tree::tree_combine_kernel<D, 1>, grid, block, 0, stream, v.pdl, 1, c);
+  const int all = c.t.nodes * c.t.G, rows = all < c.row_block ? all : c.row_block, per = deal ? 4 : 32;
+  const dim3 grid((unsigned)blocks, (rows + per - 1) / per, deal ? D / 32 : 1), block(opw_tree::kTreeCombineThreads);
+  return deal ? opw_launch(opw_tree::tree_combine_kernel<D, 8, 1>, grid, block, 0, stream, v.pdl, 1, c)
+              : opw_launch(opw_tree::tree_combine_kernel<D, 1, D / 32>, grid, block, 0, stream, v.pdl, 1, c);
 }
 
 template <int D, bool kWide>
@@ -232,9 +233,9 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   }
   if (e == cudaSuccess) {
     *v.launches += 1;
-    // Partials per row block, about: workers / blocks.  Above four the partials are dealt out to four groups of threads.
+    // Partials per row block, about: workers / blocks.  Above twelve they are dealt out to groups of threads.
     const int64_t blocks = (int64_t)batch * v.Hkv * c.max_blocks;
-    const bool deal = k.workers > 4 * blocks;
+    const bool deal = k.workers > 12 * blocks;
     e = v.D == 64 ? launch_combine<64>(v, c, blocks, deal, stream)
         : v.D == 128 ? launch_combine<128>(v, c, blocks, deal, stream) : launch_combine<256>(v, c, blocks, deal, stream);
   }

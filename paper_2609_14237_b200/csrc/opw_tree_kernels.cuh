@@ -500,12 +500,14 @@ struct TreeCombineParams {
 };
 constexpr int kTreeCombineThreads = 256;
 
-// grid (batch * Hkv * max_blocks, rows of a block / (32 / kGroups)).  Eight threads own a row, every eighth float4 each, and walk the row's
-// partials once, carrying (O, m, l) like an online softmax; with kGroups > 1 (few rows of many partials each: the walk is a
-// chain of L2 round trips) the partials are dealt out to that many groups of threads, which meet in shared memory.
-template <int D, int kGroups>
+// grid (batch * Hkv * max_blocks, rows of a block / (32 / kGroups), D / (32 V)).  Eight threads own V * 32 columns of a row, every eighth
+// float4 each, and walk the row's partials once, carrying (O, m, l) like an online softmax.  kGroups > 1, V = 1: few rows of many
+// partials each, where the walk is a chain of L2 round trips -- the columns go to blocks of their own, the partials are dealt
+// out to that many groups of threads, which meet in shared memory, and eight are in flight per thread.  (One sequence of 8000
+// keys, 125 partials a row: 21 us with whole rows and four groups of two in flight, 19 us this way and on the tensor-core kernel.)
+template <int D, int kGroups, int V>
 __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const TreeCombineParams c) {
-  constexpr int kRows = 32 / kGroups, V = D / 32, kDeep = V >= 4 ? 2 : 4;      // float4s a thread; partials in flight
+  constexpr int kRows = 32 / kGroups, kDeep = V == 1 ? 8 : V >= 8 ? 2 : 4;     // partials in flight
   const TreeParams& p = c.t;
   __shared__ int32_t slot_s[kTreeCombineThreads];
   __shared__ float4 acc_s[kGroups > 1 ? kTreeCombineThreads : 1][kGroups > 1 ? V : 1];
@@ -516,7 +518,7 @@ __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const
   const int64_t U = p.cum[p.batch], before = p.cum[b];           // asked for together with the lengths
   const Span s = span_of(p, b, c.row_block);
   const int live = s.tree * p.G;
-  const int lane8 = threadIdx.x & 7, group = threadIdx.x / (8 * kRows);
+  const int lane8 = (threadIdx.x & 7) + 8 * V * blockIdx.z, group = threadIdx.x / (8 * kRows);
   const int r = blockIdx.y * kRows + (threadIdx.x >> 3) % kRows, R = rb * c.row_block + r;   // row of the block, of (b, g)
   const int32_t cnt = tiles_of(s, c.keys);
   const int node = R / p.G;
