@@ -81,7 +81,7 @@ opw_status_t opw_rope_table(const opw_rope_config_t *cfg, double *table_host);
  * sequence seq[r]'s cache (page_table row seq[r]).  Angles are reduced in 64 bits, the rotation is fp32,
  * rounded to bf16 once.  Rows with seq[r] < 0 are padding: nothing is read or written for them.  A slot
  * outside the table or a bad page id skips that row's append (its query is still rotated); so does a
- * seq[r] >= max_batch.  Two rows of one call must not name the same (seq, slot).
+ * seq[r] >= num_rows.  Two rows of one call must not name the same (seq, slot).
  *   rotary_dim, layout : as in the table; rotary_dim <= head_dim.  OPW_ROPE_HALF or OPW_ROPE_INTERLEAVED
  *   table      : DEVICE double [rotary_dim / 2 + 1] from opw_rope_table, 8-byte aligned
  *   q, k, v    : DEVICE bf16; row r of q starts at q + r * q_stride and holds [Hq, D] (k, v: [Hkv, D]).  Strides in
@@ -90,12 +90,13 @@ opw_status_t opw_rope_table(const opw_rope_config_t *cfg, double *table_host);
  *   q_out      : DEVICE bf16 [rows, Hq, D], 16-byte aligned; may be q itself if q_stride == Hq * D
  *                q == q_out == NULL: keys and values only
  *   seq, slots, positions : DEVICE int32 [rows]
- *   page_table : DEVICE int32 [max_batch, max_pages_per_seq] (only the named rows are read)
+ *   page_table : DEVICE int32 [num_rows, max_pages_per_seq], num_rows >= 1
  */
 opw_status_t opw_rope_append(opw_attn_stage_t *stage, int32_t layer, int32_t rows, int32_t rotary_dim, int32_t layout,
                              const double *table, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                              const void *v, int64_t v_stride, const int32_t *seq, const int32_t *slots,
-                             const int32_t *positions, const int32_t *page_table, void *q_out, void *cuda_stream);
+                             const int32_t *positions, int32_t num_rows, const int32_t *page_table, void *q_out,
+                             void *cuda_stream);
 
 /* ------------------------------------------------------------------------------------------
  * Attention of a tree of drafted tokens

@@ -223,7 +223,7 @@ def lib() -> ctypes.CDLL:
     L.opw_rope_table.restype = ctypes.c_int
     L.opw_rope_table.argtypes = [ctypes.POINTER(RopeConfig), ctypes.POINTER(ctypes.c_double)]
     L.opw_rope_append.restype = ctypes.c_int
-    L.opw_rope_append.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]
+    L.opw_rope_append.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i32, vp, vp, vp]
     L.opw_tree_mask.restype = ctypes.c_int
     L.opw_tree_mask.argtypes = [i32, vp, vp, vp]
     L.opw_tree_attn_workspace_bytes.restype = ctypes.c_size_t
@@ -515,10 +515,10 @@ def opw_rope_table(rotary_dim: int, *, theta: float = 10000.0, scaling: str = "p
 
 
 def opw_rope_append(stage: int, layer: int, rows: int, rotary_dim: int, layout: int, table: int, q: Optional[int], q_stride: int,
-                    k: int, k_stride: int, v: int, v_stride: int, seq: int, slots: int, positions: int, page_table: int,
-                    q_out: Optional[int], stream: Optional[int] = None) -> None:
+                    k: int, k_stride: int, v: int, v_stride: int, seq: int, slots: int, positions: int, num_rows: int,
+                    page_table: int, q_out: Optional[int], stream: Optional[int] = None) -> None:
     _check(lib().opw_rope_append(stage, layer, rows, rotary_dim, layout, table, q, q_stride, k, k_stride, v, v_stride, seq, slots,
-                                 positions, page_table, q_out, stream), "opw_rope_append")
+                                 positions, num_rows, page_table, q_out, stream), "opw_rope_append")
 
 
 def opw_tree_mask(parents: Sequence[int]):
@@ -713,8 +713,8 @@ class Stage:
             raise ValueError(f"{where}: the rotary table is on {rope.table.device}")
         opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(),
                         None if q is None else q.data_ptr(), 0 if q is None else q.stride(0), k.data_ptr(), k.stride(0),
-                        v.data_ptr(), v.stride(0), seq.data_ptr(), slots.data_ptr(), positions.data_ptr(), page_table.data_ptr(),
-                        None if q is None else q_out.data_ptr(), self._raw_stream(dev))
+                        v.data_ptr(), v.stride(0), seq.data_ptr(), slots.data_ptr(), positions.data_ptr(), page_table.shape[0],
+                        page_table.data_ptr(), None if q is None else q_out.data_ptr(), self._raw_stream(dev))
 
     def kv_commit(self, layers, accepted, accepted_lens, ctx_lens, page_table, new_lens=None):
         """Move the rows of the accepted nodes together behind each sequence's context, in all of `layers`.  accepted: int32

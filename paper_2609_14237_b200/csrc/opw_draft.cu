@@ -33,7 +33,7 @@ struct RopeParams {
   const int32_t* page_table;
   uint32_t* status;
   int64_t q_stride, k_stride, v_stride, num_pages;
-  int32_t rows, Hq, Hkv, D, rot, max_batch, max_pages, layout_half;
+  int32_t rows, Hq, Hkv, D, rot, num_rows, max_pages, layout_half;
 };
 
 constexpr int kRopeThreads = 256;
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_append_kernel(const Rope
   // where the row's keys and values go: null if it is not appended
   __nv_bfloat16* kv = nullptr;
   const int lp = slot / kPage, t = slot % kPage;
-  if (b < p.max_batch && slot >= 0 && lp < p.max_pages) {
+  if (b < p.num_rows && slot >= 0 && lp < p.max_pages) {
     const int32_t pid = p.page_table[(int64_t)b * p.max_pages + lp];
     if (pid >= 0 && pid < p.num_pages) kv = p.pool + ((int64_t)pid * p.Hkv * 2 * kPage + t) * D;
   }
@@ -384,8 +384,9 @@ extern "C" opw_status_t opw_rope_table(const opw_rope_config_t* cfg, double* tab
 extern "C" opw_status_t opw_rope_append(opw_attn_stage_t* stage, int32_t layer, int32_t rows, int32_t rotary_dim, int32_t layout,
                                         const double* table, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                                         const void* v, int64_t v_stride, const int32_t* seq, const int32_t* slots,
-                                        const int32_t* positions, const int32_t* page_table, void* q_out, void* cuda_stream) {
-  if (!stage || rows < 0) return OPW_ERR_INVALID_ARG;
+                                        const int32_t* positions, int32_t num_rows, const int32_t* page_table, void* q_out,
+                                        void* cuda_stream) {
+  if (!stage || rows < 0 || num_rows < 1) return OPW_ERR_INVALID_ARG;
   const opw_stage_view s = opw_view_of(stage);
   if (layer < 0 || layer >= s.num_layers) return OPW_ERR_INVALID_ARG;
   if (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > s.D) return OPW_ERR_INVALID_ARG;
@@ -421,7 +422,7 @@ extern "C" opw_status_t opw_rope_append(opw_attn_stage_t* stage, int32_t layer, 
   p.Hkv = s.Hkv;
   p.D = s.D;
   p.rot = rotary_dim;
-  p.max_batch = s.max_batch;
+  p.num_rows = num_rows;
   p.max_pages = s.max_pages;
   p.layout_half = layout == OPW_ROPE_HALF;
   opw_device_guard guard(s.device);

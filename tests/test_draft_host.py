@@ -77,7 +77,7 @@ def test_null_handles_are_refused():
     assert L.opw_tree_attn_create(None, 8, 0, 256, 1 << 30, ctypes.byref(h)) == B.OPW_ERR_INVALID_ARG and h.value is None
     assert L.opw_tree_attention(None, 0, 1, 4, *[16] * 7, None, None) == B.OPW_ERR_INVALID_ARG
     assert L.opw_tree_attn_destroy(None) == B.OPW_OK
-    assert L.opw_rope_append(None, 0, 1, 64, 0, 16, 16, 64, 16, 64, 16, 64, 16, 16, 16, 16, 16, None) == B.OPW_ERR_INVALID_ARG
+    assert L.opw_rope_append(None, 0, 1, 64, 0, 16, 16, 64, 16, 64, 16, 64, 16, 16, 16, 1, 16, 16, None) == B.OPW_ERR_INVALID_ARG
     assert L.opw_kv_commit(None, one, 1, 1, 4, 16, 16, 16, 16, None, None) == B.OPW_ERR_INVALID_ARG
     assert L.opw_kv_fork(None, one, 1, 1, 16, 16, 16, 16, 1, 16, 16, None) == B.OPW_ERR_INVALID_ARG
     assert L.opw_kv_release(None, 1, 16, None, 1, 16, 16, 1, None) == B.OPW_ERR_INVALID_ARG

@@ -376,6 +376,46 @@ def test_tree_attention_refuses():
     assert call() == B.OPW_OK and st.launch_count() == before + 2 and (out == 0).all()
 
 
+def test_a_batch_beyond_the_tensor_core_kernels_reach():
+    """More than 2048 sequences: the rows of wide trees go through the kernel of few rows, sixteen at a time."""
+    rng = np.random.default_rng(1450)
+    Hq, Hkv, D, T, n = 8, 1, 64, 5, 2100
+    ctx = rng.integers(0, 40, size=n).tolist()
+    size = rng.integers(0, T + 1, size=n).tolist()
+    pool, tab, q, mask, pos = tree_inputs(rng, ctx, size, T, Hq, Hkv, D)
+    out, lse, rc = gpu_tree(pool, tab, q, mask, pos, ctx, size, Hq, Hkv, D)
+    assert rc == B.OPW_OK
+    pick = list(range(0, n, 50)) + [n - 1]
+    ref = draft.tree_attention(pool, Hq, Hkv, D, q[pick], mask[pick], pos[pick], [ctx[i] for i in pick], [size[i] for i in pick], tab[pick])
+    check_tree(out[dev(np.array(pick))], lse[dev(np.array(pick))], ref, 60)
+    # the same rows in a batch that the tensor cores take
+    few, few_lse, rc = gpu_tree(pool, tab[:300], q[:300], mask[:300], pos[:300], ctx[:300], size[:300], Hq, Hkv, D)
+    a, b = few.float(), out[:300].float()
+    assert rc == B.OPW_OK and (a - b).abs().max() <= 4 * 2.0 ** -8 * b.abs().max()      # two roundings on either side
+
+
+@pytest.mark.parametrize("T", [3, 20, 50])
+def test_handles_of_their_own_run_side_by_side(T):
+    """Two handles of one stage on two streams, launched without programmatic serialisation, against one after the other."""
+    rng = np.random.default_rng(1460 + T)
+    Hq, Hkv, D = 32, 8, 128
+    ctx, size = [900, 37, 400], [T, max(1, T - 1), T]
+    pool, tab, q, mask, pos = tree_inputs(rng, ctx, size, T, Hq, Hkv, D)
+    ref = draft.tree_attention(pool, Hq, Hkv, D, q, mask, pos, ctx, size, tab)
+    st = make_stage([dev(pool, True)], Hq, Hkv, D, 3, tab.shape[1], flags=B.OPW_FLAG_NO_PDL)
+    args = (dev(q, True), dev(mask), dev(pos), dev(np.array(ctx, np.int32)), dev(np.array(size, np.int32)), dev(tab))
+    jobs = [(B.TreeAttention(st, T), torch.cuda.Stream(), torch.empty_like(args[0]), torch.empty(3, T, Hq, device="cuda")) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for tree, stream, out, lse in jobs:
+            with torch.cuda.stream(stream):
+                tree.attention(0, *args, out, lse)
+    torch.cuda.synchronize()
+    for _, _, out, lse in jobs:
+        check_tree(out, lse, ref, 1000)
+    assert torch.equal(jobs[0][2], jobs[1][2]) and st.poll_error() == B.OPW_OK
+
+
 def test_tree_attention_in_a_graph_on_another_stream_with_lengths_changed_between_replays():
     rng = np.random.default_rng(1500)
     Hq, Hkv, D, T = 32, 8, 128, 12
@@ -482,7 +522,7 @@ def test_rope_append_skips_and_records_what_it_cannot_place(layout, rot):
     pool = rand_bits(rng, oracle.pool_elems(4, Hkv, P, D))
     q, k, v = (dev(rand_bits(rng, (rows, h, D)), True) for h in (Hq, Hkv, Hkv))
     d_pool = dev(pool, True)
-    st = make_stage([d_pool], Hq, Hkv, D, 3, 2)
+    st = make_stage([d_pool], Hq, Hkv, D, 8, 2)               # (row 3 is beyond the table, not beyond the stage)
     out = torch.zeros_like(q)
     pos = torch.zeros(rows, dtype=torch.int32, device="cuda")
     st.rope_append(0, B.Rope(rot, layout=layout), q, k, v, dev(seq), dev(slots), pos, dev(tab), out)
@@ -501,11 +541,11 @@ def test_rope_append_refuses():
     i = torch.zeros(rows, dtype=torch.int32, device="cuda")
     tab, out = torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.zeros_like(q)
     good = dict(layer=0, rows=rows, rot=64, layout=0, table=rope.table.data_ptr(), q=q.data_ptr(), qs=Hq * D, k=k.data_ptr(), ks=Hkv * D,
-                v=v.data_ptr(), vs=Hkv * D, seq=i.data_ptr(), slots=i.data_ptr(), pos=i.data_ptr(), tab=tab.data_ptr(), out=out.data_ptr())
+                v=v.data_ptr(), vs=Hkv * D, seq=i.data_ptr(), slots=i.data_ptr(), pos=i.data_ptr(), num_rows=2, tab=tab.data_ptr(), out=out.data_ptr())
     call = lambda **kw: B.lib().opw_rope_append(st.handle, *{**good, **kw}.values(), None)  # noqa: E731
     for kw in (dict(layer=1), dict(rows=-1), dict(rot=0), dict(rot=63), dict(rot=66), dict(layout=2), dict(table=None), dict(table=good["table"] + 4),
                dict(q=None), dict(out=None), dict(k=None), dict(v=good["v"] + 2), dict(qs=Hq * D - 8), dict(qs=Hq * D + 4), dict(ks=Hkv * D - 8),
-               dict(vs=Hkv * D + 1), dict(seq=None), dict(slots=good["slots"] + 2), dict(pos=None), dict(tab=None),
+               dict(vs=Hkv * D + 1), dict(seq=None), dict(slots=good["slots"] + 2), dict(pos=None), dict(num_rows=0), dict(tab=None),
                dict(out=good["q"], qs=Hq * D + 8)):
         assert call(**kw) == B.OPW_ERR_INVALID_ARG, kw
     assert st.launch_count() == 0 and call(rows=0) == B.OPW_OK
