@@ -32,9 +32,10 @@ struct ForkParams {
 constexpr int kForkThreads = 256;
 
 // grid (n, blocks per fork, layers of this launch [+ 1 in front for the bookkeeping]).  The copy moves, of each of the page's K and V tiles,
-// the contiguous `rest` rows that hold a token -- half a page on average -- as 16-byte words.  Every
-// block decides for itself whether its fork is refused: a scan of the n rows and page ids, which all
-// blocks share in L2, against a second launch that a list of accepted forks would need.
+// the contiguous `rest` rows that hold a token -- half a page on average -- as 16-byte words, a warp a tile.  (With the tile of each word
+// found by a division the kernel was bound by instructions: 256 forks x 8 layers 22.1 us, now 18.2, 6.9 TB/s of what has to move --
+// children of one parent read its page from L2.)  Every block decides for itself whether its fork is refused: a scan of the n rows and
+// page ids, which all blocks share in L2, against a second launch that a list of accepted forks would need.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constant__ ForkParams p) {
   pdl_wait();
   const int f = blockIdx.x;
@@ -90,19 +91,18 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
   const int64_t tile_vecs = (int64_t)kPage * p.row_vecs;
   const uint4* a = pool + (int64_t)from * p.tiles * tile_vecs;
   uint4* b = pool + (int64_t)fresh * p.tiles * tile_vecs;
-  const int used = rest * p.row_vecs, total = p.tiles * used;
-  const int step = gridDim.y * kForkThreads;
-  for (int i0 = blockIdx.y * kForkThreads + threadIdx.x; i0 < total; i0 += 4 * step) {
-    uint4 v[4];
+  const int used = rest * p.row_vecs, lane = threadIdx.x & 31;
+  for (int t = blockIdx.y * (kForkThreads / 32) + (threadIdx.x >> 5); t < p.tiles; t += gridDim.y * (kForkThreads / 32)) {
+    const uint4* from_tile = a + t * tile_vecs;
+    uint4* to_tile = b + t * tile_vecs;
+    for (int i0 = lane; i0 < used; i0 += 4 * 32) {
+      uint4 v[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * step;
-      if (i < total) v[u] = a[(int64_t)(i / used) * tile_vecs + i % used];
-    }
+      for (int u = 0; u < 4; ++u)
+        if (i0 + 32 * u < used) v[u] = from_tile[i0 + 32 * u];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * step;
-      if (i < total) b[(int64_t)(i / used) * tile_vecs + i % used] = v[u];
+      for (int u = 0; u < 4; ++u)
+        if (i0 + 32 * u < used) to_tile[i0 + 32 * u] = v[u];
     }
   }
 }
@@ -136,26 +136,42 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const int32_t*
 }
 
 // One cluster: each block counts the free pages of its contiguous share, the counts meet through
-// shared memory, and a second pass over the share (by now in L2) writes the ids behind those of the
-// blocks before.  Ascending by construction, no scratch memory, one launch.
+// shared memory, and the ids are written behind those of the blocks before.  Ascending by construction, no scratch memory, one
+// launch.  A thread takes four pages in a row, of up to eight such rounds it remembers the finding (256k pages in all),
+// beyond that it reads the counts again.
 constexpr int kListBlocks = 8;
 constexpr int kListThreads = 1024;
+constexpr int kListRound = 4 * kListThreads, kListKept = 8;
 __global__ void __launch_bounds__(kListThreads) free_pages_kernel(const int32_t* refs, int64_t num_pages, int32_t* list,
                                                                   int64_t max_list, int32_t* count) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
-  __shared__ int32_t warp_n[kListThreads / 32];
+  __shared__ int32_t warp_n[2][kListThreads / 32];
   __shared__ int32_t mine;
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = (int)cluster.block_rank();
   const int64_t lo = num_pages * rank / kListBlocks, hi = num_pages * (rank + 1) / kListBlocks;
+  auto look = [&](int64_t base) -> uint32_t {                     // bit k: page base + 4 * thread + k is free
+    const int64_t i = base + 4 * threadIdx.x;
+    uint32_t f = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k < hi && refs[i + k] == 0) f |= 1u << k;
+    return f;
+  };
+  uint32_t kept = 0;
   int32_t n = 0;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kListThreads) n += refs[i] == 0;
+  int round = 0;
+  for (int64_t base = lo; base < hi; base += kListRound, ++round) {
+    const uint32_t f = look(base);
+    if (round < kListKept) kept |= f << (4 * round);
+    n += __popc(f);
+  }
   n = __reduce_add_sync(0xffffffffu, n);
-  if (lane == 0) warp_n[warp] = n;
+  if (lane == 0) warp_n[0][warp] = n;
   __syncthreads();
   if (warp == 0) {
-    const int32_t t = __reduce_add_sync(0xffffffffu, warp_n[lane]);
+    const int32_t t = __reduce_add_sync(0xffffffffu, warp_n[0][lane]);
     if (lane == 0) mine = t;
   }
   cluster.sync();
@@ -167,21 +183,28 @@ __global__ void __launch_bounds__(kListThreads) free_pages_kernel(const int32_t*
   }
   if (rank == 0 && threadIdx.x == 0) *count = all;
   cluster.sync();                          // nobody leaves while its count is read
-  for (int64_t base = lo; base < hi; base += kListThreads) {
-    const int64_t i = base + threadIdx.x;
-    const bool idle = i < hi && refs[i] == 0;
-    const uint32_t bal = __ballot_sync(0xffffffffu, idle);
-    if (lane == 0) warp_n[warp] = __popc(bal);
-    __syncthreads();
-    int32_t before = 0, round = 0;
-    for (int w = 0; w < kListThreads / 32; ++w) {
-      if (w < warp) before += warp_n[w];
-      round += warp_n[w];
+  round = 0;
+  for (int64_t base = lo; base < hi; base += kListRound, ++round) {
+    const uint32_t f = round < kListKept ? (kept >> (4 * round)) & 15u : look(base);
+    const int own = __popc(f);
+    int incl = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
     }
-    const int64_t to = (int64_t)at + before + __popc(bal & ((1u << lane) - 1u));
-    if (idle && to < max_list) list[to] = (int32_t)i;
-    at += round;
+    int32_t* sums = warp_n[round & 1];     // (two in turn: one barrier a round)
+    if (lane == 31) sums[warp] = incl;
     __syncthreads();
+    const int32_t w = sums[lane];
+    int64_t to = (int64_t)at + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + incl - own;
+    at += __reduce_add_sync(0xffffffffu, w);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((f >> k) & 1u) {
+        if (to < max_list) list[to] = (int32_t)(base + 4 * threadIdx.x + k);
+        ++to;
+      }
   }
 }
 
@@ -230,9 +253,11 @@ extern "C" opw_status_t opw_kv_fork(opw_attn_stage_t* stage, const int32_t* laye
   p.row_vecs = v.D / 8;
   opw_device_guard guard(v.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
-  // Half a page per fork on average, 16 KB (four words a thread) per block and pass
-  int splits = (p.tiles * p.row_vecs * opw_pages::kPage / 2 + 4 * opw_pages::kForkThreads - 1) / (4 * opw_pages::kForkThreads);
-  if (splits < 1) splits = 1;
+  // A block of eight warps for each eight tiles of a page
+  int splits = (p.tiles + opw_pages::kForkThreads / 32 - 1) / (opw_pages::kForkThreads / 32);
+  const int entries = (v.max_pages + 2 * opw_pages::kForkThreads - 1) / (2 * opw_pages::kForkThreads);   // of the bookkeeping
+  if (splits < entries) splits = entries;
+  if (splits > 64) splits = 64;
   // The bookkeeping goes with the LAST launch: the copies of the others read the parents' rows, which it leaves alone, but
   // a later launch must still see the same table when it decides what is refused.
   for (int l0 = 0; l0 < num_layers; l0 += opw_pages::kLayersPerLaunch) {

@@ -748,7 +748,7 @@ def test_release_records_what_does_not_fit():
     assert st.poll_error() == B.OPW_ERR_BAD_PAGE and counts.tolist() == [0, 0, 1, 1] and tab[2].tolist() == [3, -1]
 
 
-@pytest.mark.parametrize("total", [1, 7, 8, 1023, 8192, 100003])
+@pytest.mark.parametrize("total", [1, 7, 8, 1023, 8192, 100003, 600001])
 def test_free_list_of_any_length(total):
     rng = np.random.default_rng(total)
     counts = (rng.random(total) < 0.4).astype(np.int32) * rng.integers(1, 5, size=total).astype(np.int32)
