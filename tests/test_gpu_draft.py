@@ -446,6 +446,31 @@ def test_tree_attention_in_a_graph_on_another_stream_with_lengths_changed_betwee
     assert st.poll_error() == B.OPW_OK
 
 
+@pytest.mark.parametrize("T", [2, 9, 64])
+def test_the_longest_windows_hide_nothing(T):
+    """Window arithmetic at the ends of 32 bits; positions far below and above the context."""
+    rng = np.random.default_rng(1510 + T)
+    Hq, Hkv, D = 32, 8, 128
+    ctx, size = [2300, 0, 77], [T, T, max(1, T - 1)]
+    pool, tab, q, mask, pos = tree_inputs(rng, ctx, size, T, Hq, Hkv, D)
+    pos[2, ::2] = -(1 << 31)
+    want = gpu_tree(pool, tab, q, mask, pos, ctx, size, Hq, Hkv, D)
+    for window in (2400, (1 << 31) - 1):
+        got = gpu_tree(pool, tab, q, mask, pos, ctx, size, Hq, Hkv, D, window)
+        assert got[2] == B.OPW_OK and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_closed_stage_is_refused():
+    st = make_stage([torch.zeros(2 * 2 * 16 * 64, dtype=torch.bfloat16, device="cuda")], 1, 1, 64, 1, 2)
+    tree = B.TreeAttention(st, 1)
+    q = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    one = torch.ones(1, 1, dtype=torch.int32, device="cuda")
+    st.close()
+    with pytest.raises(ValueError):
+        tree.attention(0, q, one.long(), one, one[0], one[0], one.repeat(1, 2), torch.empty_like(q))
+    tree.close()
+
+
 # --------------------------------------------------------------------------------- rotary ---
 
 @pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (32, 8, 128), (5, 1, 64), (6, 2, 256)])
@@ -530,6 +555,28 @@ def test_rope_append_skips_and_records_what_it_cannot_place(layout, rot):
     want = pool.copy()
     draft.append_rows(want, Hkv, D, [0], [0], tab, host_bits(k)[:1].reshape(1, Hkv, D), host_bits(v)[:1].reshape(1, Hkv, D))
     assert (host_bits(d_pool) == want).all()
+
+
+def test_rotated_queries_must_not_overlap_the_inputs():
+    Hq, Hkv, D, rows = 4, 2, 64, 5
+    st = make_stage([torch.zeros(4 * Hkv * 2 * 16 * D, dtype=torch.bfloat16, device="cuda")], Hq, Hkv, D, 2, 2)
+    rope, i = B.Rope(D), torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    tab = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+    packed = torch.zeros(4 * rows, Hq + 2 * Hkv, D, dtype=torch.bfloat16, device="cuda")
+    q, k, v = (packed[:rows, a:b] for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    flat = packed.view(-1)
+    size = rows * Hq * D
+    for at in (0, 8, D, (rows - 1) * (Hq + 2 * Hkv) * D, rows * (Hq + 2 * Hkv) * D - 8):
+        with pytest.raises(B.OpwError):
+            st.rope_append(0, rope, q, k, v, i, i, i, tab, flat[at:at + size])
+    own = torch.zeros(rows, Hq, D, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(B.OpwError):                                 # in place, but the keys lie there too
+        st.rope_append(0, rope, own, own[:, :Hkv], v, i, i, i, tab, own)
+    assert st.launch_count() == 0
+    st.rope_append(0, rope, own, k, v, i, i, i, tab, own)           # in place
+    end = rows * (Hq + 2 * Hkv) * D
+    st.rope_append(0, rope, q, k, v, i, i, i, tab, flat[end:end + size])
+    assert st.launch_count() == 2 and st.poll_error() == B.OPW_OK
 
 
 def test_rope_append_refuses():
@@ -760,6 +807,131 @@ def test_free_list_of_any_length(total):
 
 
 # ------------------------------------------------------------------------------ a whole run ---
+
+def test_a_pool_of_more_than_32_bits_of_elements():
+    """The same step on pages at the end of a pool of 4.6e9 elements and on a small one: equal bit for bit."""
+    rng = np.random.default_rng(4900)
+    Hq, Hkv, D, T, width, per = 32, 8, 128, 20, 8, 2 * 8 * 16 * 128
+    big_pages = 140000
+    assert big_pages * per > 1 << 32
+    x = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda().bfloat16()  # noqa: E731
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    n = 75
+    q, k, v = x(2, T, Hq, D), x(2 * n, Hkv, D), x(2 * n, Hkv, D)
+    seq, at = i32([0] * n + [1] * n), i32(list(range(n)) * 2)
+    ids = rng.permutation(3 * width).astype(np.int32)
+    mask = dev(np.array([B.opw_tree_mask(random_tree(rng, T))[0] for _ in range(2)], np.uint64))
+    acc = i32([[3, 5, 11] + [0] * (T - 3), [0, 1, 19] + [0] * (T - 3)])
+    res = []
+    for pages, base in ((3 * width, 0), (big_pages, big_pages - 3 * width)):
+        pool = torch.empty(pages * per, dtype=torch.bfloat16, device="cuda")
+        pool[-3 * width * per:] = 0
+        st = make_stage([pool], Hq, Hkv, D, 4, width)
+        tree = B.TreeAttention(st, T)
+        tab = dev(np.concatenate([ids[:2 * width].reshape(2, width) + base, np.full((2, width), -1, np.int32)]).astype(np.int32))
+        refs = torch.zeros(pages, dtype=torch.int32, device="cuda")
+        refs[tab[:2].long().view(-1)] = 1
+        st.rope_append(0, B.Rope(D), None, k, v, seq, at, at, tab, None)
+        out, few = torch.empty_like(q), torch.empty_like(q[:, :2])
+        ctx, sizes = i32([n - T, n - T]), i32([T, T])
+        tree.attention(0, q, mask, ctx[:, None] + i32([list(range(T))] * 2), ctx, sizes, tab, out)
+        wide = [t.repeat(40, 1, *[1] * (t.dim() - 2)) for t in (q[:, :2], mask[:, :2])]     # many rows of few nodes: a warp per page
+        st2 = make_stage([pool], Hq, Hkv, D, 80, width)
+        tree2, few = B.TreeAttention(st2, 2), torch.empty_like(wide[0].contiguous())
+        tree2.attention(0, wide[0].contiguous(), wide[1].contiguous(), i32([[n, n + 1]] * 80), ctx.repeat(40), i32([2] * 80),
+                        tab[:2].repeat(40, 1).contiguous(), few)
+        st.kv_commit([0], acc, i32([3, 3]), ctx, tab)
+        st.kv_fork([0], i32([0, 1]), i32([2, 3]), i32([n - T + 3, n - T + 3]), dev(ids[2 * width:2 * width + 2] + np.int32(base)), tab, refs)
+        assert st.poll_error() == B.OPW_OK and st2.poll_error() == B.OPW_OK
+        res.append((out, few, pool[-3 * width * per:].clone(), torch.where(tab < 0, tab, tab - base), refs[-3 * width:].clone()))
+        tree.close(), tree2.close(), st.close(), st2.close()
+        del pool, refs
+    torch.cuda.empty_cache()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
+def test_a_whole_step_captured_and_replayed_equals_eager_calls():
+    """Fork, rotary append, tree attention, commit, release and the free list in one graph, replayed with changed inputs."""
+    rng = np.random.default_rng(4950)
+    Hq, Hkv, D, T, width, total, n = 32, 8, 128, 6, 6, 48, 41
+    per = 2 * Hkv * 16 * D
+    x = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda().bfloat16()  # noqa: E731
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    start = x(total * per)
+    first_tab = np.full((4, width), -1, np.int32)
+    first_tab[0], first_tab[1] = rng.permutation(total)[:12].reshape(2, 6)
+    first_refs = np.zeros(total, np.int32)
+    first_refs[first_tab[:2].ravel()] = 1
+    spare = i32([i for i in range(total) if not first_refs[i]][:2])
+    pool = start.clone()
+    tab, refs = dev(first_tab), dev(first_refs)
+    st = make_stage([pool], Hq, Hkv, D, 4, width)
+    tree, rope = B.TreeAttention(st, T), B.Rope(64, layout="interleaved")
+    parents = random_tree(rng, T)
+    m, depth = B.opw_tree_mask(parents)
+    mask = dev(np.array([m] * 4, np.uint64))
+    q, k, v = x(4 * T, Hq, D), x(4 * T, Hkv, D), x(4 * T, Hkv, D)
+    ctx, sizes = i32([n, n + 20, 0, 0]), i32([T, 3, 2, 0])
+    new, out, lse = torch.empty_like(ctx), torch.empty(4, T, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(4, T, Hq, device="cuda")
+    took, acc = i32([2, 1, 1, 0]), i32([[1, 4, 0, 0, 0, 0], [2, 0, 0, 0, 0, 0], [0] * 6, [0] * 6])
+    lens = i32([n, n + 5])
+    seq, pos, slots = i32([b for b in range(4) for _ in range(T)]), torch.empty(4 * T, dtype=torch.int32, device="cuda"), None
+    qr, dep = torch.empty_like(q), i32([depth] * 4)
+    slots = torch.empty_like(pos)
+    lst, cnt, gone = torch.full((total,), -7, dtype=torch.int32, device="cuda"), i32([0]), i32([0])
+
+    def reset():
+        pool.copy_(start), tab.copy_(dev(first_tab)), refs.copy_(dev(first_refs)), lst.fill_(-7), out.fill_(0), lse.fill_(0)
+
+    def step():
+        st.kv_fork([0], i2[0], i2[1], lens, spare, tab, refs)
+        ctx[2:].copy_(lens)
+        pos.copy_((ctx[:, None] + dep).view(-1))
+        slots.copy_((ctx[:, None] + ar).view(-1))
+        st.rope_append(0, rope, q, k, v, seq, slots, pos, tab, qr)
+        tree.attention(0, qr.view(4, T, Hq, D), mask, pos.view(4, T), ctx, sizes, tab, out, lse)
+        st.kv_commit([0], acc, took, ctx, tab, new)
+        st.kv_release(gone, None, tab, refs)
+        st.kv_free_pages(refs, lst, cnt)
+
+    i2, ar = (i32([0, 1]), i32([2, 3])), torch.arange(T, dtype=torch.int32, device="cuda")
+    state = lambda: [t.clone() for t in (pool, tab, refs, qr, out, lse, new, lst, cnt)]  # noqa: E731
+    reset(), step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    reset()
+    with torch.cuda.graph(g):
+        step()
+    for change in ((n, n + 5), (16, 33), (0, 47)):
+        lens.copy_(i32(list(change)))
+        q.copy_(x(*q.shape))
+        reset(), step()
+        eager = state()
+        reset(), g.replay()
+        for a, b in zip(eager, state()):
+            assert torch.equal(a, b)
+        assert (eager[1][0] == -1).all() and eager[8].item() == int((eager[2] == 0).sum())
+    # rows of the forks without a page for the drafted tokens are recorded
+    assert st.poll_error() in (B.OPW_OK, B.OPW_ERR_BAD_PAGE)
+
+
+def test_empty_calls_do_nothing():
+    st = make_stage([torch.zeros(2 * 2 * 16 * 64, dtype=torch.bfloat16, device="cuda")], 2, 1, 64, 2, 2)
+    tree, rope = B.TreeAttention(st, 3), B.Rope(64)
+    e = lambda *s, t=torch.int32: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    h = lambda *s: e(*s, t=torch.bfloat16)  # noqa: E731
+    tab, refs = e(2, 2).fill_(-1), e(2).fill_(0)
+    st.rope_append(0, rope, h(0, 2, 64), h(0, 1, 64), h(0, 1, 64), e(0), e(0), e(0), tab, h(0, 2, 64))
+    tree.attention(0, h(0, 3, 2, 64), e(0, 3, t=torch.int64), e(0, 3), e(0), e(0), tab, h(0, 3, 2, 64))
+    st.kv_commit([0], e(0, 3), e(0), e(0), tab, e(0))
+    st.kv_fork([0], e(0), e(0), e(0), e(0), tab, refs)
+    st.kv_release(e(0), None, tab, refs)
+    count = e(1)
+    assert st.launch_count() == 0
+    st.kv_free_pages(refs, e(0), count)          # only counted
+    assert count.item() == 2 and st.poll_error() == B.OPW_OK
+
 
 @pytest.mark.parametrize("window", [0, 24])
 def test_draft_verify_commit_equals_token_by_token(window):
