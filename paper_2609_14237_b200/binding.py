@@ -643,7 +643,7 @@ class Stage:
         self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
         self.max_pages_per_seq, self.layer_num_pages = max_pages_per_seq, [int(n) for n in layer_num_pages]
         # what the short calls look up every time
-        self.index, self._i32, self._bf16 = dev.index or 0, torch.int32, torch.bfloat16
+        self.index, self._i32, self._bf16, self._lib = dev.index or 0, torch.int32, torch.bfloat16, lib()
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self.handle = opw_attn_stage_create(cfg)
 
@@ -692,29 +692,41 @@ class Stage:
         """The current stream of the stage's device, whichever device is current."""
         return self._raw_stream(self.index)
 
-    def _table_ok(self, where, page_table, rows):
-        _need(where, self.index, self._i32, -1, page_table)
-        if page_table.dim() != 2 or page_table.shape[0] < rows or page_table.shape[1] != self.max_pages_per_seq:
+    def _table_rows(self, where, page_table, rows):
+        """The number of rows of a page table that is fit for `rows` sequences."""
+        shape = page_table.shape
+        if len(shape) != 2 or shape[0] < rows or shape[1] != self.max_pages_per_seq:
             raise ValueError(f"{where}: page_table must be [at least {rows}, {self.max_pages_per_seq}]")
+        if page_table.dtype is not self._i32 or page_table.get_device() != self.index or not page_table.is_contiguous():
+            _need(where, self.index, self._i32, -1, page_table)
+        return shape[0]
 
     def rope_append(self, layer, rope, q, k, v, seq, slots, positions, page_table, q_out):
         """Rotate q into q_out, append rotated k and v to the cache; q, k, v: [rows, heads, head_dim], rows may be strided
         (views into one projection).  q = q_out = None: keys and values only."""
-        where, D, rows, dev = "rope_append", self.head_dim, seq.shape[0], self.index
+        where, D, rows, dev, bf16 = "rope_append", self.head_dim, seq.shape[0], self.index, self._bf16
         _need(where, dev, self._i32, rows, seq, slots, positions)
-        self._table_ok(where, page_table, 1)
-        for t, heads in ((k, self.num_kv_heads), (v, self.num_kv_heads)) if q is None else (
-                (q, self.num_q_heads), (k, self.num_kv_heads), (v, self.num_kv_heads)):
-            if t.dtype is not self._bf16 or t.get_device() != dev or t.shape != (rows, heads, D) or t.stride()[1:] != (D, 1):
-                raise ValueError(f"{where}: q, k, v must be bfloat16 [{rows}, heads, {D}] on {self.device} with contiguous heads")
-        if q is not None:
-            _need(where, dev, self._bf16, rows * self.num_q_heads * D, q_out)
+        table_rows = self._table_rows(where, page_table, 1)
+        kv, k_st, v_st = (rows, self.num_kv_heads, D), k.stride(), v.stride()
+        fits = (k.dtype is bf16 and v.dtype is bf16 and k.get_device() == dev and v.get_device() == dev and k.shape == kv and v.shape == kv
+                and k_st[1] == D and v_st[1] == D and k_st[2] == 1 and v_st[2] == 1)
+        q_ptr = out_ptr = None
+        q_stride = 0
+        if fits and q is not None:
+            q_st = q.stride()
+            fits = (q.dtype is bf16 and q.get_device() == dev and q.shape == (rows, self.num_q_heads, D) and q_st[1] == D and q_st[2] == 1)
+            if fits:
+                _need(where, dev, bf16, rows * self.num_q_heads * D, q_out)
+                q_ptr, q_stride, out_ptr = q.data_ptr(), q_st[0], q_out.data_ptr()
+        if not fits:
+            raise ValueError(f"{where}: q, k, v must be bfloat16 [{rows}, heads, {D}] on {self.device} with contiguous heads")
         if rope.table.get_device() != dev:
             raise ValueError(f"{where}: the rotary table is on {rope.table.device}")
-        opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(),
-                        None if q is None else q.data_ptr(), 0 if q is None else q.stride(0), k.data_ptr(), k.stride(0),
-                        v.data_ptr(), v.stride(0), seq.data_ptr(), slots.data_ptr(), positions.data_ptr(), page_table.shape[0],
-                        page_table.data_ptr(), None if q is None else q_out.data_ptr(), self._raw_stream(dev))
+        rc = self._lib.opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(), q_ptr, q_stride,
+                                       k.data_ptr(), k_st[0], v.data_ptr(), v_st[0], seq.data_ptr(), slots.data_ptr(),
+                                       positions.data_ptr(), table_rows, page_table.data_ptr(), out_ptr, self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_rope_append")
 
     def kv_commit(self, layers, accepted, accepted_lens, ctx_lens, page_table, new_lens=None):
         """Move the rows of the accepted nodes together behind each sequence's context, in all of `layers`.  accepted: int32
@@ -723,45 +735,54 @@ class Stage:
         nodes = accepted.shape[1]
         _need(where, dev, self._i32, batch, ctx_lens, accepted_lens)
         _need(where, dev, self._i32, batch * nodes, accepted)
-        self._table_ok(where, page_table, batch)
+        self._table_rows(where, page_table, batch)
         new = None
         if new_lens is not None:
             _need(where, dev, self._i32, batch, new_lens)
             new = new_lens.data_ptr()
-        opw_kv_commit(self.handle, layers, batch, nodes, accepted.data_ptr(), accepted_lens.data_ptr(), ctx_lens.data_ptr(),
-                      page_table.data_ptr(), new, self._raw_stream(dev))
+        rc = self._lib.opw_kv_commit(self.handle, _layer_array(layers), len(layers), batch, nodes, accepted.data_ptr(),
+                                     accepted_lens.data_ptr(), ctx_lens.data_ptr(), page_table.data_ptr(), new, self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_kv_commit")
 
     def kv_fork(self, layers, src_rows, dst_rows, lens, new_pages, page_table, refcounts):
         """Let table rows dst_rows share the first lens tokens of src_rows; a last partial page is copied to new_pages."""
         where, n, dev = "kv_fork", src_rows.shape[0], self.index
         _need(where, dev, self._i32, n, src_rows, dst_rows, lens, new_pages)
         _need(where, dev, self._i32, -1, refcounts)
-        self._table_ok(where, page_table, 1)
+        table_rows = self._table_rows(where, page_table, 1)
         if refcounts.numel() < min(self.layer_num_pages[i] for i in layers):
             raise ValueError(f"{where}: refcounts must have an entry per page")
-        opw_kv_fork(self.handle, layers, n, src_rows.data_ptr(), dst_rows.data_ptr(), lens.data_ptr(), new_pages.data_ptr(),
-                    page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(), self._raw_stream(dev))
+        rc = self._lib.opw_kv_fork(self.handle, _layer_array(layers), len(layers), n, src_rows.data_ptr(), dst_rows.data_ptr(),
+                                   lens.data_ptr(), new_pages.data_ptr(), table_rows, page_table.data_ptr(), refcounts.data_ptr(),
+                                   self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_kv_fork")
 
     def kv_release(self, rows, keep_lens, page_table, refcounts):
         """Drop the pages of table rows behind their first keep_lens tokens (None: all)."""
         where, n, dev = "kv_release", rows.shape[0], self.index
         _need(where, dev, self._i32, n, rows)
         _need(where, dev, self._i32, -1, refcounts)
-        self._table_ok(where, page_table, 1)
+        table_rows = self._table_rows(where, page_table, 1)
         keep = None
         if keep_lens is not None:
             _need(where, dev, self._i32, n, keep_lens)
             keep = keep_lens.data_ptr()
-        opw_kv_release(self.handle, n, rows.data_ptr(), keep, page_table.shape[0], page_table.data_ptr(), refcounts.data_ptr(),
-                       refcounts.numel(), self._raw_stream(dev))
+        rc = self._lib.opw_kv_release(self.handle, n, rows.data_ptr(), keep, table_rows, page_table.data_ptr(), refcounts.data_ptr(),
+                                      refcounts.numel(), self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_kv_release")
 
     def kv_free_pages(self, refcounts, free_list, count):
         """List the pages nobody holds, ascending, in free_list; their number in count."""
         dev = self.index
         _need("kv_free_pages", dev, self._i32, -1, refcounts, free_list)
         _need("kv_free_pages", dev, self._i32, 1, count)
-        opw_kv_free_pages(self.handle, refcounts.data_ptr(), refcounts.numel(), free_list.data_ptr(), free_list.numel(),
-                          count.data_ptr(), self._raw_stream(dev))
+        rc = self._lib.opw_kv_free_pages(self.handle, refcounts.data_ptr(), refcounts.numel(), free_list.data_ptr(), free_list.numel(),
+                                         count.data_ptr(), self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_kv_free_pages")
 
     def packed_host_buffers(self, batch):
         """One pinned host buffer holding q, k_new, v_new, positions at the packed offsets;
@@ -813,23 +834,26 @@ class TreeAttention:
         """q, out: bf16 [batch, nodes, Hq, D]; tree_mask: int64 [batch, nodes] (the bits of a uint64); positions: int32
         [batch, nodes]; lse: fp32 [batch, nodes, Hq] or None."""
         where, st = "tree attention", self.stage
-        batch, nodes, dev = q.shape[0], q.shape[1], st.index
+        shape, dev = q.shape, st.index
         if not st.handle:
             raise ValueError(f"{where}: the stage is closed")
-        if q.shape != (batch, nodes, st.num_q_heads, st.head_dim):
-            raise ValueError(f"{where}: q must be [batch, nodes, {st.num_q_heads}, {st.head_dim}], got {tuple(q.shape)}")
+        if len(shape) != 4 or shape[2] != st.num_q_heads or shape[3] != st.head_dim:
+            raise ValueError(f"{where}: q must be [batch, nodes, {st.num_q_heads}, {st.head_dim}], got {tuple(shape)}")
+        batch, nodes = shape[0], shape[1]
         _need(where, dev, st._bf16, batch * nodes * st.num_q_heads * st.head_dim, q, out)
         _need(where, dev, st._i32, batch, ctx_lens, tree_lens)
         _need(where, dev, st._i32, batch * nodes, positions)
         _need(where, dev, self._i64, batch * nodes, tree_mask)
-        st._table_ok(where, page_table, batch)
+        st._table_rows(where, page_table, batch)
         lse_ptr = None
         if lse is not None:
             _need(where, dev, self._f32, batch * nodes * st.num_q_heads, lse)
             lse_ptr = lse.data_ptr()
-        opw_tree_attention(self.handle, layer, batch, nodes, q.data_ptr(), tree_mask.data_ptr(), positions.data_ptr(),
-                           ctx_lens.data_ptr(), tree_lens.data_ptr(), page_table.data_ptr(), out.data_ptr(), lse_ptr,
-                           st._raw_stream(dev))
+        rc = st._lib.opw_tree_attention(self.handle, layer, batch, nodes, q.data_ptr(), tree_mask.data_ptr(), positions.data_ptr(),
+                                        ctx_lens.data_ptr(), tree_lens.data_ptr(), page_table.data_ptr(), out.data_ptr(), lse_ptr,
+                                        st._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_tree_attention")
 
     def close(self):
         if getattr(self, "handle", None):
