@@ -248,6 +248,7 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
   };
   int64_t wbase = u0;
   Desc wa = describe(u0 + lane), wb = describe(u0 + 32 + lane);
+  pdl_launch_dependents();                    // (as in the tensor-core kernel)
   pdl_wait();                                 // up to here only this step's lengths and the page table were read
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i <= p.batch; i += blockDim.x) p.cum[i] = cum[i];
@@ -482,7 +483,6 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
       on_first_row = false;
     }
   }
-  pdl_launch_dependents();
   if (failed) {
     // A copy did not arrive in time: record it, then give every copy still in flight a bounded chance to land.
     if (lane == 0) atomicOr(p.status, kErrTimeout);
@@ -508,17 +508,15 @@ constexpr int kTreeCombineThreads = 256;
 // partials each, where the walk is a chain of L2 round trips -- the columns go to blocks of their own, the partials are dealt
 // out to that many groups of threads, which meet in shared memory, and eight are in flight per thread.  (One sequence of 8000
 // keys, 125 partials a row: 21 us with whole rows and four groups of two in flight, 19 us this way and on the tensor-core kernel.)
+// It adds 4 us to a call of one short sequence and 6 to 64 trees of 8 (measured by leaving it out): a launch and its round trips.
 template <int D, int kGroups, int V>
-__global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const TreeCombineParams c) {
-  constexpr int kRows = 32 / kGroups, kDeep = V == 1 ? 8 : V >= 8 ? 2 : 4;     // partials in flight
+__global__ void __launch_bounds__(kTreeCombineThreads, V == 1 ? 1 : D == 256 ? 2 : 3) tree_combine_kernel(const TreeCombineParams c) {
+  constexpr int kRows = 32 / kGroups, kDeep = V == 1 ? 8 : 2;     // partials in flight (with four, two blocks an SM)
   const TreeParams& p = c.t;
   __shared__ int32_t slot_s[kTreeCombineThreads];
   __shared__ float4 acc_s[kGroups > 1 ? kTreeCombineThreads : 1][kGroups > 1 ? V : 1];
   __shared__ float2 ml_s[kGroups > 1 ? kTreeCombineThreads : 1];
-  pdl_launch_dependents();
-  pdl_wait();
   const int rb = blockIdx.x % c.max_blocks, bg = blockIdx.x / c.max_blocks, g = bg % p.Hkv, b = bg / p.Hkv;
-  const int64_t U = p.cum[p.batch], before = p.cum[b];           // asked for together with the lengths
   const Span s = span_of(p, b, c.row_block);
   const int live = s.tree * p.G;
   const int lane8 = (threadIdx.x & 7) + 8 * V * blockIdx.z, group = threadIdx.x / (8 * kRows);
@@ -526,6 +524,9 @@ __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const
   const int32_t cnt = tiles_of(s, c.keys);
   const int node = R / p.G;
   const int64_t row = ((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
+  pdl_launch_dependents();
+  pdl_wait();                                                    // up to here only the lengths were read
+  const int64_t U = p.cum[p.batch], before = p.cum[b];
   if ((cnt == 0 || R >= live) && R < p.nodes * p.G && group == 0) {
     // a node that is not there (or a sequence without a key): zeros
 #pragma unroll
