@@ -26,7 +26,7 @@ constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the sha
 // Which kernel.  The tensor-core kernel reads a key tile once for 128 or 256 rows, a CTA at a time; the warp kernel once for 16 rows, a page
 // and a warp at a time.  Measured at 32/8 heads of 128, us:
 //   up to 16 rows, many sequences (64 of 1k to 4k keys, trees of 2 and 4)    warp 116 and 121, tensor core 132 and 135
-//   up to 16 rows, fewer heads than twice the SMs (1 sequence of 1000 keys)  warp 14.7, tensor core 12.5: a partial per CTA, not per warp
+//   up to 16 rows, fewer heads than twice the SMs (1 sequence of 1000 keys)  warp 14.7, tensor core 12.5 (now 11.5): a partial per CTA, not per warp
 //   17 to 32 rows (64 sequences, trees of 8)   warp, with two row tiles a warp, 139; tensor core 130
 //   beyond, the warp kernel would read the cache once per 16 rows (16 x 32k keys, 256 rows: 3133; tensor core 560)
 // The wide instance (two query tiles in shared memory) from 129 rows on; for up to 128 rows the narrow one with its deeper ring (130 against

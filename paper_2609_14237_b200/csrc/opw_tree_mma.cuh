@@ -19,7 +19,7 @@
 // The running maximum is only raised when a row's new maximum exceeds it by 2^8: P stays below 2^8, exact in the same
 // relative sense, and O is rescaled a few times per row instead of once per tile.
 //
-// Measured, 32/8 heads of 128.  Narrow, 32 sequences with a window of 4096 and trees of 26: 109 us, 553 MB, 5.1 TB/s; bound by the bytes in
+// Measured, 32/8 heads of 128.  Narrow, 32 sequences with a window of 4096 and trees of 26: 111 us, 553 MB, 5.0 TB/s; bound by the bytes in
 // flight (the tensor pipe is 35 % busy).  Wide, 16 sequences of 32k keys and trees of 64 (550 GFLOP on 2.2 GB): 565 us, 0.97 PFLOP/s, 60 % of
 // what a library matrix product reaches.  There the chain bounds it: with N = 64 keys an MMA takes 48 cycles (64 with N = 128, which shared
 // memory sets), so 128 keys of both slots want 2400 cycles of the tensor core, and the issue waits for the softmax on top; with the
@@ -252,8 +252,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   const bool spare = blockIdx.x >= workers;           // fewer units than blocks
   const int64_t u0 = spare ? U : worker_begin(U, blockIdx.x, workers), u1 = spare ? U : worker_begin(U, blockIdx.x + 1, workers);
   // The combine kernel may queue up behind the first blocks that finish: its blocks do not fit beside one of these (registers), and
-  // where they wait they have their index work behind them.  (Released at the end instead: chain of 4 12.2 us, now 11.5; 32 x window
-  // 4096 129 to 145 us in the same loop, now 110 to 112.)
+  // where they wait they have their index work behind them.  (Released at the end instead, in a replayed graph: chain of 4
+  // 12.2 us, this way 11.8; 32 x window 4096 133 to 145 us, this way 111 to 113; call by call there is no difference.)
   pdl_launch_dependents();
   pdl_wait();                                         // up to here only this step's lengths were read
   if (blockIdx.x == 0)
