@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       mbar_init(smem_u32(&p_bar[0][0] + i), 4);       // a lane of each warp
       mbar_init(smem_u32(&o_bar[0][0] + i), 1);
     }
-    mbar_init(smem_u32(&seg_bar), 256);
+    mbar_init(smem_u32(&seg_bar), 256 + 2);           // the softmax threads and both MMA issuers (at the issuers' loop)
     mbar_init(smem_u32(&end_bar[0]), 1);
     mbar_init(smem_u32(&end_bar[1]), 1);
     dead_s = 0;
@@ -356,6 +356,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       const Segment s = segment_at<C::kRows>(p, cum, u, u1);
       const uint32_t step = s.shared ? 1u : 2u, end = tiles + (uint32_t)s.n;
       uint32_t t = s.shared ? tiles : tiles + x;
+      // An issuer arrives for a segment itself, and only once it has seen the one before: its waits go by parity, and a slot without
+      // a tile in a segment (one tile, alternating slots) would otherwise let its softmax threads and the other slot complete the
+      // barrier twice while this warp has not looked once.
+      __syncwarp();
+      if (el) mbar_arrive(smem_u32(&seg_bar));
       if (!wait(&seg_bar, n_seg++ & 1u)) break;
       tc_after();
       if (t < end && !scores(t, mine)) break;
