@@ -170,7 +170,7 @@ __device__ __forceinline__ int32_t window_border(const TreeParams& p, int b, con
   if (p.window == 0) return 0;
   int32_t border = s.lo;
   const int32_t* pos = p.positions + (int64_t)b * p.nodes;
-  for (int i = lane; i < s.tree; i += 32) border = max(border, pos[i] - p.window + 1);
+  for (int i = lane; i < s.tree; i += 32) border = max(border, max(pos[i], s.ctx) - p.window + 1);
   return __reduce_max_sync(0xffffffffu, border);
 }
 __device__ __forceinline__ bool any_not_finite(const uint4& w) {   // of eight bf16

@@ -51,3 +51,28 @@ def test_runs_of_row_blocks_of_one_key_tile(Hq, Hkv, D, T, long):
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
     assert st.poll_error() == B.OPW_OK
     check_tree(first[0], first[1], [many(a) for a in ref], 300)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(32, 8, 128), (8, 2, 64), (16, 2, 256)])
+def test_positions_far_below_the_context_count_as_its_length(Hq, Hkv, D):
+    """A position below the context's length counts as that length, the type's lowest value too: the same bits.  (A hidden key would
+    show, and so would another path through the kernel: the infinity sits at a key whose weight has left the range of 32 bits.)"""
+    rng = np.random.default_rng(2100 + D)
+    T, ctx, size = 5, [1000, 300], [5, 4]
+    pool, tab, q, mask, _ = tree_inputs(rng, ctx, size, T, Hq, Hkv, D)
+    q = oracle.f32_to_bf16_bits(np.ones((2, T, Hq, D), np.float32))
+    far = oracle.f32_to_bf16_bits(np.full((Hkv, D), -32.0, np.float32))
+    for b in range(2):
+        v = rand_bits(rng, (Hkv, D))
+        v[:, 3] = 0x7F80
+        draft._put_row(pool, Hkv, D, tab[b, 0], 5, far, v)
+    st = make_stage([dev(pool, True)], Hq, Hkv, D, 2, tab.shape[1], window=2000)
+    tree, res = B.TreeAttention(st, T), []
+    for low in (None, 0, -(1 << 31)):
+        at = np.tile(np.asarray(ctx, np.int32)[:, None], (1, T)) if low is None else np.full((2, T), low, np.int32)
+        out, lse = torch.empty(2, T, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(2, T, Hq, device="cuda")
+        tree.attention(0, dev(q, True), dev(mask), dev(at), dev(np.array(ctx, np.int32)), dev(np.array(size, np.int32)), dev(tab), out, lse)
+        res.append((out.view(torch.int16), lse.view(torch.int32)))
+    assert st.poll_error() == B.OPW_OK
+    for out, lse in res[1:]:
+        assert torch.equal(out, res[0][0]) and torch.equal(lse, res[0][1])
