@@ -522,7 +522,8 @@ def opw_rope_append(stage: int, layer: int, rows: int, rotary_dim: int, layout: 
 
 
 def opw_tree_mask(parents: Sequence[int]):
-    """(mask words, depths) of a tree given by each node's parent (-1: the committed context)."""
+    """(mask words, depths) of a tree given by each node's parent (-1: the committed context).  The words are unsigned: a tensor of
+    those of a full tree of 64 needs dtype=torch.uint64."""
     n = len(parents)
     par, mask, depth = (ctypes.c_int32 * n)(*parents), (ctypes.c_uint64 * n)(), (ctypes.c_int32 * n)()
     _check(lib().opw_tree_mask(n, par, mask, depth), "opw_tree_mask")
@@ -822,7 +823,7 @@ class TreeAttention:
     def __init__(self, stage: Stage, max_nodes: int = OPW_TREE_MAX_NODES):
         import torch
 
-        self.stage, self.max_nodes, self._i64, self._f32 = stage, max_nodes, torch.int64, torch.float32
+        self.stage, self.max_nodes, self._u64, self._i64, self._f32 = stage, max_nodes, torch.uint64, torch.int64, torch.float32
         nbytes = opw_tree_attn_workspace_bytes(stage.handle, max_nodes)
         if nbytes == 0:
             raise OpwError(OPW_ERR_INVALID_ARG, "opw_tree_attn_workspace_bytes")
@@ -831,8 +832,8 @@ class TreeAttention:
         self.handle = opw_tree_attn_create(stage.handle, max_nodes, base, nbytes)
 
     def attention(self, layer, q, tree_mask, positions, ctx_lens, tree_lens, page_table, out, lse=None):
-        """q, out: bf16 [batch, nodes, Hq, D]; tree_mask: int64 [batch, nodes] (the bits of a uint64); positions: int32
-        [batch, nodes]; lse: fp32 [batch, nodes, Hq] or None."""
+        """q, out: bf16 [batch, nodes, Hq, D]; tree_mask: uint64 [batch, nodes], or int64 with the same bits; positions:
+        int32 [batch, nodes]; lse: fp32 [batch, nodes, Hq] or None."""
         where, st = "tree attention", self.stage
         shape, dev = q.shape, st.index
         if not st.handle:
@@ -843,7 +844,7 @@ class TreeAttention:
         _need(where, dev, st._bf16, batch * nodes * st.num_q_heads * st.head_dim, q, out)
         _need(where, dev, st._i32, batch, ctx_lens, tree_lens)
         _need(where, dev, st._i32, batch * nodes, positions)
-        _need(where, dev, self._i64, batch * nodes, tree_mask)
+        _need(where, dev, self._u64 if tree_mask.dtype is self._u64 else self._i64, batch * nodes, tree_mask)
         st._table_rows(where, page_table, batch)
         lse_ptr = None
         if lse is not None:

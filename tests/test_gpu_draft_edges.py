@@ -76,3 +76,27 @@ def test_positions_far_below_the_context_count_as_its_length(Hq, Hkv, D):
     assert st.poll_error() == B.OPW_OK
     for out, lse in res[1:]:
         assert torch.equal(out, res[0][0]) and torch.equal(lse, res[0][1])
+
+
+def test_masks_of_full_trees_as_unsigned_words():
+    """The words that opw_tree_mask returns for a tree of 64 do not all fit a signed 64-bit integer: as torch.uint64 they are taken as
+    they are."""
+    rng = np.random.default_rng(2150)
+    Hq, Hkv, D, T = 8, 2, 64, 64
+    pool, tab, q, _, _ = tree_inputs(rng, [40], [T], T, Hq, Hkv, D)
+    words, depth = B.opw_tree_mask([i - 1 for i in range(T)])
+    mask = torch.tensor([words], dtype=torch.uint64, device="cuda")
+    pos = 40 + np.array([depth], np.int32)
+    ref = draft.tree_attention(pool, Hq, Hkv, D, q, np.array([words], np.uint64), pos, [40], [T], tab)
+    st = make_stage([dev(pool, True)], Hq, Hkv, D, 1, tab.shape[1])
+    tree = B.TreeAttention(st, T)
+    out, lse = torch.empty(1, T, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(1, T, Hq, device="cuda")
+    args = dev(pos), dev(np.array([40], np.int32)), dev(np.array([T], np.int32)), dev(tab)
+    tree.attention(0, dev(q, True), mask, *args, out, lse)
+    assert st.poll_error() == B.OPW_OK
+    check_tree(out, lse, ref, 104)
+    signed = torch.empty_like(out)
+    tree.attention(0, dev(q, True), mask.view(torch.int64), *args, signed)
+    assert torch.equal(signed, out)
+    with pytest.raises(ValueError):
+        tree.attention(0, dev(q, True), mask.view(torch.float64), *args, out)
