@@ -708,23 +708,26 @@ class Stage:
         where, D, rows, dev, bf16 = "rope_append", self.head_dim, seq.shape[0], self.index, self._bf16
         _need(where, dev, self._i32, rows, seq, slots, positions)
         table_rows = self._table_rows(where, page_table, 1)
-        kv, k_st, v_st = (rows, self.num_kv_heads, D), k.stride(), v.stride()
+        Hq, Hkv = self.num_q_heads, self.num_kv_heads
+        kv, k_st, v_st = (rows, Hkv, D), k.stride(), v.stride()
         fits = (k.dtype is bf16 and v.dtype is bf16 and k.get_device() == dev and v.get_device() == dev and k.shape == kv and v.shape == kv
-                and k_st[1] == D and v_st[1] == D and k_st[2] == 1 and v_st[2] == 1)
+                and (Hkv == 1 or (k_st[1] == D and v_st[1] == D)) and k_st[2] == 1 and v_st[2] == 1)
         q_ptr = out_ptr = None
         q_stride = 0
         if fits and q is not None:
             q_st = q.stride()
-            fits = (q.dtype is bf16 and q.get_device() == dev and q.shape == (rows, self.num_q_heads, D) and q_st[1] == D and q_st[2] == 1)
+            fits = q.dtype is bf16 and q.get_device() == dev and q.shape == (rows, Hq, D) and (Hq == 1 or q_st[1] == D) and q_st[2] == 1
             if fits:
-                _need(where, dev, bf16, rows * self.num_q_heads * D, q_out)
-                q_ptr, q_stride, out_ptr = q.data_ptr(), q_st[0], q_out.data_ptr()
+                _need(where, dev, bf16, rows * Hq * D, q_out)
+                q_ptr, q_stride, out_ptr = q.data_ptr(), q_st[0] if rows != 1 else Hq * D, q_out.data_ptr()
         if not fits:
             raise ValueError(f"{where}: q, k, v must be bfloat16 [{rows}, heads, {D}] on {self.device} with contiguous heads")
         if rope.table.get_device() != dev:
             raise ValueError(f"{where}: the rotary table is on {rope.table.device}")
+        # (the stride of a single row says nothing, as that of a single head)
+        k_stride, v_stride = (k_st[0], v_st[0]) if rows != 1 else (Hkv * D, Hkv * D)
         rc = self._lib.opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(), q_ptr, q_stride,
-                                       k.data_ptr(), k_st[0], v.data_ptr(), v_st[0], seq.data_ptr(), slots.data_ptr(),
+                                       k.data_ptr(), k_stride, v.data_ptr(), v_stride, seq.data_ptr(), slots.data_ptr(),
                                        positions.data_ptr(), table_rows, page_table.data_ptr(), out_ptr, self._raw_stream(dev))
         if rc:
             _check(rc, "opw_rope_append")

@@ -100,3 +100,30 @@ def test_masks_of_full_trees_as_unsigned_words():
     assert torch.equal(signed, out)
     with pytest.raises(ValueError):
         tree.attention(0, dev(q, True), mask.view(torch.float64), *args, out)
+
+
+def test_rotary_append_ignores_strides_of_single_rows_and_heads():
+    """The stride of an axis of one element says nothing: torch calls such tensors contiguous whatever it is."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(21)
+    x = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    rope, tab = B.Rope(64), i32([[0, 1]])
+    for Hq, Hkv, rows in ((4, 1, 3), (4, 2, 1), (1, 1, 5), (1, 1, 1)):
+        q, k, v = (x(h, rows, 64).transpose(0, 1) for h in (Hq, Hkv, Hkv))
+        if rows > 1 and Hq > 1:
+            q = q.contiguous()
+        pools = [torch.zeros(2 * Hkv * 2 * 16 * 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        at, seq, res = i32(list(range(7, 7 + rows))), i32([0] * rows), []
+        for pool, plain in zip(pools, (True, False)):
+            st = make_stage([pool], Hq, Hkv, 64, 1, 2)
+            plain_of = lambda t: torch.empty(t.shape, dtype=t.dtype, device="cuda").copy_(t)  # noqa: E731
+            a, b, c = (plain_of(t) if plain else t for t in (q, k, v))
+            out = torch.empty(rows, Hq, 64, dtype=torch.bfloat16, device="cuda")
+            st.rope_append(0, rope, a, b, c, seq, at, at, tab, out)
+            assert st.poll_error() == B.OPW_OK
+            res.append(out)
+            if rows == 1 and not plain:                          # in place too
+                st.rope_append(0, rope, a, b, c, seq, at, at, tab, a)
+                assert torch.equal(a, out)
+        assert torch.equal(res[0], res[1]) and torch.equal(pools[0], pools[1])
