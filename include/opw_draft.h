@@ -162,7 +162,8 @@ opw_status_t opw_tree_attention(opw_tree_attn_t *tree, int32_t layer, int32_t ba
  * m = accepted_lens[b], cached row c + i takes what row c + accepted[b,i] held before the call, for i < m, bit for
  * bit, keys and values of all heads.  (A gather: accepted may name a row twice; an accepted path lists ascending
  * nodes.)  Rows from c + m on are left as they are.  new_lens[b] = c + m (c where c < 0; m < 0 counts as 0).  An accepted
- * node outside [0, nodes) or a bad page skips its row, m > nodes is cut to nodes; both are recorded.
+ * node outside [0, nodes) or a bad page skips its row (a row that is in place already has its page looked at too), m > nodes is
+ * cut to nodes; both are recorded.  new_lens counts skipped rows all the same.
  *   layers     : HOST int32 [num_layers], layers that share the page table, without repetition
  *   accepted   : DEVICE int32 [batch, nodes], 1 <= nodes <= OPW_TREE_MAX_NODES
  *   accepted_lens, ctx_lens : DEVICE int32 [batch]

@@ -302,7 +302,6 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_con
     to[u] = -1;
     if (i >= m) continue;
     const int32_t a = p.accepted[(int64_t)b * p.nodes + i];
-    if (a == i) continue;                          // already in place
     int64_t from = -1;
     if (a >= 0 && a < p.nodes) {
       from = place(a, c);
@@ -311,6 +310,10 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const __grid_con
     if (from < 0 || to[u] < 0) {
       to[u] = -1;
       atomicOr(p.status, kErrBadPage);
+      continue;
+    }
+    if (a == i) {                                  // already in place: looked up all the same, for the record (0.2 us more where all are: 1.5 -> 1.7)
+      to[u] = -1;
       continue;
     }
 #pragma unroll

@@ -127,3 +127,21 @@ def test_rotary_append_ignores_strides_of_single_rows_and_heads():
                 st.rope_append(0, rope, a, b, c, seq, at, at, tab, a)
                 assert torch.equal(a, out)
         assert torch.equal(res[0], res[1]) and torch.equal(pools[0], pools[1])
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_commit_records_rows_in_place_on_bad_pages(D):
+    """An accepted row that is in its place already has nothing to move, but a page or a slot that does not exist is recorded."""
+    rng = np.random.default_rng(2300 + D)
+    Hkv, T, width = 2, 6, 3
+    pool = rand_bits(rng, oracle.pool_elems(8, Hkv, P, D))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    for table, ctx, took, status in (([[5, 2, 7]], 14, 4, B.OPW_OK), ([[5, -1, 7]], 14, 4, B.OPW_ERR_BAD_PAGE), ([[5, -1, 7]], 14, 2, B.OPW_OK),
+                                     ([[5, 8, 7]], 15, 3, B.OPW_ERR_BAD_PAGE), ([[5, 2, 7]], 46, 2, B.OPW_OK),
+                                     ([[5, 2, 7]], 46, 3, B.OPW_ERR_BAD_PAGE)):
+        d_pool = dev(pool, True)
+        st = make_stage([d_pool], Hkv, Hkv, D, 1, width)
+        new = i32([-9])
+        st.kv_commit([0], i32([list(range(T))]), i32([took]), i32([ctx]), i32(table), new)
+        assert st.poll_error() == status, (table, ctx, took)
+        assert new.item() == ctx + took and (host_bits(d_pool) == pool).all()
