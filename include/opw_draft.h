@@ -167,7 +167,7 @@ opw_status_t opw_tree_attention(opw_tree_attn_t *tree, int32_t layer, int32_t ba
  *   layers     : HOST int32 [num_layers], layers that share the page table, without repetition
  *   accepted   : DEVICE int32 [batch, nodes], 1 <= nodes <= OPW_TREE_MAX_NODES
  *   accepted_lens, ctx_lens : DEVICE int32 [batch]
- *   new_lens   : DEVICE int32 [batch] or NULL; must not overlap ctx_lens or accepted_lens
+ *   new_lens   : DEVICE int32 [batch] or NULL; must not overlap any of the inputs
  * Sequences must not share the pages of their drafted rows (they never do while only whole, full pages are shared).
  */
 opw_status_t opw_kv_commit(opw_attn_stage_t *stage, const int32_t *layers, int32_t num_layers, int32_t batch, int32_t nodes,

@@ -465,9 +465,10 @@ extern "C" opw_status_t opw_kv_commit(opw_attn_stage_t* stage, const int32_t* la
   if (((uintptr_t)accepted | (uintptr_t)accepted_lens | (uintptr_t)ctx_lens | (uintptr_t)page_table | (uintptr_t)new_lens) % 4)
     return OPW_ERR_INVALID_ARG;
   if (batch > s.max_batch) return OPW_ERR_CAPACITY;
-  const uintptr_t n0 = (uintptr_t)new_lens, n1 = n0 + (size_t)batch * 4;
-  for (const int32_t* in : {accepted_lens, ctx_lens})
-    if (new_lens && n0 < (uintptr_t)in + (size_t)batch * 4 && (uintptr_t)in < n1) return OPW_ERR_INVALID_ARG;
+  const size_t per_seq = (size_t)batch * 4;
+  if (new_lens && (opw_overlap(new_lens, per_seq, accepted_lens, per_seq) || opw_overlap(new_lens, per_seq, ctx_lens, per_seq) ||
+                   opw_overlap(new_lens, per_seq, accepted, per_seq * nodes) || opw_overlap(new_lens, per_seq, page_table, per_seq * s.max_pages)))
+    return OPW_ERR_INVALID_ARG;
   opw_draft::CommitParams p;
   p.accepted = accepted;
   p.accepted_lens = accepted_lens;

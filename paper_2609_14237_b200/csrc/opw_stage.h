@@ -1,6 +1,8 @@
 // What the translation units beside opw_attn.cu need of a stage: a view of its static part, a launch helper, and a
 // guard that makes the stage's device current for the length of a call.  Not part of the ABI.
 #pragma once
+#include <cstdint>
+
 #include <cuda_runtime.h>
 
 #include "opw_attn.h"
@@ -37,6 +39,11 @@ class opw_device_guard {
   int before_;
   bool ok_;
 };
+
+// Do [a, a + an) and [b, b + bn) share a byte?
+inline bool opw_overlap(const void* a, size_t an, const void* b, size_t bn) {
+  return reinterpret_cast<uintptr_t>(a) < reinterpret_cast<uintptr_t>(b) + bn && reinterpret_cast<uintptr_t>(b) < reinterpret_cast<uintptr_t>(a) + an;
+}
 
 // Launch with (or without) programmatic stream serialisation; see launch() in opw_attn.cu.
 template <typename... KArgs, typename... Args>

@@ -145,3 +145,19 @@ def test_commit_records_rows_in_place_on_bad_pages(D):
         st.kv_commit([0], i32([list(range(T))]), i32([took]), i32([ctx]), i32(table), new)
         assert st.poll_error() == status, (table, ctx, took)
         assert new.item() == ctx + took and (host_bits(d_pool) == pool).all()
+
+
+def test_commit_refuses_lengths_that_overlap_what_it_reads():
+    """new_lens is written while other blocks still read the path and the page table."""
+    st = make_stage([torch.zeros(4 * 2 * 16 * 64, dtype=torch.bfloat16, device="cuda")], 1, 1, 64, 4, 2)
+    buf = torch.zeros(64, dtype=torch.int32, device="cuda")
+    base, h = buf.data_ptr(), B.lib()
+    layers = (B.ctypes.c_int32 * 1)(0)
+    # accepted [2, 3] at 0..5, accepted_lens at 8, ctx_lens at 12, page table [2, 2] at 16..19
+    call = lambda new: h.opw_kv_commit(st.handle, layers, 1, 2, 3, base, base + 32, base + 48, base + 64, new, None)  # noqa: E731
+    for at in (0, 1, 5, 7, 8, 9, 11, 12, 13, 15, 16, 19):
+        assert call(base + 4 * at) == B.OPW_ERR_INVALID_ARG, at
+    assert st.launch_count() == 0
+    for at in (6, 10, 14, 20):
+        assert call(base + 4 * at) == B.OPW_OK, at
+    torch.cuda.synchronize()
