@@ -139,7 +139,7 @@ opw_status_t opw_tree_attn_destroy(opw_tree_attn_t *tree); /* NULL is accepted *
  * A node that sees nothing, nodes i >= t and inactive sequences (c < 0 or t <= 0) get out = 0, lse = -inf.
  * t > nodes, rows beyond the table and bad page ids are cut off or masked out and recorded as OPW_ERR_BAD_PAGE.
  *   nodes      : 1..max_nodes, the row stride of q, tree_mask, positions, out and lse
- *   q, out     : DEVICE bf16 [batch, nodes, Hq, D], 16-byte aligned; out must not overlap q
+ *   q, out     : DEVICE bf16 [batch, nodes, Hq, D], 16-byte aligned; out and lse must not overlap each other or any of the inputs
  *   tree_mask  : DEVICE uint64 [batch, nodes], 8-byte aligned
  *   positions  : DEVICE int32 [batch, nodes]; read on window layers only
  *   ctx_lens, tree_lens : DEVICE int32 [batch]

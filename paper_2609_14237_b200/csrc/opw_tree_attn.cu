@@ -198,8 +198,15 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
       ((uintptr_t)positions | (uintptr_t)ctx_lens | (uintptr_t)tree_lens | (uintptr_t)page_table | (uintptr_t)lse) % 4)
     return OPW_ERR_INVALID_ARG;
   if (nodes > tree->max_nodes || batch > v.max_batch || batch > opw_tree::kMaxTreeBatch) return OPW_ERR_CAPACITY;
-  const size_t bytes = (size_t)batch * nodes * v.Hq * v.D * 2;
-  if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return OPW_ERR_INVALID_ARG;
+  // what is written must not meet what other blocks still read
+  const size_t rows = (size_t)batch * nodes, lse_bytes = lse ? rows * v.Hq * 4 : 0, out_bytes = rows * v.Hq * v.D * 2;
+  auto meets = [&](const void* in, size_t bytes) {
+    return opw_overlap(out, out_bytes, in, bytes) || (lse && opw_overlap(lse, lse_bytes, in, bytes));
+  };
+  if (meets(q, out_bytes) || meets(tree_mask, rows * 8) || meets(positions, rows * 4) || meets(ctx_lens, (size_t)batch * 4) ||
+      meets(tree_lens, (size_t)batch * 4) || meets(page_table, (size_t)batch * v.max_pages * 4) ||
+      (lse && opw_overlap(lse, lse_bytes, out, out_bytes)))
+    return OPW_ERR_INVALID_ARG;
   const Variant k = pick(v, nodes, batch);
   opw_tree::TreeCombineParams c;
   opw_tree::TreeParams& p = c.t;

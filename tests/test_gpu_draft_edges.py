@@ -161,3 +161,25 @@ def test_commit_refuses_lengths_that_overlap_what_it_reads():
     for at in (6, 10, 14, 20):
         assert call(base + 4 * at) == B.OPW_OK, at
     torch.cuda.synchronize()
+
+
+def test_tree_attention_refuses_outputs_that_overlap():
+    """out and lse are written while other blocks still read the inputs."""
+    st = make_stage([torch.zeros(4 * 2 * 16 * 64, dtype=torch.bfloat16, device="cuda")], 1, 1, 64, 2, 2)
+    tree = B.TreeAttention(st, 3)
+    buf = torch.zeros(8192, dtype=torch.uint8, device="cuda")
+    base, h = buf.data_ptr(), B.lib()
+    at = dict(q=0, mask=1024, pos=1088, ctx=1120, sizes=1136, table=1152, out=2048, lse=4096)    # [2, 3, 1, 64]: q and out 768 bytes
+
+    def call(**other):
+        a = {k: base + v for k, v in {**at, **other}.items()}
+        return h.opw_tree_attention(tree.handle, 0, 2, 3, a["q"], a["mask"], a["pos"], a["ctx"], a["sizes"], a["table"], a["out"], a["lse"],
+                                    None)
+
+    for other in (dict(lse=0), dict(lse=764), dict(lse=1024), dict(lse=1068), dict(lse=1088), dict(lse=1120), dict(lse=1136), dict(lse=1164),
+                  dict(lse=2048), dict(lse=2812), dict(out=512), dict(out=1024), dict(out=1152), dict(out=400)):
+        assert call(**other) == B.OPW_ERR_INVALID_ARG, other
+    assert st.launch_count() == 0
+    assert call() == call(lse=2816) == call(lse=1168) == B.OPW_OK
+    torch.cuda.synchronize()
+    assert st.poll_error() == B.OPW_OK
