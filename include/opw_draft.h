@@ -88,7 +88,7 @@ opw_status_t opw_rope_table(const opw_rope_config_t *cfg, double *table_host);
  *                elements, multiples of 8, at least a row's length (views into one packed projection are fine);
  *                16-byte aligned
  *   q_out      : DEVICE bf16 [rows, Hq, D], 16-byte aligned; may be q itself if q_stride == Hq * D, must not
- *                overlap q, k or v in any other way; q == q_out == NULL: keys and values only
+ *                overlap q in any other way, nor any other input; q == q_out == NULL: keys and values only
  *   seq, slots, positions : DEVICE int32 [rows]
  *   page_table : DEVICE int32 [num_rows, max_pages_per_seq], num_rows >= 1
  */

@@ -405,11 +405,12 @@ extern "C" opw_status_t opw_rope_append(opw_attn_stage_t* stage, int32_t layer, 
     return OPW_ERR_INVALID_ARG;
   if (q && q == q_out && q_stride != q_row) return OPW_ERR_INVALID_ARG;
   // q_out is written while other rows are still read: it may be q, but not meet the inputs in any other way
-  auto meets = [&](const void* in, int64_t stride, int64_t row) {
-    const uintptr_t a = (uintptr_t)in, o = (uintptr_t)q_out;
-    return a < o + (uintptr_t)rows * q_row * 2 && o < a + ((uintptr_t)(rows - 1) * stride + row) * 2;
-  };
-  if (q && ((q != q_out && meets(q, q_stride, q_row)) || meets(k, k_stride, kv_row) || meets(v, v_stride, kv_row)))
+  const size_t out_bytes = (size_t)rows * q_row * 2;
+  auto meets = [&](const void* in, size_t bytes) { return opw_overlap(q_out, out_bytes, in, bytes); };
+  auto rows_of = [&](int64_t stride, int64_t row) { return ((size_t)(rows - 1) * stride + row) * 2; };
+  if (q && ((q != q_out && meets(q, rows_of(q_stride, q_row))) || meets(k, rows_of(k_stride, kv_row)) || meets(v, rows_of(v_stride, kv_row)) ||
+            meets(seq, (size_t)rows * 4) || meets(slots, (size_t)rows * 4) || meets(positions, (size_t)rows * 4) ||
+            meets(table, (size_t)(rotary_dim / 2 + 1) * 8) || meets(page_table, (size_t)num_rows * s.max_pages * 4)))
     return OPW_ERR_INVALID_ARG;
   opw_draft::RopeParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);

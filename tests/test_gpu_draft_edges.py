@@ -183,3 +183,24 @@ def test_tree_attention_refuses_outputs_that_overlap():
     assert call() == call(lse=2816) == call(lse=1168) == B.OPW_OK
     torch.cuda.synchronize()
     assert st.poll_error() == B.OPW_OK
+
+
+def test_rotary_append_refuses_queries_over_what_it_reads():
+    """q_out is written while other rows' numbers are still read."""
+    st = make_stage([torch.zeros(4 * 2 * 16 * 64, dtype=torch.bfloat16, device="cuda")], 1, 1, 64, 2, 2)
+    buf = torch.zeros(8192, dtype=torch.uint8, device="cuda")
+    base, h = buf.data_ptr(), B.lib()
+    at = dict(table=64, q=512, k=1152, v=1792, seq=2448, slots=2480, pos=2512, pages=2544, out=4096)    # 5 rows of 128 bytes
+    buf[2448:2448 + 20] = 255                                    # padding rows: nothing is read or written for them
+
+    def call(out):
+        a = {k: base + x for k, x in at.items()}
+        return h.opw_rope_append(st.handle, 0, 5, 64, 0, a["table"], a["q"], 64, a["k"], 64, a["v"], 64, a["seq"], a["slots"], a["pos"], 2,
+                                 a["pages"], base + out, None)
+
+    for out in (0, 320, 528, 1104, 1776, 1936, 2432, 2464, 2480, 2496, 2544):
+        assert call(out) == B.OPW_ERR_INVALID_ARG, out
+    assert st.launch_count() == 0
+    assert call(512) == call(2560) == call(4096) == B.OPW_OK
+    torch.cuda.synchronize()
+    assert st.poll_error() == B.OPW_OK
