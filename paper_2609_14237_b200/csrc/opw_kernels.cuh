@@ -267,6 +267,7 @@ struct ShareMath {
   }
 };
 
+#ifndef OPW_NO_STAGE_KERNELS    // (a unit under another namespace has no use for a second copy)
 // ---------------------------------------------------------------------------------
 // KV append: one thread block per sequence, one thread per 16-byte group
 // ---------------------------------------------------------------------------------
@@ -371,6 +372,7 @@ __global__ void __launch_bounds__(256) read_probe_kernel(const uint4* __restrict
     sink[blockIdx.x] = __uint_as_float(t & 0x3fffffffu);   // any value: it only has to depend on every load
   }
 }
+#endif  // OPW_NO_STAGE_KERNELS
 
 // ---------------------------------------------------------------------------------
 // split-KV partial attention

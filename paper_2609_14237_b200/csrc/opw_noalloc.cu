@@ -25,6 +25,7 @@
 #include "opw_attn.h"
 
 #define OPW_NAMESPACE opw_na
+#define OPW_NO_STAGE_KERNELS
 #undef OPW_DYN_PER_SHARE
 #define OPW_DYN_PER_SHARE 0
 #include "opw_kernels.cuh"

@@ -14,6 +14,7 @@
 #pragma once
 
 #define OPW_NAMESPACE opw_tree
+#define OPW_NO_STAGE_KERNELS
 #include "opw_kernels.cuh"
 
 namespace opw_tree {
