@@ -368,6 +368,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       bool ok = true;
       for (; t < end; t += step, ++mine) {
         const uint32_t st = t % NV, buf = mine & 1u, phase = (mine >> 1) & 1u;
+        __syncwarp();                                // no lane's wait falls two phases behind the elected one
         ok = wait_at(vf + 8 * st, (t / NV) & 1u) && wait_at(pb + 8 * buf, phase);
         if (!ok) break;
         tc_after();
