@@ -114,14 +114,14 @@ typedef struct opw_tree_attn opw_tree_attn_t; /* opaque handle (host memory only
  */
 opw_status_t opw_tree_mask(int32_t nodes, const int32_t *parents, uint64_t *mask, int32_t *depth);
 
-/* Scratch bytes of one handle (0 on invalid arguments). */
+/* Scratch bytes of one handle (0 on invalid arguments and for stages that opw_tree_attn_create does not take). */
 size_t opw_tree_attn_workspace_bytes(const opw_attn_stage_t *stage, int32_t max_nodes);
 
 /*
  * Binds tree attention to a stage (all of its layers).  max_nodes in 1..OPW_TREE_MAX_NODES; flags must be 0;
  * workspace: DEVICE, 256-byte aligned, caller-owned.  The calls of one handle use its workspace one after the
  * other: calls (or captured graphs) that may overlap on the device need a handle each.  The stage must outlive
- * the handle.
+ * the handle.  A stage whose tables hold more than INT32_MAX - 128 tokens per sequence is refused (OPW_ERR_UNSUPPORTED).
  */
 opw_status_t opw_tree_attn_create(opw_attn_stage_t *stage, int32_t max_nodes, uint32_t flags, void *workspace,
                                   size_t workspace_bytes, opw_tree_attn_t **out);

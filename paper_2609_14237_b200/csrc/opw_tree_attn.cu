@@ -21,6 +21,11 @@ struct Variant {              // a kernel, and how it cuts rows and keys
   bool mma, wide;
 };
 
+// Keys are numbered in 32 bits, and the last tile reaches past the last key: the table has to leave it that room.
+bool keys_fit(const opw_stage_view& v) {
+  return (int64_t)v.max_pages * opw_tree::kPage <= INT32_MAX - 2 * opw_tree::kMmaKeys;
+}
+
 constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the shared memory beside the tiles
 
 // Which kernel.  The tensor-core kernel reads a key tile once for 128 or 256 rows, a CTA at a time; the warp kernel once for 16 rows, a page
@@ -131,7 +136,8 @@ extern "C" opw_status_t opw_tree_mask(int32_t nodes, const int32_t* parents, uin
 
 extern "C" size_t opw_tree_attn_workspace_bytes(const opw_attn_stage_t* stage, int32_t max_nodes) {
   if (!stage || max_nodes < 1 || max_nodes > OPW_TREE_MAX_NODES) return 0;
-  return carve(opw_view_of(const_cast<opw_attn_stage_t*>(stage)), max_nodes).total;
+  const opw_stage_view v = opw_view_of(const_cast<opw_attn_stage_t*>(stage));
+  return keys_fit(v) ? carve(v, max_nodes).total : 0;
 }
 
 extern "C" opw_status_t opw_tree_attn_create(opw_attn_stage_t* stage, int32_t max_nodes, uint32_t flags, void* workspace,
@@ -139,6 +145,7 @@ extern "C" opw_status_t opw_tree_attn_create(opw_attn_stage_t* stage, int32_t ma
   if (!stage || !out || !workspace || flags != 0) return OPW_ERR_INVALID_ARG;
   if (max_nodes < 1 || max_nodes > OPW_TREE_MAX_NODES || (uintptr_t)workspace % 256) return OPW_ERR_INVALID_ARG;
   const opw_stage_view v = opw_view_of(stage);
+  if (!keys_fit(v)) return OPW_ERR_UNSUPPORTED;
   const TreeLayout lay = carve(v, max_nodes);
   if (workspace_bytes < lay.total) return OPW_ERR_CAPACITY;
   opw_device_guard guard(v.device);

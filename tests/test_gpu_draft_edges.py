@@ -428,3 +428,41 @@ def test_a_captured_step_equals_the_oracle_and_records_exactly_what_it_should():
         assert (host_bits(pool) == w_pool).all() and (new.cpu().numpy() == w_new).all()
         assert (tab.cpu().numpy() == w_tab).all() and (refs.cpu().numpy() == w_refs).all()
         assert cnt.item() == len(free) and (lst[:len(free)].cpu().numpy() == free).all() and (lst[len(free):] == -7).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,T", [(32, 8, 128, 5), (8, 2, 64, 40), (16, 2, 256, 3)])
+def test_contexts_at_the_end_of_32_bits(Hq, Hkv, D, T):
+    """A window at the far end of the longest table that is taken equals, bit for bit, the same window near the start; a table whose
+    last key tile could pass 32 bits is refused."""
+    rng = np.random.default_rng(2400 + D)
+    window, width, far = 100, 30, (1 << 27) - 9
+    cap = far * 16
+    assert cap <= (1 << 31) - 1 - 128 < (far + 1) * 16
+    near = width * 16 - 3 - T                                    # drafted rows end three slots before the table does
+    pool, tab, q, mask, pos = tree_inputs(rng, [near], [T], T, Hq, Hkv, D)
+    d_pool, i32 = dev(pool, True), lambda a: dev(np.asarray(a, np.int32))  # noqa: E731
+    junk = rand_bits(rng, (3, Hkv, D))
+    junk[:] = 0x7FC0
+    draft.append_rows(pool, Hkv, D, [0] * 3, [width * 16 - 3 + i for i in range(3)], tab, junk, junk)
+    d_pool.copy_(dev(pool, True))
+    res = []
+    for pages in (width, far):
+        shift = (pages - width) * 16
+        st = make_stage([d_pool], Hq, Hkv, D, 1, pages, window)
+        tree = B.TreeAttention(st, T)
+        table = torch.full((1, pages), -1, dtype=torch.int32, device="cuda")
+        table[0, pages - width:] = i32(tab[0])
+        out, lse = torch.empty(1, T, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(1, T, Hq, device="cuda")
+        tree.attention(0, dev(q, True), dev(mask), i32(pos.astype(np.int64) + shift), i32([near + shift]), i32([T]), table, out, lse)
+        assert st.poll_error() == B.OPW_OK
+        res.append((out, lse))
+        tree.close(), st.close()
+        del table
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
+    ref = draft.tree_attention(pool, Hq, Hkv, D, q, mask, pos, [near], [T], tab, window)
+    check_tree(*res[1], ref, 200)
+    st = make_stage([d_pool], Hq, Hkv, D, 1, far + 1, window)
+    assert B.opw_tree_attn_workspace_bytes(st.handle, T) == 0
+    h = B.ctypes.c_void_p()
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    assert B.lib().opw_tree_attn_create(st.handle, T, 0, ws.data_ptr(), 1 << 28, B.ctypes.byref(h)) == B.OPW_ERR_UNSUPPORTED and h.value is None
