@@ -14,6 +14,11 @@
  * after which the sequence is an ordinary one again (opw_decode_step may follow).
  * opw_rope_append also takes prompts into the cache: its rows are any tokens of any sequences.
  *
+ * These calls are no plan items and no part of opw_decode_step_host or of the attention module (opw_afd.h); a caller who wants
+ * one submission per step captures them into a CUDA graph of its own.  Layers with recurrent state (opw_linear_attn.h) have no
+ * form for drafted tokens: their state cannot be advanced along a tree nor taken back, so that in a hybrid stack these calls
+ * serve the attention layers only.
+ *
  * Conventions as in opw_attn.h: plain C, status codes, DEVICE pointers are caller-owned memory
  * on the stage's device, calls only enqueue on the stream and never synchronise.  The calls may
  * be made while another device is current.  Page ids and positions that are out of range are
@@ -135,7 +140,11 @@ opw_status_t opw_tree_attn_destroy(opw_tree_attn_t *tree); /* NULL is accepted *
  *     the drafted rows j = c + m, m < t, with bit m of tree_mask[b,i] set (its own bit is not implied),
  * on a window layer (window W) only those whose position is above p_i - W, where the position of context row j is j, that
  * of drafted row c + m is positions[b,m], and p_i = positions[b,i] (a position below c counts as c).  Cached
- * rows that a node does not see do not touch its result, whatever they hold (NaN and infinities included).
+ * rows that a node does not see do not touch its result, whatever they hold (NaN and infinities included).  An infinite value that it
+ * does see leaves an infinity or a NaN (NaN where its weight is below what fp32 holds).
+ * Scores, maxima, sums and the accumulated output are fp32.  The weights p_j = 2^(score - running maximum) are rounded to bf16 for the
+ * product with V -- not for the sum -- as the decode kernels do, which moves an output by at most 2^-8 sum_j p_j |V_j| / sum_j p_j;
+ * the output is rounded to bf16 once.
  * A node that sees nothing, nodes i >= t and inactive sequences (c < 0 or t <= 0) get out = 0, lse = -inf.
  * t > nodes, rows beyond the table and bad page ids are cut off or masked out and recorded as OPW_ERR_BAD_PAGE.
  *   nodes      : 1..max_nodes, the row stride of q, tree_mask, positions, out and lse

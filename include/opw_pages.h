@@ -28,7 +28,8 @@ extern "C" {
  *     if rest > 0, entry w names new_pages[f], whose count becomes 1, and the first `rest` slots of the parent's page w
  *         are copied into it, in every layer of the group,
  *     entries behind are -1.
- * The child row must hold no pages (opw_kv_release first).  Refused, skipped as a whole and recorded: a row outside
+ * The child row must hold no pages (opw_kv_release first) and new_pages[f], where rest > 0, must be free: a count of 0, named by no
+ * entry of the table.  Neither is checked.  Refused, skipped as a whole and recorded: a row outside
  * [0, num_rows), a dst row that is also a source or named twice, lens[f] < 0 or beyond the table, and, where rest > 0, a
  * parent without a page w, a new page outside the pool or named twice by forks that need one.
  *   layers     : HOST int32 [num_layers], the table group, without repetition

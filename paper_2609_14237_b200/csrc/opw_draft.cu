@@ -72,7 +72,10 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 // Measured at 32/8 heads of 128, rotary 128 half and 64 interleaved, us with a block and with a warp per row: 128 rows
 // 3.9 / 6.5 and 3.5 / 5.6, 512 rows 5.1 / 6.7 and 4.2 / 5.7, 1184 rows 12.0 / 11.1 and 9.1 / 9.0, 8192 rows 76.7 / 39.6 and 62.9 / 36.2
 // (5.1 and 5.6 TB/s of the bytes that have to move).  A block per row spends most of its life in the latencies before its first load; a warp per
-// row keeps more rows in flight.
+// row keeps more rows in flight.  Block and warp at other shapes, half layout: 5/1 heads of 64, 512 rows 4.0 / 3.8,
+// 1184 rows 7.2 / 3.8, 8192 rows 40.7 / 9.5; 64/8 of 128, 512 rows 5.8 / 9.3, 1184 rows 14.0 / 15.2, 2368 rows 28.1 / 22.6; 16/2 of 256, rotary
+// 64, 1184 rows 10.1 / 10.7, 2368 rows 25.3 / 20.6.  kVec 2 has the block form only: 8192 rows at rotary 34 take 117 us.  The half layout, with two
+// words and eight pairs a thread, spills 17 words (21 loads) in the warp form and 6 in the block form; the interleaved one none.
 template <int kVec, int kGroup>
 __global__ void __launch_bounds__(kRopeThreads, 4) rope_append_kernel(const RopeParams p) {
   constexpr int kRows = kRopeThreads / kGroup, kWarps = kRopeThreads / 32;

@@ -33,8 +33,9 @@ constexpr int kForkThreads = 256;
 
 // grid (n, blocks per fork, layers of this launch [+ 1 in front for the bookkeeping]).  The copy moves, of each of the page's K and V tiles,
 // the contiguous `rest` rows that hold a token -- half a page on average -- as 16-byte words, a warp a tile.  (With the tile of each word
-// found by a division the kernel was bound by instructions: 256 forks x 8 layers 22.1 us, now 18.2, 6.9 TB/s of what has to move --
-// children of one parent read its page from L2.)  Every block decides for itself whether its fork is refused: a scan of the n rows and
+// found by a division the kernel was bound by instructions: 256 forks x 8 layers 22.1 us, now 18.2.  Of that the
+// 63 MB written and the 8 MB read, the page of a parent with many children once, would take a copy 10.8: most of the rest is each of the
+// 4608 blocks finding out what it has to copy.)  Every block decides for itself whether its fork is refused: a scan of the n rows and
 // page ids, which all blocks share in L2, against a second launch that a list of accepted forks would need.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constant__ ForkParams p) {
   pdl_wait();
@@ -137,7 +138,8 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const int32_t*
 
 // One cluster: each block counts the free pages of its contiguous share, the counts meet through shared memory, and the ids are
 // written behind those of the blocks before.  Ascending by construction, no scratch memory, one launch.  A thread takes four pages in
-// a row; of up to eight such rounds it remembers the finding (256k pages in all), beyond that it reads the counts again.  1000 pages 3.3 us, 40000 5.5, 600000 38 (most of the small ones: launch and two cluster barriers).
+// a row; of up to eight such rounds it remembers the finding (256k pages in all), beyond that it reads the counts again.  1000 pages 3.3 us, 40000 4.6, 100000 6.4, 300000 13,
+// 1000000 44 (most of the small ones: launch and two cluster barriers; the large ones: eight SMs).
 constexpr int kListBlocks = 8;
 constexpr int kListThreads = 1024;
 constexpr int kListRound = 4 * kListThreads, kListKept = 8;

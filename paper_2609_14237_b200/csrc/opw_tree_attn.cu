@@ -34,6 +34,11 @@ constexpr int kMmaMaxBatch = 2048;   // what the prefix sums may take of the sha
 //   up to 16 rows, fewer heads than twice the SMs (1 sequence of 1000 keys)  warp 14.7, tensor core 12.5 (now 11.5): a partial per CTA, not per warp
 //   17 to 32 rows (64 sequences, trees of 8)   warp, with two row tiles a warp, 139; tensor core 130
 //   beyond, the warp kernel would read the cache once per 16 rows (16 x 32k keys, 256 rows: 3133; tensor core 560)
+// Both sides at other shapes (warp, tensor core; 64 sequences of 1k to 4k keys unless said): 64/8 heads of 128, 8 and 16 rows 114 and 126, 32 rows
+// 183 and 129.  32/8 of 64, 8 and 16 rows 62 and 105, 32 rows 98 and 106; 40 sequences, 16 rows 43 and 69.  One sequence of 1000 keys, a
+// chain of 4: 64/8 of 128 13.6 and 12.2, 16/1 of 128 11.8 and 11.0, 8/2 of 64 11.0 and 8.9.  16/1 of 128, 16 and 32 rows 33 and 27, 34 and 28.
+// Known misses, where the rule of few heads takes the tensor cores and the warp kernel is faster: head_dim 64, 32 sequences of 8 kv heads 38 and
+// 57; one kv head of 128, 16 sequences of 16 rows 15 and 22.
 // The wide instance (two query tiles in shared memory) from 129 rows on; for up to 128 rows the narrow one with its deeper ring (130 against
 // 138 us for the trees of 8).  At head_dim 256 two slots' accumulators alone would take all 512 columns of TMEM; those heads go through the
 // warp kernel at every number of rows.
@@ -258,7 +263,9 @@ extern "C" opw_status_t opw_tree_attention(opw_tree_attn_t* tree, int32_t layer,
     *v.launches += 1;
     // Partials per row block, about: workers / blocks.  Above twelve they are dealt out to groups of threads: one chain of 4 at 1000
     // keys 12.5 us without, 12.2 with, at 8000 keys 21 and 19; where blocks are many it only adds blocks (64 trees of 8: 129 us
-    // without, 208 with).
+    // without, 208 with).  Without and with, chains of 4 at other shapes: 8/2 heads of 64, 8000 keys 28 and 12, 4 sequences 19 and 15.6;
+    // 16/1 of 128 64 and 14, 4 sequences 35 and 15, 16 of them (not dealt out) 31 and 34; 16/2 of 256 64 and 18, 4 sequences 55 and 32, 16 (dealt out,
+    // a miss) 66 and 75.
     const int64_t blocks = (int64_t)batch * v.Hkv * c.max_blocks;
     const bool deal = k.workers > 12 * blocks;
     e = v.D == 64 ? launch_combine<64>(v, c, blocks, deal, stream)

@@ -190,7 +190,8 @@ __device__ __forceinline__ float bf16_at(uint32_t addr) {
 // A unit is one page, K and V of a head in one bulk copy; a row block is 16 rows, the accumulators of one mma.sync tile in registers.
 // At these sizes the products are next to nothing (16 rows: 8 flops a byte) and the copy is what bounds it; a warp that
 // waits for nobody else keeps the memory busy with two pages in flight each.  64 sequences of 1k to 4k keys, a tree of 2: 669 MB in 112 us,
-// 6.0 TB/s, 91 % of what a copy reaches.
+// 6.0 TB/s, 91 % of what a copy reaches.  At head_dim 256 the accumulators take 128 registers more: 255 and a spill of 21 words stored and 17 loaded;
+// a tree of 2 still runs at 5.0 TB/s, but a larger one reads its pages once per 16 rows (16 x 16k keys, 512 rows: 2385 us, floor 169).
 template <int D>
 struct WarpTree {
   static constexpr int kTile = 2 * kPage * D * 2;

@@ -17,11 +17,13 @@
 // beyond the tensor's end, which TMA fills with zeros: no traffic, and no stale shared memory in the product.
 //
 // The running maximum is only raised when a row's new maximum exceeds it by 2^8: P stays below 2^8, exact in the same
-// relative sense, and O is rescaled a few times per row instead of once per tile.
+// relative sense, and O is rescaled only where a row's scores climb: where they stay within 2^8 of those of its first tile, as with the normal
+// inputs of the timings here, not at all.
 //
-// Measured, 32/8 heads of 128.  Narrow, 32 sequences with a window of 4096 and trees of 26: 111 us, 553 MB, 5.0 TB/s; bound by the bytes in
-// flight (the tensor pipe is 35 % busy).  Wide, 16 sequences of 32k keys and trees of 64 (550 GFLOP on 2.2 GB): 565 us, 0.97 PFLOP/s, 60 % of
-// what a library matrix product reaches.  There the chain bounds it: with N = 64 keys an MMA takes 48 cycles (64 with N = 128, which shared
+// Measured, 32/8 heads of 128, in a replayed graph and, in brackets, called in a loop (where the clock is lower: the power limit).  Narrow, 32
+// sequences with a window of 4096 and trees of 26: 105 to 114 us (117 to 125), 553 MB, 5.0 TB/s (4.6); bound by the bytes in
+// flight (the tensor pipe is 35 % busy).  Wide, 16 sequences of 32k keys and trees of 64 (550 GFLOP on 2.2 GB): 537 to 576 us (620 to 640), 0.96 to
+// 1.02 PFLOP/s (0.89), about 60 % of what a library matrix product reaches.  There the chain bounds it: with N = 64 keys an MMA takes 48 cycles (64 with N = 128, which shared
 // memory sets), so 128 keys of both slots want 2400 cycles of the tensor core, and the issue waits for the softmax on top; with the
 // softmax skipped the same loop takes 450 us.  Tried and slower: tiles of 128 keys with one buffer (559 against 547), an issuer per
 // buffer (565 against 536), no turns at the exponentials (584), a third of the exponentials as a polynomial (645).
@@ -266,8 +268,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     return mbar_try_wait(a, parity) || mbar_wait_or_dead(a, parity, &dead_s, p.status);
   };
 
-  // Registers: 384 threads are launched with 168 each (64512); a softmax thread holds a row of 128 scores and wants
-  // more, the third warpgroup needs little: 256 x 200 + 128 x 104 = 64512.
+  // Registers: 384 threads are launched with 168 each (64512); a softmax thread holds a row's 64 scores of a tile
+  // beside what it keeps and wants more, the third warpgroup needs little: 256 x 200 + 128 x 104 = 64512.
   if (warp >= 8) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
   if (warp == 8 || warp == 11) {
