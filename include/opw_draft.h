@@ -141,7 +141,7 @@ opw_status_t opw_tree_attn_destroy(opw_tree_attn_t *tree); /* NULL is accepted *
  * on a window layer (window W) only those whose position is above p_i - W, where the position of context row j is j, that
  * of drafted row c + m is positions[b,m], and p_i = positions[b,i] (a position below c counts as c).  Cached
  * rows that a node does not see do not touch its result, whatever they hold (NaN and infinities included).  An infinite value that it
- * does see leaves an infinity or a NaN (NaN where its weight is below what fp32 holds).
+ * does see leaves an infinity or a NaN (either, where its weight is below what fp32 holds).
  * Scores, maxima, sums and the accumulated output are fp32.  The weights p_j = 2^(score - running maximum) are rounded to bf16 for the
  * product with V -- not for the sum -- as the decode kernels do, which moves an output by at most 2^-8 sum_j p_j |V_j| / sum_j p_j;
  * the output is rounded to bf16 once.
