@@ -8,7 +8,8 @@
  *     opw_rope_append      rotate the nodes' queries and keys, append keys and values to the
  *                          cache, node i of sequence b in slot ctx[b] + i
  *     opw_tree_attention   every node against the context and the nodes its mask names
- * and, once the step's logits have decided which path is accepted,
+ * (opw_norm_rope_append in the place of the first for models that normalise queries and keys), and, once the step's logits are there,
+ *     opw_tree_verify      which path the target's probabilities accept, and the token that follows
  *     opw_kv_commit        move the accepted nodes' cached rows together, in slots ctx[b],
  *                          ctx[b] + 1, ..., of all layers that share a page table
  * after which the sequence is an ordinary one again (opw_decode_step may follow).
@@ -103,6 +104,23 @@ opw_status_t opw_rope_append(opw_attn_stage_t *stage, int32_t layer, int32_t row
                              const int32_t *positions, int32_t num_rows, const int32_t *page_table, void *q_out,
                              void *cuda_stream);
 
+/*
+ * opw_rope_append for models that normalise queries and keys head by head: every head x of q[r] and k[r] becomes
+ *     x * weight / sqrt(sum_d x_d^2 / D + eps)
+ * over all D elements, then is rotated (its first rotary_dim elements), stored and appended as above; values are appended as they are.
+ * Sums, weights and rotation are fp32 (a head whose squares pass fp32 becomes 0), rounded to bf16 once.
+ *   q_weight, k_weight : DEVICE float [D], or [Hq, D] and [Hkv, D] with weights_per_head = 1 (else 0); 16-byte aligned; either may be
+ *                NULL (ones).  A model that stores them as an offset from 1, or in 16 bits, has them laid out once
+ *   eps        : > 0
+ * Everything else, and what is refused, as in opw_rope_append.
+ */
+opw_status_t opw_norm_rope_append(opw_attn_stage_t *stage, int32_t layer, int32_t rows, int32_t rotary_dim, int32_t layout,
+                                  const double *table, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                  const void *v, int64_t v_stride, const float *q_weight, const float *k_weight,
+                                  int32_t weights_per_head, float eps, const int32_t *seq, const int32_t *slots,
+                                  const int32_t *positions, int32_t num_rows, const int32_t *page_table, void *q_out,
+                                  void *cuda_stream);
+
 /* ------------------------------------------------------------------------------------------
  * Attention of a tree of drafted tokens
  * ------------------------------------------------------------------------------------------ */
@@ -161,6 +179,51 @@ opw_status_t opw_tree_attention(opw_tree_attn_t *tree, int32_t layer, int32_t ba
                                 const uint64_t *tree_mask, const int32_t *positions, const int32_t *ctx_lens,
                                 const int32_t *tree_lens, const int32_t *page_table, void *out, float *lse,
                                 void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Verification of the drafted tokens
+ * ------------------------------------------------------------------------------------------ */
+
+#define OPW_PROBS_F32 0
+#define OPW_PROBS_BF16 1
+
+/* How the children of a node were drafted from the drafter's distribution there:
+ *   AGAIN     each drawn from it, independently (a token may come twice)
+ *   DISTINCT  one after the other without replacement: the next from what is left, rescaled
+ *   CERTAIN   chosen by a rule (the likeliest, a table): no distribution, draft == NULL */
+#define OPW_DRAW_AGAIN 0
+#define OPW_DRAW_DISTINCT 1
+#define OPW_DRAW_CERTAIN 2
+
+/*
+ * Which of a tree's drafted tokens the target accepts, and the token that follows them, so that the tokens are distributed as if each
+ * had been drawn from the target.  Node 0 of sequence b is the last token that is decided already (its key and value are cached with the
+ * step's); node i > 0 carries tokens[b,i] and follows node parents[b,i] < i.  target[b,i,:] are the target's probabilities after node i,
+ * draft[b,i,:] those that node i's children were drafted from.  From node 0 on, with r_0 = target, q_0 = draft of the current
+ * node, its children x = tokens[b,i] in ascending order of i:
+ *     accepted if uniforms[b,i] * q_j(x) < r_j(x): the walk goes on from that child; else
+ *     r_{j+1} = max(r_j - q_j, 0) / sum(max(r_j - q_j, 0))    (r_j where the sum is 0)
+ *     q_{j+1} = q_j (AGAIN), or q_j without x, divided by its sum (DISTINCT); CERTAIN: q_j is 1 at x and 0 elsewhere
+ * until no child is accepted.  Then next_tokens[b] is the smallest token v with sum_{w <= v} r(w) > uniforms[b,0] * sum_w r(w), of the
+ * r that is left (the last token with r > 0 where rounding leaves none; -1 if all are 0).  All of this in 64 bits, from the
+ * probabilities as they are; negative ones and NaN count as 0.  Neither r_0 nor q_0 is rescaled to a sum of 1.
+ *     path[b, 0 .. path_lens[b])   the accepted nodes, ascending, node 0 first: what opw_kv_commit takes; -1 behind
+ * Sequences with tree_lens[b] <= 0 are inactive: path_lens 0, next_tokens -1.  tree_lens beyond nodes is cut and recorded
+ * (OPW_ERR_BAD_PAGE); a node whose token is outside [0, vocab) or whose parent is not an earlier node is passed over, and recorded.
+ *   dtype      : OPW_PROBS_F32 or OPW_PROBS_BF16, of target and draft
+ *   target     : DEVICE [batch * nodes] rows of vocab probabilities, target_stride >= vocab elements apart, aligned to an element;
+ *   draft        likewise, NULL for CERTAIN only.  Rows that the walk does not need are not read.  16-byte aligned rows, or rows of
+ *                target and draft that are misaligned alike, are read fastest
+ *   tokens, parents : DEVICE int32 [batch, nodes] (entry 0 of either is not read);  tree_lens : DEVICE int32 [batch]
+ *   uniforms   : DEVICE float [batch, nodes], independent and uniform in [0, 1)
+ *   path       : DEVICE int32 [batch, nodes];  path_lens, next_tokens : DEVICE int32 [batch]; must not overlap each other or the inputs
+ * 1 <= nodes <= OPW_TREE_MAX_NODES; batch <= 65535 and vocab <= 2^24 (OPW_ERR_CAPACITY).  The stage gives the device and the status word;
+ * no cache is touched.  The result does not vary from run to run.
+ */
+opw_status_t opw_tree_verify(opw_attn_stage_t *stage, int32_t batch, int32_t nodes, int32_t vocab, int32_t dtype, int32_t draw,
+                             const void *target, int64_t target_stride, const void *draft, int64_t draft_stride,
+                             const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens, const float *uniforms,
+                             int32_t *path, int32_t *path_lens, int32_t *next_tokens, void *cuda_stream);
 
 /* ------------------------------------------------------------------------------------------
  * The accepted path

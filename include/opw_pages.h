@@ -60,6 +60,41 @@ opw_status_t opw_kv_release(opw_attn_stage_t *stage, int32_t n, const int32_t *r
 opw_status_t opw_kv_free_pages(opw_attn_stage_t *stage, const int32_t *refcounts, int64_t num_pages, int32_t *free_list,
                                int64_t max_list, int32_t *count, void *cuda_stream);
 
+/*
+ * Pages and places for the new tokens of n ragged requests, prompts and single tokens alike: request f adds new_tokens[f] = m tokens
+ * behind the old_lens[f] = c that table row rows[f] holds.  What follows is all that opw_rope_append and opw_norm_rope_append need of
+ * them when the requests' tokens lie one behind the other.
+ *     row_starts[f] = sum of max(new_tokens[i], 0) over i < f, and row_starts[n] their total: the requests' rows
+ *     entries p of the request's table row, c / page_size <= p < ceil((c + m) / page_size), that name no page (< 0) get one:
+ *         the next of free_list, whose count becomes 1.  Pages are dealt in the order of the requests, and within one in that of
+ *         its entries, from free_list[*free_begin] on; free_list and *free_count as opw_kv_free_pages leaves them
+ *     new_lens[f] = c + m, and for the request's rows r: seq[r] = rows[f], slots[r] = c + (r - row_starts[f])
+ * A request gets all that it needs or nothing: with nothing, new_lens[f] = c, its rows get seq[r] = slots[r] = -1 (padding for the calls
+ * that follow), and its entries stay.  A request gets nothing
+ *   - if it lacks pages, and they and those that the requests before it lack are more than the list has left: not an error;
+ *   - if rows[f] < 0: not an error, the request is idle;
+ *   - and is recorded, if rows[f] >= num_rows or is named by another request too, a length is negative, c + m is beyond the table, the
+ *     page that holds its last c % page_size tokens is missing, one of the entries that its tokens go to names a page outside
+ *     [0, num_pages) or one whose count is not 1 (its tokens would show up in other sequences), or its rows end beyond max_rows.
+ * Requests that are refused or idle take nothing from the list; those for whom it was too short come after all that were served
+ * from it.  An id of the list that is out of range or not free (a list that is out of date) is not dealt: its entry stays as it
+ * is, and it is recorded.
+ *   rows, old_lens, new_tokens : DEVICE int32 [n]
+ *   page_table : DEVICE int32 [num_rows, max_pages_per_seq];  refcounts : DEVICE int32 [num_pages]; both changed in place
+ *   free_list  : DEVICE int32 [max_list];  free_count : DEVICE int32 [1]: the list's length is min(*free_count, max_list)
+ *   free_begin : DEVICE int32 [1] or NULL (0; so is a negative one): where dealing begins
+ *   free_end   : DEVICE int32 [1] or NULL: where it ended; may be free_begin, which makes that a cursor through one list
+ *   row_starts : DEVICE int32 [n + 1] or NULL; starts beyond max_rows count as max_rows
+ *   new_lens   : DEVICE int32 [n] or NULL
+ *   seq, slots : DEVICE int32 [max_rows]; rows behind the last request's get -1, so that a captured step may have more rows than
+ *                tokens.  max_rows = -1: NULL both, no rows are placed and none is too many
+ * What is written must not overlap what is read, nor each other.  n <= 8192 and num_rows <= 262144 (OPW_ERR_CAPACITY).
+ */
+opw_status_t opw_kv_extend(opw_attn_stage_t *stage, int32_t n, const int32_t *rows, const int32_t *old_lens, const int32_t *new_tokens,
+                           int32_t num_rows, int32_t *page_table, int32_t *refcounts, int64_t num_pages, const int32_t *free_list,
+                           int64_t max_list, const int32_t *free_count, const int32_t *free_begin, int32_t *free_end,
+                           int32_t *row_starts, int32_t *new_lens, int32_t max_rows, int32_t *seq, int32_t *slots, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,12 +18,13 @@ LIB_PATH = os.path.join(_HERE, "libopw_attn.so")
 SOURCES = [os.path.join(_HERE, "csrc", "opw_attn.cu"), os.path.join(_HERE, "csrc", "opw_noalloc.cu"),
            os.path.join(_HERE, "csrc", "opw_linear_attn.cu"), os.path.join(_HERE, "csrc", "opw_afd.cu"),
            os.path.join(_HERE, "csrc", "opw_tree_attn.cu"), os.path.join(_HERE, "csrc", "opw_draft.cu"),
-           os.path.join(_HERE, "csrc", "opw_pages.cu")]
+           os.path.join(_HERE, "csrc", "opw_pages.cu"), os.path.join(_HERE, "csrc", "opw_norm_rope.cu"),
+           os.path.join(_HERE, "csrc", "opw_verify.cu")]
 HEADERS = [os.path.join(_HERE, "csrc", "opw_kernels.cuh"), os.path.join(_HERE, "csrc", "opw_afd_gemm.cuh"), os.path.join(_ROOT, "include", "opw_attn.h"),
            os.path.join(_ROOT, "include", "opw_linear_attn.h"), os.path.join(_ROOT, "include", "opw_afd.h"),
            os.path.join(_ROOT, "include", "opw_draft.h"), os.path.join(_ROOT, "include", "opw_pages.h"),
            os.path.join(_HERE, "csrc", "opw_stage.h"), os.path.join(_HERE, "csrc", "opw_tree_kernels.cuh"),
-           os.path.join(_HERE, "csrc", "opw_tree_mma.cuh")]
+           os.path.join(_HERE, "csrc", "opw_tree_mma.cuh"), os.path.join(_HERE, "csrc", "opw_words.cuh")]
 
 OPW_FLAG_NO_PDL = 1
 OPW_FLAG_COPY_STREAMS = 2
@@ -42,6 +43,7 @@ EXPORTS = [
     "opw_afd_module_launch_count", "opw_afd_module_set_trace", "opw_hbm_read_probe",
     "opw_rope_table", "opw_rope_append", "opw_tree_mask", "opw_tree_attn_workspace_bytes", "opw_tree_attn_create",
     "opw_tree_attn_destroy", "opw_tree_attention", "opw_kv_commit", "opw_kv_fork", "opw_kv_release", "opw_kv_free_pages",
+    "opw_norm_rope_append", "opw_tree_verify", "opw_kv_extend",
 ]
 
 
@@ -114,6 +116,8 @@ class RopeConfig(ctypes.Structure):
 OPW_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 OPW_ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
 OPW_TREE_MAX_NODES = 64
+OPW_PROBS_F32, OPW_PROBS_BF16 = 0, 1
+OPW_DRAW_AGAIN, OPW_DRAW_DISTINCT, OPW_DRAW_CERTAIN = 0, 1, 2
 OPW_OP_ATTENTION, OPW_OP_LINEAR, OPW_OP_AFD_MODULE = 0, 1, 2
 OPW_PLAN_GRAPH, OPW_PLAN_ADVANCE, OPW_PLAN_OVERLAP = 1, 2, 4
 OPW_AFD_LIBRARY_GEMM, OPW_AFD_NO_PDL, OPW_AFD_NO_CLUSTER = 1, 2, 4
@@ -242,6 +246,13 @@ def lib() -> ctypes.CDLL:
     L.opw_kv_release.argtypes = [vp, i32, vp, vp, i32, vp, vp, i64, vp]
     L.opw_kv_free_pages.restype = ctypes.c_int
     L.opw_kv_free_pages.argtypes = [vp, vp, i64, vp, i64, vp, vp]
+    L.opw_norm_rope_append.restype = ctypes.c_int
+    L.opw_norm_rope_append.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, i32, ctypes.c_float, vp, vp, vp, i32,
+                                       vp, vp, vp]
+    L.opw_tree_verify.restype = ctypes.c_int
+    L.opw_tree_verify.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.opw_kv_extend.restype = ctypes.c_int
+    L.opw_kv_extend.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     L.opw_attn_stage_launch_count.restype = i64
     L.opw_attn_stage_launch_count.argtypes = [vp]
     L.opw_attn_stage_destroy.restype = ctypes.c_int
@@ -586,6 +597,30 @@ def opw_kv_free_pages(stage: int, refcounts: int, num_pages: int, free_list: Opt
     _check(lib().opw_kv_free_pages(stage, refcounts, num_pages, free_list, max_list, count, stream), "opw_kv_free_pages")
 
 
+def opw_norm_rope_append(stage: int, layer: int, rows: int, rotary_dim: int, layout: int, table: int, q: Optional[int], q_stride: int,
+                         k: int, k_stride: int, v: int, v_stride: int, q_weight: Optional[int], k_weight: Optional[int],
+                         weights_per_head: int, eps: float, seq: int, slots: int, positions: int, num_rows: int, page_table: int,
+                         q_out: Optional[int], stream: Optional[int] = None) -> None:
+    _check(lib().opw_norm_rope_append(stage, layer, rows, rotary_dim, layout, table, q, q_stride, k, k_stride, v, v_stride, q_weight,
+                                      k_weight, weights_per_head, eps, seq, slots, positions, num_rows, page_table, q_out, stream),
+           "opw_norm_rope_append")
+
+
+def opw_tree_verify(stage: int, batch: int, nodes: int, vocab: int, dtype: int, draw: int, target: int, target_stride: int,
+                    draft: Optional[int], draft_stride: int, tokens: int, parents: int, tree_lens: int, uniforms: int, path: int,
+                    path_lens: int, next_tokens: int, stream: Optional[int] = None) -> None:
+    _check(lib().opw_tree_verify(stage, batch, nodes, vocab, dtype, draw, target, target_stride, draft, draft_stride, tokens, parents,
+                                 tree_lens, uniforms, path, path_lens, next_tokens, stream), "opw_tree_verify")
+
+
+def opw_kv_extend(stage: int, n: int, rows: int, old_lens: int, new_tokens: int, num_rows: int, page_table: int, refcounts: int,
+                  num_pages: int, free_list: int, max_list: int, free_count: int, free_begin: Optional[int] = None,
+                  free_end: Optional[int] = None, row_starts: Optional[int] = None, new_lens: Optional[int] = None, max_rows: int = -1,
+                  seq: Optional[int] = None, slots: Optional[int] = None, stream: Optional[int] = None) -> None:
+    _check(lib().opw_kv_extend(stage, n, rows, old_lens, new_tokens, num_rows, page_table, refcounts, num_pages, free_list, max_list,
+                               free_count, free_begin, free_end, row_starts, new_lens, max_rows, seq, slots, stream), "opw_kv_extend")
+
+
 def _need(where: str, index: int, dtype, count: int, *tensors) -> None:
     """The kernels see addresses only: a tensor of another type, device, size or memory order would be read wrongly.
     count: elements each must have (-1: any)."""
@@ -644,7 +679,7 @@ class Stage:
         self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
         self.max_pages_per_seq, self.layer_num_pages = max_pages_per_seq, [int(n) for n in layer_num_pages]
         # what the short calls look up every time
-        self.index, self._i32, self._bf16, self._lib = dev.index or 0, torch.int32, torch.bfloat16, lib()
+        self.index, self._i32, self._bf16, self._f32, self._lib = dev.index or 0, torch.int32, torch.bfloat16, torch.float32, lib()
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self.handle = opw_attn_stage_create(cfg)
 
@@ -702,10 +737,9 @@ class Stage:
             _need(where, self.index, self._i32, -1, page_table)
         return shape[0]
 
-    def rope_append(self, layer, rope, q, k, v, seq, slots, positions, page_table, q_out):
-        """Rotate q into q_out, append rotated k and v to the cache; q, k, v: [rows, heads, head_dim], rows may be strided
-        (views into one projection).  q = q_out = None: keys and values only."""
-        where, D, rows, dev, bf16 = "rope_append", self.head_dim, seq.shape[0], self.index, self._bf16
+    def _append_args(self, where, rope, q, k, v, seq, slots, positions, page_table, q_out):
+        """The checked addresses and strides of the rotary appends."""
+        D, rows, dev, bf16 = self.head_dim, seq.shape[0], self.index, self._bf16
         _need(where, dev, self._i32, rows, seq, slots, positions)
         table_rows = self._table_rows(where, page_table, 1)
         Hq, Hkv = self.num_q_heads, self.num_kv_heads
@@ -726,11 +760,71 @@ class Stage:
             raise ValueError(f"{where}: the rotary table is on {rope.table.device}")
         # (the stride of a single row says nothing, as that of a single head)
         k_stride, v_stride = (k_st[0], v_st[0]) if rows != 1 else (Hkv * D, Hkv * D)
-        rc = self._lib.opw_rope_append(self.handle, layer, rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(), q_ptr, q_stride,
-                                       k.data_ptr(), k_stride, v.data_ptr(), v_stride, seq.data_ptr(), slots.data_ptr(),
-                                       positions.data_ptr(), table_rows, page_table.data_ptr(), out_ptr, self._raw_stream(dev))
+        return ((rows, rope.rotary_dim, rope.layout, rope.table.data_ptr(), q_ptr, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride),
+                (seq.data_ptr(), slots.data_ptr(), positions.data_ptr(), table_rows, page_table.data_ptr(), out_ptr, self._raw_stream(dev)))
+
+    def rope_append(self, layer, rope, q, k, v, seq, slots, positions, page_table, q_out):
+        """Rotate q into q_out, append rotated k and v to the cache; q, k, v: [rows, heads, head_dim], rows may be strided
+        (views into one projection).  q = q_out = None: keys and values only."""
+        a, c = self._append_args("rope_append", rope, q, k, v, seq, slots, positions, page_table, q_out)
+        rc = self._lib.opw_rope_append(self.handle, layer, *a, *c)
         if rc:
             _check(rc, "opw_rope_append")
+
+    def norm_rope_append(self, layer, rope, q, k, v, q_weight, k_weight, seq, slots, positions, page_table, q_out, eps=1e-6):
+        """rope_append of queries and keys that are normalised head by head first.  q_weight, k_weight: fp32 [head_dim], or both
+        [heads, head_dim] with a row for each head; either may be None (ones)."""
+        where, D, dev = "norm_rope_append", self.head_dim, self.index
+        a, c = self._append_args(where, rope, q, k, v, seq, slots, positions, page_table, q_out)
+        per_head, ptrs = None, []
+        for w, heads in ((q_weight, self.num_q_heads), (k_weight, self.num_kv_heads)):
+            if w is None:
+                ptrs.append(None)
+                continue
+            rows = len(w.shape) == 2
+            if w.shape != ((heads, D) if rows else (D,)) or per_head not in (None, rows):
+                raise ValueError(f"{where}: weights must both be [{D}], or [{self.num_q_heads}, {D}] and [{self.num_kv_heads}, {D}]")
+            _need(where, dev, self._f32, -1, w)
+            per_head = rows
+            ptrs.append(w.data_ptr())
+        rc = self._lib.opw_norm_rope_append(self.handle, layer, *a, ptrs[0], ptrs[1], 1 if per_head else 0, eps, *c)
+        if rc:
+            _check(rc, "opw_norm_rope_append")
+
+    def tree_verify(self, target, draft, tokens, parents, tree_lens, uniforms, path, path_lens, next_tokens, distinct=False):
+        """Accept drafted tokens by the target's probabilities and draw the token that follows.  target, draft: fp32 or bf16
+        [batch, nodes, vocab], the rows of a sequence's nodes at one stride throughout (a view into padded rows is fine); draft None:
+        the tokens were chosen by a rule.  distinct: siblings were drawn without replacement."""
+        where, dev, shape = "tree_verify", self.index, target.shape
+        if len(shape) != 3 or (draft is not None and draft.shape != shape):
+            raise ValueError(f"{where}: target and draft must be [batch, nodes, vocab]")
+        batch, nodes, vocab = shape
+        kind = target.dtype
+        if kind is not self._f32 and kind is not self._bf16:
+            raise ValueError(f"{where}: probabilities must be float32 or bfloat16, got {kind}")
+        ptrs = []
+        for x in (target, draft):
+            if x is None:
+                ptrs += [None, 0]
+                continue
+            st = x.stride()
+            # (the stride of a single node, sequence or token says nothing)
+            step = st[1] if nodes != 1 else st[0] if batch != 1 else vocab
+            if (x.dtype is not kind or x.get_device() != dev or (st[2] != 1 and vocab != 1) or step < vocab
+                    or (batch != 1 and st[0] != nodes * step)):
+                raise ValueError(f"{where}: target and draft must be of one type on {self.device}, with rows of contiguous tokens, all at one stride")
+            ptrs += [x.data_ptr(), step]
+        if draft is None and distinct:
+            raise ValueError(f"{where}: distinct needs the drafter's probabilities")
+        _need(where, dev, self._i32, batch * nodes, tokens, parents, path)
+        _need(where, dev, self._f32, batch * nodes, uniforms)
+        _need(where, dev, self._i32, batch, tree_lens, path_lens, next_tokens)
+        draw = OPW_DRAW_CERTAIN if draft is None else OPW_DRAW_DISTINCT if distinct else OPW_DRAW_AGAIN
+        rc = self._lib.opw_tree_verify(self.handle, batch, nodes, vocab, OPW_PROBS_F32 if kind is self._f32 else OPW_PROBS_BF16, draw, *ptrs,
+                                       tokens.data_ptr(), parents.data_ptr(), tree_lens.data_ptr(), uniforms.data_ptr(), path.data_ptr(),
+                                       path_lens.data_ptr(), next_tokens.data_ptr(), self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_tree_verify")
 
     def kv_commit(self, layers, accepted, accepted_lens, ctx_lens, page_table, new_lens=None):
         """Move the rows of the accepted nodes together behind each sequence's context, in all of `layers`.  accepted: int32
@@ -787,6 +881,30 @@ class Stage:
                                          count.data_ptr(), self._raw_stream(dev))
         if rc:
             _check(rc, "opw_kv_free_pages")
+
+    def kv_extend(self, rows, old_lens, new_tokens, page_table, refcounts, free_list, free_count, *, row_starts=None, new_lens=None,
+                  seq=None, slots=None, free_begin=None, free_end=None):
+        """Deal pages of free_list to the new tokens of ragged requests and say where their rows go.  rows, old_lens, new_tokens,
+        new_lens: int32 [n]; row_starts: int32 [n + 1]; seq, slots: int32 [at most so many rows], -1 where there is none."""
+        where, n, dev = "kv_extend", rows.shape[0], self.index
+        _need(where, dev, self._i32, n, rows, old_lens, new_tokens)
+        _need(where, dev, self._i32, -1, refcounts, free_list)
+        _need(where, dev, self._i32, 1, free_count)
+        table_rows = self._table_rows(where, page_table, 1)
+        if (seq is None) != (slots is None):
+            raise ValueError(f"{where}: seq and slots go together")
+        max_rows = -1 if seq is None else seq.shape[0]
+        ptrs = []
+        for t, count in ((free_begin, 1), (free_end, 1), (row_starts, n + 1), (new_lens, n), (seq, max_rows), (slots, max_rows)):
+            if t is not None:
+                _need(where, dev, self._i32, count, t)
+            ptrs.append(None if t is None else t.data_ptr())
+        rc = self._lib.opw_kv_extend(self.handle, n, rows.data_ptr(), old_lens.data_ptr(), new_tokens.data_ptr(), table_rows,
+                                     page_table.data_ptr(), refcounts.data_ptr(), refcounts.numel(), free_list.data_ptr(),
+                                     free_list.numel(), free_count.data_ptr(), ptrs[0], ptrs[1], ptrs[2], ptrs[3], max_rows, ptrs[4],
+                                     ptrs[5], self._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_kv_extend")
 
     def packed_host_buffers(self, batch):
         """One pinned host buffer holding q, k_new, v_new, positions at the packed offsets;

@@ -7,6 +7,7 @@
 
 #include "opw_draft.h"
 #include "opw_stage.h"
+#include "opw_words.cuh"
 
 namespace opw_draft {
 
@@ -14,8 +15,10 @@ constexpr int kPage = 16;
 constexpr uint32_t kErrBadPage = 1u;      // bit of the stage's status word
 constexpr int kLayersPerLaunch = 64;
 
-__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+using opw_words::pack8;
+using opw_words::pdl_launch_dependents;
+using opw_words::pdl_wait;
+using opw_words::unpack8;
 
 // ---------------------------------------------------------------------------------
 // rotary encoding and append
@@ -44,24 +47,6 @@ template <bool X>
 struct Flag {
   static constexpr bool value = X;
 };
-__device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
-}
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // kGroup threads per token row, a block (256) or a warp (32, eight rows to a block).  The row's cosines and sines are computed
 // once (the angle in 64 bits: turns = position * turns_per_position, reduced to [-1/2, 1/2] before it is rounded to 32)

@@ -209,6 +209,237 @@ __global__ void __launch_bounds__(kListThreads) free_pages_kernel(const int32_t*
   }
 }
 
+// Pages and places of the new tokens of ragged requests.  One cluster:
+//   rows named twice          every block, in bits of its own shared memory
+//   row starts                every block scans the requests' tokens
+//   entries without a page    each block looks at its share of the requests' table entries and counts
+//   pages dealt               the counts meet through shared memory; every block scans them
+//   table, counts, lengths, places of the rows: all threads of the cluster, a row's request found by bisection of the starts
+// Nothing is written before the cluster barrier behind the counts, so no block sees a table that is half changed.
+constexpr int kExtendBlocks = 8, kExtendThreads = 1024, kExtendMax = 8192, kExtendRows = 1 << 18;
+constexpr int kLongPages = 4;              // entries that a thread walks by itself; beyond, its warp does
+struct ExtendParams {
+  const int32_t* rows;
+  const int32_t* old_lens;
+  const int32_t* new_tokens;
+  int32_t* table;
+  int32_t* refs;
+  const int32_t* free_list;
+  const int32_t* free_count;
+  const int32_t* free_begin;
+  int32_t* free_end;
+  int32_t* row_starts;
+  int32_t* new_lens;
+  int32_t* seq;
+  int32_t* slots;
+  uint32_t* status;
+  int64_t num_pages, max_list;
+  int32_t n, num_rows, max_pages, max_rows;
+};
+size_t extend_smem(int n, int num_rows) { return (size_t)(2 * ((num_rows + 31) / 32) + 3 * n + 2) * 4; }
+
+__global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendParams p) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  extern __shared__ int32_t extend_s[];
+  __shared__ int64_t wsum[kExtendThreads / 32];
+  const int bits = (p.num_rows + 31) / 32, n = p.n;
+  uint32_t* once = reinterpret_cast<uint32_t*>(extend_s);        // rows that are named, and named twice
+  uint32_t* twice = once + bits;
+  int32_t* need = extend_s + 2 * bits;                            // pages a request lacks, -1 if it is refused or idle
+  int32_t* base = need + n;                                       // the first of its pages in the list, -1 if it gets none
+  int32_t* start = base + n;                                      // [n + 1] its first row
+  const int rank = (int)cluster.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  for (int i = tid; i < 2 * bits; i += kExtendThreads) once[i] = 0u;
+  __syncthreads();
+  const int per = (n + kExtendThreads - 1) / kExtendThreads, f0 = min(tid * per, n), f1 = min(f0 + per, n);   // requests this thread scans
+  // exclusive prefix over the threads of one value each; `all`: the sum
+  auto scan = [&](int64_t v, int64_t& all) -> int64_t {
+    int64_t incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (lane == 31) wsum[warp] = incl;
+    __syncthreads();
+    if (warp == 0) {
+      int64_t w = wsum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
+      }
+      wsum[lane] = w;
+    }
+    __syncthreads();
+    const int64_t before = (warp ? wsum[warp - 1] : 0) + incl - v;
+    all = wsum[31];
+    __syncthreads();
+    return before;
+  };
+  int64_t tokens = 0, all_tokens;
+  for (int f = f0; f < f1; ++f) {
+    const int32_t row = p.rows[f];
+    if (row >= 0 && row < p.num_rows) {
+      const uint32_t bit = 1u << (row & 31);
+      if (atomicOr(once + (row >> 5), bit) & bit) atomicOr(twice + (row >> 5), bit);
+    }
+    tokens += max(p.new_tokens[f], 0);
+  }
+  int64_t at = scan(tokens, all_tokens);                          // (its barriers also close the bits)
+  const int64_t room = p.max_rows >= 0 ? p.max_rows : INT32_MAX;
+  for (int f = f0; f < f1; ++f) {
+    start[f] = (int32_t)min(at, room);
+    at += max(p.new_tokens[f], 0);
+    base[f] = at > room ? -1 : 0;                                 // do its rows fit?
+  }
+  if (tid == 0) start[n] = (int32_t)min(all_tokens, room);
+  const int64_t count = min((int64_t)*p.free_count, p.max_list), begin = p.free_begin ? max(*p.free_begin, 0) : 0;
+  __syncthreads();
+
+  // a thread per request of this block's share; long ones by the warp
+  const int s0 = (int)((int64_t)n * rank / kExtendBlocks), s1 = (int)((int64_t)n * (rank + 1) / kExtendBlocks);
+  for (int g0 = s0 + warp * 32; g0 < s1; g0 += kExtendThreads) {
+    const int f = g0 + lane;
+    int32_t row = -1, c = 0, first = 0, end = 0, lacks = -1;
+    bool bad = false;
+    if (f < s1) {
+      row = p.rows[f];
+      c = p.old_lens[f];
+      const int32_t m = p.new_tokens[f];
+      if (row >= 0) {
+        bad = row >= p.num_rows || (twice[row >> 5] >> (row & 31) & 1u) || c < 0 || m < 0 ||
+              (int64_t)c + m > min((int64_t)p.max_pages * kPage, (int64_t)INT32_MAX) || base[f] < 0;
+        if (!bad) {
+          lacks = 0;
+          if (m > 0) {
+            first = c / kPage;
+            end = (c + m - 1) / kPage + 1;
+          }
+        }
+      }
+    }
+    auto look = [&](int32_t row, int32_t c, int32_t i, bool& wrong) -> int {   // does entry i lack a page?
+      const int32_t id = p.table[(int64_t)row * p.max_pages + i];
+      if (id < 0) {
+        wrong |= i == c / kPage && c % kPage != 0;                // the tokens in it are gone
+        return 1;
+      }
+      wrong |= id >= p.num_pages || p.refs[id] != 1;              // tokens must not be written to a page that others hold
+      return 0;
+    };
+    if (end - first <= kLongPages)
+      for (int i = first; i < end; ++i) lacks += look(row, c, i, bad);
+    uint32_t rest = __ballot_sync(0xffffffffu, end - first > kLongPages);
+    for (; rest; rest &= rest - 1) {
+      const int who = __ffs(rest) - 1;
+      const int32_t r = __shfl_sync(0xffffffffu, row, who), cc = __shfl_sync(0xffffffffu, c, who);
+      const int32_t a = __shfl_sync(0xffffffffu, first, who), e = __shfl_sync(0xffffffffu, end, who);
+      int32_t sum = 0;
+      bool wrong = false;
+      for (int i = a + lane; i < e; i += 32) sum += look(r, cc, i, wrong);
+      sum = __reduce_add_sync(0xffffffffu, sum);
+      wrong = __any_sync(0xffffffffu, wrong);
+      if (lane == who) {
+        lacks = sum;
+        bad = wrong;
+      }
+    }
+    if (bad) {
+      lacks = -1;
+      atomicOr(p.status, kErrBadPage);
+    }
+    if (f < s1) need[f] = lacks;
+  }
+  cluster.sync();
+  for (int f = tid; f < n; f += kExtendThreads) {                 // the other blocks' counts
+    int r = (int)((int64_t)f * kExtendBlocks / n);
+    while (f >= (int)((int64_t)n * (r + 1) / kExtendBlocks)) ++r;
+    while (f < (int)((int64_t)n * r / kExtendBlocks)) --r;
+    if (r != rank) need[f] = *cluster.map_shared_rank(need + f, r);
+  }
+  cluster.sync();                                                 // (nobody leaves, or changes the table, while its counts are read)
+  int64_t pages = 0, all_pages;
+  for (int f = f0; f < f1; ++f) pages += max(need[f], 0);
+  at = scan(pages, all_pages);
+  const int64_t avail = max(count - begin, (int64_t)0);
+  int64_t given = 0;
+  for (int f = f0; f < f1; ++f) {
+    const int32_t k = need[f];
+    if (k > 0) at += k;
+    base[f] = k < 0 || (k > 0 && at > avail) ? -1 : (int32_t)(at - max(k, 0));
+    if (k > 0 && at <= avail) given = at;
+  }
+  // what is dealt out is a prefix of the list: the largest end of a request that was served
+  for (int o = 16; o > 0; o >>= 1) given = max(given, __shfl_xor_sync(0xffffffffu, given, o));
+  if (lane == 0) wsum[warp] = given;
+  __syncthreads();
+  if (p.free_end && rank == 0 && tid == 0) {
+    for (int w = 0; w < kExtendThreads / 32; ++w) given = max(given, wsum[w]);
+    *p.free_end = (int32_t)(begin + given);
+  }
+
+  const int all = kExtendBlocks * kExtendThreads, gt = rank * kExtendThreads + tid;
+  for (int g0 = gt - lane; g0 < n; g0 += all) {
+    const int f = g0 + lane;
+    int32_t row = -1, c = 0, first = 0, end = 0, from = -1;
+    if (f < n) {
+      from = base[f];
+      c = p.old_lens[f];
+      const int32_t m = p.new_tokens[f];
+      if (p.row_starts) p.row_starts[f] = start[f];
+      if (p.new_lens) p.new_lens[f] = from >= 0 ? c + m : c;
+      if (from >= 0 && need[f] > 0) {
+        row = p.rows[f];
+        first = c / kPage;
+        end = (c + m - 1) / kPage + 1;
+      }
+    }
+    auto deal = [&](int32_t* entry, int64_t k) {                  // the k-th page from the cursor
+      const int32_t id = p.free_list[begin + k];
+      if (id < 0 || id >= p.num_pages || atomicCAS(p.refs + id, 0, 1) != 0) atomicOr(p.status, kErrBadPage);
+      else *entry = id;
+    };
+    int32_t* mine = p.table + (int64_t)row * p.max_pages;
+    if (end - first <= kLongPages)
+      for (int i = first; i < end; ++i)
+        if (mine[i] < 0) deal(mine + i, from++);
+    uint32_t rest = __ballot_sync(0xffffffffu, end - first > kLongPages);
+    for (; rest; rest &= rest - 1) {
+      const int who = __ffs(rest) - 1;
+      int32_t* theirs = p.table + (int64_t)__shfl_sync(0xffffffffu, row, who) * p.max_pages;
+      const int32_t a = __shfl_sync(0xffffffffu, first, who), e = __shfl_sync(0xffffffffu, end, who);
+      int32_t k = __shfl_sync(0xffffffffu, from, who);
+      for (int i0 = a; i0 < e; i0 += 32) {
+        const int i = i0 + lane;
+        const bool wants = i < e && theirs[i] < 0;
+        const uint32_t who_wants = __ballot_sync(0xffffffffu, wants);
+        if (wants) deal(theirs + i, k + __popc(who_wants & ((1u << lane) - 1u)));
+        k += __popc(who_wants);
+      }
+    }
+  }
+  if (p.row_starts && gt == 0) p.row_starts[n] = start[n];
+  for (int r = gt; r < p.max_rows; r += all) {
+    int32_t seq = -1, slot = -1;
+    if (r < start[n]) {
+      int lo = 0, hi = n;                                         // start[lo] <= r < start[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= r) lo = mid; else hi = mid;
+      }
+      if (base[lo] >= 0) {
+        seq = p.rows[lo];
+        slot = p.old_lens[lo] + (r - start[lo]);
+      }
+    }
+    p.seq[r] = seq;
+    p.slots[r] = slot;
+  }
+}
+
 // The layers of a table group: in range and named once.
 bool layers_ok(const opw_stage_view& v, const int32_t* layers, int32_t n) {
   if (!layers || n < 1 || n > v.num_layers) return false;
@@ -311,6 +542,74 @@ extern "C" opw_status_t opw_kv_free_pages(opw_attn_stage_t* stage, const int32_t
     (void)cudaGetLastError();
     return OPW_ERR_CUDA;
   }
+  *v.launches += 1;
+  return OPW_OK;
+}
+
+extern "C" opw_status_t opw_kv_extend(opw_attn_stage_t* stage, int32_t n, const int32_t* rows, const int32_t* old_lens,
+                                      const int32_t* new_tokens, int32_t num_rows, int32_t* page_table, int32_t* refcounts,
+                                      int64_t num_pages, const int32_t* free_list, int64_t max_list, const int32_t* free_count,
+                                      const int32_t* free_begin, int32_t* free_end, int32_t* row_starts, int32_t* new_lens,
+                                      int32_t max_rows, int32_t* seq, int32_t* slots, void* cuda_stream) {
+  if (!stage || n < 0 || num_rows < 1 || num_pages < 1 || num_pages > INT32_MAX || max_list < 0 || max_list > INT32_MAX || max_rows < -1)
+    return OPW_ERR_INVALID_ARG;
+  if ((seq == nullptr) != (slots == nullptr) || (seq ? max_rows < 0 : max_rows > 0)) return OPW_ERR_INVALID_ARG;
+  if (!free_count || (max_list > 0 && !free_list) || (n > 0 && (!rows || !old_lens || !new_tokens || !page_table || !refcounts)))
+    return OPW_ERR_INVALID_ARG;
+  if (((uintptr_t)rows | (uintptr_t)old_lens | (uintptr_t)new_tokens | (uintptr_t)page_table | (uintptr_t)refcounts | (uintptr_t)free_list |
+       (uintptr_t)free_count | (uintptr_t)free_begin | (uintptr_t)free_end | (uintptr_t)row_starts | (uintptr_t)new_lens | (uintptr_t)seq |
+       (uintptr_t)slots) % 4)
+    return OPW_ERR_INVALID_ARG;
+  const opw_stage_view v = opw_view_of(stage);
+  if (n > opw_pages::kExtendMax || num_rows > opw_pages::kExtendRows) return OPW_ERR_CAPACITY;
+  // what is written must not meet what other blocks still read, nor each other
+  const size_t each = (size_t)n * 4, map = max_rows > 0 ? (size_t)max_rows * 4 : 0;
+  const struct { const void* at; size_t bytes; } ins[] = {{rows, each}, {old_lens, each}, {new_tokens, each}, {free_list, (size_t)max_list * 4}, {free_count, 4}};
+  const struct { const void* at; size_t bytes; } outs[] = {{page_table, (size_t)num_rows * v.max_pages * 4}, {refcounts, (size_t)num_pages * 4},
+                                                           {free_end, 4}, {row_starts, each + 4}, {new_lens, each}, {seq, map}, {slots, map}};
+  constexpr int kOuts = sizeof(outs) / sizeof(outs[0]);
+  for (int i = 0; i < kOuts; ++i) {
+    if (!outs[i].at || outs[i].bytes == 0) continue;
+    auto meets = [&](const void* in, size_t bytes) { return in && bytes && opw_overlap(outs[i].at, outs[i].bytes, in, bytes); };
+    for (const auto& in : ins)
+      if (meets(in.at, in.bytes)) return OPW_ERR_INVALID_ARG;
+    if (outs[i].at != free_begin && meets(free_begin, 4)) return OPW_ERR_INVALID_ARG;
+    if (outs[i].at == free_begin && outs[i].at != free_end) return OPW_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (meets(outs[j].at, outs[j].bytes)) return OPW_ERR_INVALID_ARG;
+  }
+  opw_pages::ExtendParams p;
+  p.rows = rows;
+  p.old_lens = old_lens;
+  p.new_tokens = new_tokens;
+  p.table = page_table;
+  p.refs = refcounts;
+  p.free_list = free_list;
+  p.free_count = free_count;
+  p.free_begin = free_begin;
+  p.free_end = free_end;
+  p.row_starts = row_starts;
+  p.new_lens = new_lens;
+  p.seq = seq;
+  p.slots = slots;
+  p.status = v.status;
+  p.num_pages = num_pages;
+  p.max_list = max_list;
+  p.n = n;
+  p.num_rows = num_rows;
+  p.max_pages = v.max_pages;
+  p.max_rows = max_rows;
+  opw_device_guard guard(v.device);
+  if (!guard.ok()) return OPW_ERR_CUDA;
+  const size_t smem = opw_pages::extend_smem(n, num_rows);
+  cudaError_t e = cudaSuccess;
+  if (smem > 40 * 1024)
+    e = cudaFuncSetAttribute(opw_pages::extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)opw_pages::extend_smem(opw_pages::kExtendMax, opw_pages::kExtendRows));
+  if (e == cudaSuccess)
+    e = opw_launch(opw_pages::extend_kernel, dim3(opw_pages::kExtendBlocks), dim3(opw_pages::kExtendThreads), smem,
+                   static_cast<cudaStream_t>(cuda_stream), v.pdl, opw_pages::kExtendBlocks, p);
+  if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   *v.launches += 1;
   return OPW_OK;
 }
