@@ -19,12 +19,13 @@ SOURCES = [os.path.join(_HERE, "csrc", "opw_attn.cu"), os.path.join(_HERE, "csrc
            os.path.join(_HERE, "csrc", "opw_linear_attn.cu"), os.path.join(_HERE, "csrc", "opw_afd.cu"),
            os.path.join(_HERE, "csrc", "opw_tree_attn.cu"), os.path.join(_HERE, "csrc", "opw_draft.cu"),
            os.path.join(_HERE, "csrc", "opw_pages.cu"), os.path.join(_HERE, "csrc", "opw_norm_rope.cu"),
-           os.path.join(_HERE, "csrc", "opw_verify.cu")]
+           os.path.join(_HERE, "csrc", "opw_verify.cu"), os.path.join(_HERE, "csrc", "opw_prefix_attn.cu")]
 HEADERS = [os.path.join(_HERE, "csrc", "opw_kernels.cuh"), os.path.join(_HERE, "csrc", "opw_afd_gemm.cuh"), os.path.join(_ROOT, "include", "opw_attn.h"),
            os.path.join(_ROOT, "include", "opw_linear_attn.h"), os.path.join(_ROOT, "include", "opw_afd.h"),
            os.path.join(_ROOT, "include", "opw_draft.h"), os.path.join(_ROOT, "include", "opw_pages.h"),
            os.path.join(_HERE, "csrc", "opw_stage.h"), os.path.join(_HERE, "csrc", "opw_tree_kernels.cuh"),
-           os.path.join(_HERE, "csrc", "opw_tree_mma.cuh"), os.path.join(_HERE, "csrc", "opw_words.cuh")]
+           os.path.join(_ROOT, "include", "opw_prefix.h"), os.path.join(_HERE, "csrc", "opw_prefix_kernels.cuh"),
+           os.path.join(_HERE, "csrc", "opw_pool_map.h"), os.path.join(_HERE, "csrc", "opw_tree_mma.cuh"), os.path.join(_HERE, "csrc", "opw_words.cuh")]
 
 OPW_FLAG_NO_PDL = 1
 OPW_FLAG_COPY_STREAMS = 2
@@ -43,7 +44,8 @@ EXPORTS = [
     "opw_afd_module_launch_count", "opw_afd_module_set_trace", "opw_hbm_read_probe",
     "opw_rope_table", "opw_rope_append", "opw_tree_mask", "opw_tree_attn_workspace_bytes", "opw_tree_attn_create",
     "opw_tree_attn_destroy", "opw_tree_attention", "opw_kv_commit", "opw_kv_fork", "opw_kv_release", "opw_kv_free_pages",
-    "opw_norm_rope_append", "opw_tree_verify", "opw_kv_extend",
+    "opw_norm_rope_append", "opw_tree_verify", "opw_kv_extend", "opw_prefix_attn_workspace_bytes", "opw_prefix_attn_create",
+    "opw_prefix_attn_destroy", "opw_prefix_attention",
 ]
 
 
@@ -116,6 +118,7 @@ class RopeConfig(ctypes.Structure):
 OPW_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 OPW_ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
 OPW_TREE_MAX_NODES = 64
+OPW_PREFIX_MAX_BATCH, OPW_PREFIX_MAX_GROUPS = 2048, 1024
 OPW_PROBS_F32, OPW_PROBS_BF16 = 0, 1
 OPW_DRAW_AGAIN, OPW_DRAW_DISTINCT, OPW_DRAW_CERTAIN = 0, 1, 2
 OPW_OP_ATTENTION, OPW_OP_LINEAR, OPW_OP_AFD_MODULE = 0, 1, 2
@@ -251,6 +254,14 @@ def lib() -> ctypes.CDLL:
                                        vp, vp, vp]
     L.opw_tree_verify.restype = ctypes.c_int
     L.opw_tree_verify.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.opw_prefix_attn_workspace_bytes.restype = ctypes.c_size_t
+    L.opw_prefix_attn_workspace_bytes.argtypes = [vp]
+    L.opw_prefix_attn_create.restype = ctypes.c_int
+    L.opw_prefix_attn_create.argtypes = [vp, ctypes.c_uint32, vp, ctypes.c_size_t, ctypes.POINTER(vp)]
+    L.opw_prefix_attn_destroy.restype = ctypes.c_int
+    L.opw_prefix_attn_destroy.argtypes = [vp]
+    L.opw_prefix_attention.restype = ctypes.c_int
+    L.opw_prefix_attention.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.opw_kv_extend.restype = ctypes.c_int
     L.opw_kv_extend.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     L.opw_attn_stage_launch_count.restype = i64
@@ -559,6 +570,26 @@ def opw_tree_attention(tree: int, layer: int, batch: int, nodes: int, q: int, tr
                        tree_lens: int, page_table: int, out: int, lse: Optional[int] = None, stream: Optional[int] = None) -> None:
     _check(lib().opw_tree_attention(tree, layer, batch, nodes, q, tree_mask, positions, ctx_lens, tree_lens, page_table, out, lse,
                                     stream), "opw_tree_attention")
+
+
+def opw_prefix_attn_workspace_bytes(stage: int) -> int:
+    return int(lib().opw_prefix_attn_workspace_bytes(stage))
+
+
+def opw_prefix_attn_create(stage: int, workspace: int, workspace_bytes: int, flags: int = 0) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().opw_prefix_attn_create(stage, flags, workspace, workspace_bytes, ctypes.byref(h)), "opw_prefix_attn_create")
+    return h.value
+
+
+def opw_prefix_attn_destroy(prefix: Optional[int]) -> None:
+    _check(lib().opw_prefix_attn_destroy(prefix), "opw_prefix_attn_destroy")
+
+
+def opw_prefix_attention(prefix: int, layer: int, batch: int, groups: int, q: int, kv_lens: int, group_starts: int, prefix_lens: int,
+                         page_table: int, out: int, lse: Optional[int] = None, stream: Optional[int] = None) -> None:
+    _check(lib().opw_prefix_attention(prefix, layer, batch, groups, q, kv_lens, group_starts, prefix_lens, page_table, out, lse, stream),
+           "opw_prefix_attention")
 
 
 _layer_arrays: dict = {}
@@ -980,6 +1011,56 @@ class TreeAttention:
     def close(self):
         if getattr(self, "handle", None):
             opw_tree_attn_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class PrefixAttention:
+    """Owner of one handle of attention behind shared prefixes and of its workspace.  Calls of one handle must not overlap."""
+
+    def __init__(self, stage: Stage):
+        import torch
+
+        self.stage = stage
+        nbytes = opw_prefix_attn_workspace_bytes(stage.handle)
+        if nbytes == 0:
+            raise OpwError(OPW_ERR_UNSUPPORTED, "opw_prefix_attn_workspace_bytes")
+        self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=stage.device)
+        base = (self.workspace.data_ptr() + 255) // 256 * 256
+        self.handle = opw_prefix_attn_create(stage.handle, base, nbytes)
+
+    def attention(self, layer, q, kv_lens, group_starts, prefix_lens, page_table, out, lse=None):
+        """q, out: bf16 [batch, Hq, D]; kv_lens: int32 [batch]; group_starts: int32 [groups + 1], prefix_lens: int32 [groups]: rows
+        group_starts[g] .. group_starts[g + 1] - 1 hold the same pages in their first prefix_lens[g] tokens; lse: fp32 [batch, Hq] or None."""
+        where, st = "prefix attention", self.stage
+        shape, dev = q.shape, st.index
+        if not st.handle:
+            raise ValueError(f"{where}: the stage is closed")
+        if len(shape) != 3 or shape[1] != st.num_q_heads or shape[2] != st.head_dim:
+            raise ValueError(f"{where}: q must be [batch, {st.num_q_heads}, {st.head_dim}], got {tuple(shape)}")
+        batch, groups = shape[0], prefix_lens.shape[0]
+        _need(where, dev, st._bf16, batch * st.num_q_heads * st.head_dim, q, out)
+        _need(where, dev, st._i32, batch, kv_lens)
+        _need(where, dev, st._i32, groups, prefix_lens)
+        _need(where, dev, st._i32, groups + 1, group_starts)
+        st._table_rows(where, page_table, batch)
+        lse_ptr = None
+        if lse is not None:
+            _need(where, dev, st._f32, batch * st.num_q_heads, lse)
+            lse_ptr = lse.data_ptr()
+        rc = st._lib.opw_prefix_attention(self.handle, layer, batch, groups, q.data_ptr(), kv_lens.data_ptr(), group_starts.data_ptr(),
+                                          prefix_lens.data_ptr(), page_table.data_ptr(), out.data_ptr(), lse_ptr, st._raw_stream(dev))
+        if rc:
+            _check(rc, "opw_prefix_attention")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            opw_prefix_attn_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

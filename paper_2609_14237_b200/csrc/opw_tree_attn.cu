@@ -4,6 +4,7 @@
 #include <vector>
 
 #include "opw_draft.h"
+#include "opw_pool_map.h"
 #include "opw_stage.h"
 #include "opw_tree_kernels.cuh"
 #include "opw_tree_mma.cuh"
@@ -102,21 +103,6 @@ cudaError_t launch_mma(const opw_stage_view& v, const CUtensorMap& map, const op
                     opw_tree::MmaTree<D, kWide>::smem(p.batch), stream, v.pdl, 1, map, p);
 }
 
-typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// One layer's pool as [page and head][K, V][slot][64 dimensions at a time][64]; a box is 16 slots of 64 dimensions.  No
-// swizzle: the pool's own permutation is the one the tensor core expects.
-bool encode_pool(TensorMapEncodeFn fn, CUtensorMap* map, void* pool, const opw_stage_view& v, int64_t num_pages) {
-  const cuuint64_t row = (cuuint64_t)v.D * 2;
-  const cuuint64_t dims[5] = {64, (cuuint64_t)v.D / 64, 16, 2, (cuuint64_t)num_pages * v.Hkv};
-  const cuuint64_t strides[4] = {128, row, 16 * row, 32 * row};
-  const cuuint32_t box[5] = {64, 1, 16, 1, 1}, elem[5] = {1, 1, 1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, pool, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 }  // namespace
 
 struct opw_tree_attn {
@@ -167,23 +153,14 @@ extern "C" opw_status_t opw_tree_attn_create(opw_attn_stage_t* stage, int32_t ma
   } else {
     e = raise_smem<256>();
   }
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
-  if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !fn) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
+  if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   opw_tree_attn* t = new (std::nothrow) opw_tree_attn();
   if (!t) return OPW_ERR_INVALID_ARG;
-  try {
-    t->maps.resize(v.D == 256 ? 0 : v.num_layers);
-  } catch (...) {
+  const opw_status_t mapped = v.D == 256 ? OPW_OK : opw_map_pools(v, &t->maps);
+  if (mapped != OPW_OK) {
     delete t;
-    return OPW_ERR_INVALID_ARG;
+    return mapped;
   }
-  for (size_t i = 0; i < t->maps.size(); ++i)
-    if (!encode_pool(reinterpret_cast<TensorMapEncodeFn>(fn), &t->maps[i], v.pool[i], v, v.num_pages[i])) {
-      delete t;
-      return OPW_ERR_CUDA;
-    }
   t->stage = stage;
   t->max_nodes = max_nodes;
   t->lay = lay;

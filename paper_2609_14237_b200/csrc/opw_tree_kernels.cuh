@@ -39,15 +39,18 @@ struct TreeParams {
   float scale_log2e;
 };
 
-// What of sequence b takes part: context length, tree size, first key that any node can see, end, row blocks.
+// What of sequence b takes part: context length, tree size, first key that any node can see, end, row blocks; the row of the page table
+// and the first row of the queries.
 struct Span {
-  int32_t ctx, tree, lo, n, blocks;
+  int32_t ctx, tree, lo, n, blocks, table_row, first_row;
   bool cut;              // the lengths did not fit the table or the call: recorded as OPW_ERR_BAD_PAGE
 };
 __device__ __forceinline__ Span span_of(const TreeParams& p, int b, int row_block) {
   Span s;
   s.ctx = p.ctx_lens[b];
   s.tree = p.tree_lens[b];
+  s.table_row = b;
+  s.first_row = b * p.nodes;
   s.cut = false;
   if (s.ctx < 0 || s.tree <= 0) { s.ctx = s.tree = s.lo = s.n = s.blocks = 0; return s; }
   if (s.tree > p.nodes) { s.tree = p.nodes; s.cut = true; }
@@ -67,19 +70,32 @@ __device__ __forceinline__ int32_t tiles_of(const Span& s, int keys) {
   return (s.n - first + keys - 1) / keys;
 }
 
-// Units before each sequence, for the whole block: cum[0..batch] in shared memory.  Also records cut lengths (block 0).
-__device__ __forceinline__ void scan_units(const TreeParams& p, int64_t* cum, int row_block, int keys) {
+// The kernels below take any problem that answers as this one does: `entities` of it, each with its span, whose row r is node r / G with
+// query head g * G + r % G, what a row of it sees, and where a row's result goes.  (Attention behind shared prefixes is the other one.)
+__device__ __forceinline__ int entities(const TreeParams& p) { return p.batch; }
+// Where a row's unnormalised output, maximum and sum go.
+struct RowPart {
+  float *o, *m, *l;
+};
+__device__ __forceinline__ RowPart whole_row(const TreeParams&, const Span&, int64_t) { return {nullptr, nullptr, nullptr}; }   // (never asked)
+// Is a row that one worker has seen all of finished there and then, as opposed to left in fp32 for a merge?
+__device__ __forceinline__ bool finished_at_once(const TreeParams&, const Span&) { return true; }
+
+// Units before each entity, for the whole block: cum[0..entities] in shared memory.  `record`: note lengths that were cut (one block does).
+template <class Problem>
+__device__ __forceinline__ void scan_units(const Problem& p, int64_t* cum, int row_block, int keys, bool record) {
   __shared__ int64_t wsum[32];
   __shared__ int64_t carry;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) carry = 0;
   __syncthreads();
-  for (int base = 0; base < p.batch; base += blockDim.x) {
+  const int batch = entities(p);
+  for (int base = 0; base < batch; base += blockDim.x) {
     const int b = base + threadIdx.x;
     int64_t cnt = 0;
-    if (b < p.batch) {
+    if (b < batch) {
       const Span s = span_of(p, b, row_block);
-      if (s.cut && blockIdx.x == 0) atomicOr(p.status, kErrBadPage);
+      if (s.cut && record) atomicOr(p.status, kErrBadPage);
       cnt = (int64_t)tiles_of(s, keys) * s.blocks * p.Hkv;
     }
     int64_t incl = cnt;
@@ -92,12 +108,12 @@ __device__ __forceinline__ void scan_units(const TreeParams& p, int64_t* cum, in
     __syncthreads();
     int64_t before = carry;
     for (int w = 0; w < warp; ++w) before += wsum[w];
-    if (b < p.batch) cum[b] = before + incl - cnt;
+    if (b < batch) cum[b] = before + incl - cnt;
     __syncthreads();
     if (threadIdx.x == blockDim.x - 1) carry = before + incl;
     __syncthreads();
   }
-  if (threadIdx.x == 0) cum[p.batch] = carry;
+  if (threadIdx.x == 0) cum[batch] = carry;
   __syncthreads();
 }
 // How many of the launched workers share U units: never more than there are units, and with single pages as units (a warp each) at least
@@ -124,7 +140,7 @@ struct RowView {
 };
 // (Called, not inlined, as all of the rare paths here: the kernels' loops have to stay in the instruction cache.  With everything
 // inlined the tensor-core kernel had 180 KB of code and spent most of its time fetching it.)
-__device__ __noinline__ RowView row_view(const uint64_t* mask, const int32_t* pos, int32_t window, int32_t ctx, int32_t n, int32_t tree,
+static __device__ __noinline__ RowView row_view(const uint64_t* mask, const int32_t* pos, int32_t window, int32_t ctx, int32_t n, int32_t tree,
                                          int node) {
   RowView v;
   v.bits = mask[node];
@@ -145,7 +161,7 @@ __device__ __forceinline__ RowView row_view(const TreeParams& p, int b, const Sp
   return row_view(p.mask + (int64_t)b * p.nodes, p.positions + (int64_t)b * p.nodes, p.window, s.ctx, s.n, s.tree, node);
 }
 // The bounded wait with its loop out of line.
-__device__ __noinline__ bool mbar_wait_loop(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ bool mbar_wait_loop(uint32_t bar, uint32_t parity) {
   const uint64_t t0 = global_timer_ns();
 #pragma unroll 1
   for (;;) {
@@ -203,20 +219,19 @@ struct WarpTree {
   }
 };
 
-template <int D>
-__global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(TreeParams p) {
+// kWarps warps of a block take part; worker numbers go across the blocks first.  `block` of `blocks` are this problem's.  smem: the rings,
+// then their barriers; cum: the entities' units (scan_units).
+template <int D, int kWarps, class Problem>
+__device__ __forceinline__ void warp_body(const Problem& p, unsigned char* smem, const int64_t* cum, int block, int blocks) {
   using C = WarpTree<D>;
   constexpr int KS = D / 16, NT = D / 8, ROWB = D * 2, TILE = C::kTile;
   constexpr uint32_t kFirst = 1u << 28, kLast = 1u << 29, kBad = 1u << 30, kPageBits = kFirst - 1;
-  extern __shared__ __align__(128) unsigned char smem[];
-  const int warps = C::kWarps, stages = C::kStages;
+  const int warps = kWarps, stages = C::kStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)warps * stages * TILE);
-  int64_t* cum = reinterpret_cast<int64_t*>(bars + warps * stages);
-
-  scan_units(p, cum, C::kRows, kPage);
-  const int64_t U = cum[p.batch];
-  const int64_t workers = workers_for(U, (int64_t)gridDim.x * warps, kPage), worker = (int64_t)warp * gridDim.x + blockIdx.x;
+  const int batch = entities(p);
+  const int64_t U = cum[batch];
+  const int64_t workers = workers_for(U, (int64_t)blocks * warps, kPage), worker = (int64_t)warp * blocks + block;
   const uint32_t ring = smem_u32(smem + (size_t)warp * stages * TILE);
   const uint32_t bar0 = smem_u32(bars + warp * stages);
   if (lane == 0) {
@@ -232,13 +247,13 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
   auto describe = [&](int64_t u) -> Desc {
     Desc d = {0, 0u};
     if (u >= u1) return d;
-    const int b = find_sequence(cum, p.batch, u);
+    const int b = find_sequence(cum, batch, u);
     const Span s = span_of(p, b, C::kRows);
     const int32_t cnt = tiles_of(s, kPage);
     const int64_t rem = u - cum[b];
     const int32_t ri = (int32_t)(rem / cnt), i = (int32_t)(rem - (int64_t)ri * cnt), g = ri / s.blocks;
     const int32_t lp = s.lo / kPage + i;
-    int64_t pid = p.page_table[(int64_t)b * p.max_pages + lp];
+    int64_t pid = p.page_table[(int64_t)s.table_row * p.max_pages + lp];
     d.page = (uint32_t)lp | (i == 0 ? kFirst : 0u) | (i == cnt - 1 ? kLast : 0u);
     if (pid < 0 || pid >= p.num_pages) {      // never dereference a bad page: mask it out
       atomicOr(p.status, kErrBadPage);
@@ -252,8 +267,8 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
   Desc wa = describe(u0 + lane), wb = describe(u0 + 32 + lane);
   pdl_launch_dependents();                    // (as in the tensor-core kernel)
   pdl_wait();                                 // up to here only this step's lengths and the page table were read
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i <= p.batch; i += blockDim.x) p.cum[i] = cum[i];
+  if (block == 0)
+    for (int i = threadIdx.x; i <= batch; i += kWarps * 32) p.cum[i] = cum[i];
 
   const uint64_t policy = l2_evict_first_policy();
   auto issue = [&](int64_t u, int slot) {
@@ -275,7 +290,7 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
   float o[NT][4], mx[2], l[2];
   int b = 0, g = 0, rb = 0, rows = 0;
   int32_t border = 0;
-  Span sp = {0, 0, 0, 0, 1, false};
+  Span sp = {0, 0, 0, 0, 1, 0, 0, false};
   bool from_first = false, on_first_row = true, failed = false;
   int slot = 0;
   uint32_t phase = 0;
@@ -290,7 +305,7 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
     const bool last = page & kLast;
     if (u == u0 || (page & kFirst)) {         // a new row block: its queries, an empty state
       from_first = page & kFirst;
-      b = find_sequence(cum, p.batch, u);
+      b = find_sequence(cum, batch, u);
       sp = span_of(p, b, C::kRows);
       const int32_t ri = (int32_t)((u - cum[b]) / tiles_of(sp, kPage));
       g = ri / sp.blocks;
@@ -302,7 +317,7 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
         const int r = h * 8 + qrow;
         const bool live = r < rows;
         const int R = rb * C::kRows + r, node = R / p.G;
-        const __nv_bfloat16* qb = p.q + (((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G)) * D + qcol;
+        const __nv_bfloat16* qb = p.q + (((int64_t)sp.first_row + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G)) * D + qcol;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           qa[ks][h] = live ? *reinterpret_cast<const uint32_t*>(qb + ks * 16) : 0u;
@@ -453,7 +468,7 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
     if (++slot == stages) { slot = 0; phase ^= 1u; }
 
     if (last || u == u1 - 1) {                // the row block, or this worker's part of it, is done
-      const bool complete = from_first && last;
+      const bool complete = from_first && last, finish = complete && finished_at_once(p, sp);
       float* pb = p.partials + (2 * worker + (on_first_row ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -462,9 +477,9 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
         t += __shfl_xor_sync(0xffffffffu, t, 2);
         const int r = h * 8 + qrow;
         if (r >= rows) continue;
-        if (complete) {
-          const int R = rb * C::kRows + r, node = R / p.G;
-          const int64_t row = ((int64_t)b * p.nodes + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
+        const int R = rb * C::kRows + r, node = R / p.G;
+        const int64_t row = ((int64_t)sp.first_row + node) * p.Hq + (int64_t)g * p.G + (R - node * p.G);
+        if (finish) {
           const float inv = t > 0.f ? 1.f / t : 0.f;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -473,12 +488,13 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
           if (p.lse && (lane & 3) == 0)
             p.lse[row] = t > 0.f ? (mx[h] + log2f(t)) * 0.6931471805599453f : t == 0.f ? -INFINITY : t;
         } else {
+          const RowPart part = complete ? whole_row(p, sp, row) : RowPart{pb + r * D, pb + C::kRows * D + r, pb + C::kRows * (D + 1) + r};
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
-            *reinterpret_cast<float2*>(pb + r * D + nt * 8 + qcol) = make_float2(o[nt][2 * h], o[nt][2 * h + 1]);
+            *reinterpret_cast<float2*>(part.o + nt * 8 + qcol) = make_float2(o[nt][2 * h], o[nt][2 * h + 1]);
           if ((lane & 3) == 0) {
-            pb[C::kRows * D + r] = mx[h];
-            pb[C::kRows * (D + 1) + r] = t;
+            *part.m = mx[h];
+            *part.l = t;
           }
         }
       }
@@ -493,6 +509,15 @@ __global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(
       if (++slot == stages) { slot = 0; phase ^= 1u; }
     }
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(WarpTree<D>::kWarps * 32, 1) tree_warp_kernel(TreeParams p) {
+  using C = WarpTree<D>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  int64_t* cum = reinterpret_cast<int64_t*>(smem + (size_t)C::kWarps * C::kStages * (C::kTile + 8));
+  scan_units(p, cum, C::kRows, kPage, blockIdx.x == 0);
+  warp_body<D, C::kWarps>(p, smem, cum, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------------------------

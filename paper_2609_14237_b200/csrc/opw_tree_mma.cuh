@@ -186,10 +186,10 @@ struct Segment {
   bool shared;                 // both slots on every tile (more than 128 rows), or alternate tiles
   Span sp;
 };
-template <int kRows>
-__device__ __forceinline__ Segment segment_at(const TreeParams& p, const int64_t* cum, int64_t u, int64_t u1) {
+template <int kRows, class Problem>
+__device__ __forceinline__ Segment segment_at(const Problem& p, const int64_t* cum, int64_t u, int64_t u1) {
   Segment s;
-  s.b = find_sequence(cum, p.batch, u);
+  s.b = find_sequence(cum, entities(p), u);
   s.sp = span_of(p, s.b, kRows);
   const int32_t cnt = tiles_of(s.sp, kMmaKeys);
   const int64_t rem = u - cum[s.b];
@@ -204,11 +204,12 @@ __device__ __forceinline__ Segment segment_at(const TreeParams& p, const int64_t
   s.shared = kRows > 128 && s.rows > 128;
   return s;
 }
-template <int D, bool kWide>
-__global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_constant__ CUtensorMap map, const TreeParams p) {
+// `block` of `blocks` are this problem's.  smem_raw: kPieces tiles and kQTiles query tiles from its first multiple of 1024 on; cum: room for
+// the entities' units.
+template <int D, bool kWide, class Problem>
+__device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& p, unsigned char* smem_raw, int64_t* cum, int block, int blocks) {
   using C = MmaTree<D, kWide>;
   constexpr uint32_t NK = C::kStagesK, NV = C::kStagesV;
-  extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[NK + NV], empty_bar[NK + NV], s_bar[2][2], p_bar[2][2], o_bar[2][2], seg_bar, end_bar[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int bad_s[kBadRing];                     // pages of a tile that are bad: bit per page; by tile, the last few
@@ -220,7 +221,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t q_smem = base, ring = base + C::kQTiles * C::kQTile, ring_v = ring + NK * C::kPiece;
-  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + (base - raw) + (size_t)C::kPieces * C::kPiece + C::kQTiles * C::kQTile);
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
@@ -246,20 +246,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_before();
-  scan_units(p, cum, C::kRows, kMmaKeys);             // begins and ends with a barrier of the block
+  scan_units(p, cum, C::kRows, kMmaKeys, block == 0);             // begins and ends with a barrier of the block
   tc_after();
   constexpr uint32_t tmem = 0;                        // all 512 columns are this block's: they begin at column 0
-  const int64_t U = cum[p.batch];
-  const int64_t workers = workers_for(U, gridDim.x, kMmaKeys);
-  const bool spare = blockIdx.x >= workers;           // fewer units than blocks
-  const int64_t u0 = spare ? U : worker_begin(U, blockIdx.x, workers), u1 = spare ? U : worker_begin(U, blockIdx.x + 1, workers);
+  const int64_t U = cum[entities(p)];
+  const int64_t workers = workers_for(U, blocks, kMmaKeys);
+  const bool spare = block >= workers;                // fewer units than blocks
+  const int64_t u0 = spare ? U : worker_begin(U, block, workers), u1 = spare ? U : worker_begin(U, block + 1, workers);
   // The combine kernel may queue up behind the first blocks that finish: its blocks do not fit beside one of these (registers), and
   // where they wait they have their index work behind them.  (Released at the end instead, in a replayed graph: chain of 4
   // 12.2 us, this way 11.8; 32 x window 4096 133 to 145 us, this way 111 to 113; call by call there is no difference.)
   pdl_launch_dependents();
   pdl_wait();                                         // up to here only this step's lengths were read
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i <= p.batch; i += kMmaThreads) p.cum[i] = cum[i];
+  if (block == 0)
+    for (int i = threadIdx.x; i <= entities(p); i += kMmaThreads) p.cum[i] = cum[i];
 
   // Bounded wait; after the first that ran out, every wait of the block returns at once and the roles walk on through the
   // same control flow (which depends on lengths only), so that no named barrier is left short.
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       const int32_t page0 = s.sp.lo / kPage + s.t0 * kTilePages + (lane & (kTilePages - 1));
       auto fetch = [&](int t) -> int32_t {            // this lane's page of tile t: raw id, or -2 where there is none
         const int32_t lp = page0 + t * kTilePages;
-        return t < s.n && (int64_t)lp * kPage < s.sp.n ? __ldg(p.page_table + (int64_t)s.b * p.max_pages + lp) : -2;
+        return t < s.n && (int64_t)lp * kPage < s.sp.n ? __ldg(p.page_table + (int64_t)s.sp.table_row * p.max_pages + lp) : -2;
       };
       int32_t id = fetch(0), next = fetch(1);
       for (int t = 0; t < s.n; ++t) {
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
       const int R = s.rb * C::kRows + r, node = R / p.G;
       auto global_row = [&](int rr) {
         const int RR = s.rb * C::kRows + rr, nn = RR / p.G;
-        return ((int64_t)s.b * p.nodes + nn) * p.Hq + (int64_t)s.g * p.G + (RR - nn * p.G);
+        return ((int64_t)sp.first_row + nn) * p.Hq + (int64_t)s.g * p.G + (RR - nn * p.G);
       };
       // queries to shared memory, in the layout of a K-major swizzled operand; rows that are not there: zeros
       const uint32_t qs = q_smem + (kWide ? (uint32_t)x * C::kQTile : 0u);
@@ -654,10 +654,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         c1 = c0 + D / 2;
       }
       tc_after();
-      const bool complete = s.first && s.last;
-      const float inv = !complete ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-      float* pb = p.partials + (2 * (int64_t)blockIdx.x + (on_first ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
+      const bool complete = s.first && s.last, finish = complete && finished_at_once(p, sp);
+      const float inv = !finish ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+      float* pb = p.partials + (2 * (int64_t)block + (on_first ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
       const int64_t grow = live ? global_row(r) : 0;
+      const RowPart part = complete && !finish ? whole_row(p, sp, grow) : RowPart{pb + r * D, pb + C::kRows * D + r, pb + C::kRows * (D + 1) + r};
 #pragma unroll 1
       for (int c = c0; c < c1; c += 32) {
         uint32_t o[32];
@@ -671,7 +672,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
           for (int e = 0; e < 32; ++e)
             o[e] = __float_as_uint(__uint_as_float(o[e]) * scale0 + __uint_as_float(o2[e]) * scale1);
         }
-        if (live && complete) {
+        if (live && finish) {
 #pragma unroll
           for (int e = 0; e < 32; e += 8) {
             uint4 w;
@@ -684,14 +685,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
         } else if (live) {
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<uint4*>(pb + r * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            *reinterpret_cast<uint4*>(part.o + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
         __syncwarp();
       }
       if (live && (s.shared || x == 0)) {
-        if (!complete) {
-          pb[C::kRows * D + r] = m;
-          pb[C::kRows * (D + 1) + r] = l;
+        if (!finish) {
+          *part.m = m;
+          *part.l = l;
         } else if (p.lse) {
           p.lse[grow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
         }
@@ -711,6 +712,15 @@ __global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_c
     tc_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
+}
+
+template <int D, bool kWide>
+__global__ void __launch_bounds__(kMmaThreads, 1) tree_mma_kernel(const __grid_constant__ CUtensorMap map, const TreeParams p) {
+  using C = MmaTree<D, kWide>;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t skip = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
+  int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + skip + (size_t)C::kPieces * C::kPiece + C::kQTiles * C::kQTile);
+  mma_body<D, kWide>(map, p, smem_raw, cum, blockIdx.x, gridDim.x);
 }
 
 }  // namespace opw_tree

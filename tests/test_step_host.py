@@ -75,3 +75,11 @@ def test_the_oracle_of_extending():
     assert starts.tolist() == [0, 2, 35, 75] and lens.tolist() == [17, 33, 0] and end == 4 and not bad
     assert table.tolist() == [[5, 1, -1, -1], [-1] * 4, [2, 3, 4, -1]] and counts.tolist() == [0, 1, 1, 1, 1, 1, 0, 0]
     assert seq.tolist() == [0] * 2 + [2] * 33 + [-1] * 45 and slots.tolist() == [15, 16, *range(33)] + [-1] * 45
+
+
+def test_null_prefix_handles_are_refused():
+    L, h = B.lib(), ctypes.c_void_p()
+    assert L.opw_prefix_attn_workspace_bytes(None) == 0
+    assert L.opw_prefix_attn_create(None, 0, 256, 1 << 30, ctypes.byref(h)) == B.OPW_ERR_INVALID_ARG and h.value is None
+    assert L.opw_prefix_attention(None, 0, 1, 1, *[16] * 6, None, None) == B.OPW_ERR_INVALID_ARG
+    assert L.opw_prefix_attn_destroy(None) == B.OPW_OK
