@@ -15,7 +15,7 @@ namespace cg = cooperative_groups;
 using opw_words::pdl_wait;
 
 constexpr uint32_t kErrBadPage = 1u;      // bit of the stage's status word
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 
 struct Params {
@@ -35,75 +35,76 @@ struct Params {
 
 enum Draw { kAgain = OPW_DRAW_AGAIN, kDistinct = OPW_DRAW_DISTINCT, kCertain = OPW_DRAW_CERTAIN };
 
-// What the branches that the current node has refused leave of its distribution.  r_{j+1} = max(r_j - q_j, 0) / total without a division:
-//     R_0 = r_0, R_{j+1} = max(R_j - c_j Q_j, 0),   r_j = R_j / C_j,  q_j = Q_j / S_j,  c_j = C_j / S_j,
-// C_0 = S_0 = 1, C_{j+1} = sum of R_{j+1} and, for kDistinct, Q_{j+1} = Q_j without its token and S_{j+1} its sum.
-struct Refused {
-  int32_t token[OPW_TREE_MAX_NODES];
-  double c[OPW_TREE_MAX_NODES];           // c_j; 0 where nothing was left: R stays
-};
-
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// R_n of token v, and its Q_n.
+// A node's distribution after n of its branches were refused, without a division per token.  With R_0 = r_0 and C_0 = S_0 = 1,
+//     R_{j+1} = max(R_j - c_j Q_j, 0),   c_j = C_j / S_j,   C_{j+1} = sum of R_{j+1},   r_j = R_j / C_j,   q_j = Q_j / S_j,
+// and as max(max(x - a, 0) - b, 0) = max(x - a - b, 0) for a, b >= 0, nearly all of it is one number, a = the sum of the c_j:
+//     kAgain     R = max(p - a q, 0)
+//     kDistinct  the same, but for the refused tokens, whose R stays what their refusal left; S = the sum of q without them
+//     kCertain   R = p, but for the refused tokens, whose R is max(R - C, 0)
+// So a refusal costs a pass over the row for the new sum (kCertain: the first at a node only), and a token a product and a sum however many were
+// refused.
+struct Refused {                          // tokens refused at this node, each once
+  int32_t token[OPW_TREE_MAX_NODES];
+  float p[OPW_TREE_MAX_NODES], q[OPW_TREE_MAX_NODES];
+  double r[OPW_TREE_MAX_NODES];           // what is left of them
+};
 template <Draw kDraw>
-__device__ __forceinline__ double left_of(int32_t v, float p32, float q32, const Refused& f, int n, double& q) {
-  double r = (double)fmaxf(p32, 0.f);     // (a NaN counts as 0)
-  q = kDraw == kCertain ? 0.0 : (double)fmaxf(q32, 0.f);
-  for (int j = 0; j < n; ++j) {
-    const bool same = kDraw != kAgain && f.token[j] == v;
-    const double c = f.c[j];
-    if (c > 0.0) r = fmax(r - c * (kDraw == kCertain ? (same ? 1.0 : 0.0) : q), 0.0);
-    if (kDraw == kDistinct && same) q = 0.0;
-  }
-  return r;
+__device__ __forceinline__ double left_of(float p, float q, double a) {
+  const double r = (double)fmaxf(p, 0.f); // (negative and NaN: 0)
+  return kDraw == kCertain ? r : fmax(fma(-a, (double)fmaxf(q, 0.f), r), 0.0);
 }
 
 // The 16-byte word at token v of a row, 0 for what lies outside of the row.
 template <typename T>
-struct Lane {
+struct Word {
   static constexpr int kN = 16 / sizeof(T);
-  float x[kN];
+  T x[kN];
   __device__ __forceinline__ void load(const T* row, int v, int vocab, bool wide) {
     if (wide && v >= 0 && v + kN <= vocab) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + v));
-      const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-      for (int i = 0; i < kN; ++i) x[i] = to_float(e[i]);
+      *reinterpret_cast<uint4*>(x) = __ldg(reinterpret_cast<const uint4*>(row + v));
     } else {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) x[i] = v + i >= 0 && v + i < vocab ? to_float(row[v + i]) : 0.f;
+      for (int i = 0; i < kN; ++i) x[i] = v + i >= 0 && v + i < vocab ? row[v + i] : T(0.f);
     }
   }
 };
 
-// A cluster per sequence; its blocks decide alike and share the rows of the vocabulary.
+// A cluster per sequence; its blocks decide alike and share the rows of the vocabulary, a contiguous part a warp.
 //
 // What decides is scalar: the target's and the drafter's probability of each node's token, gathered at the start in one round trip.
-// Only a refusal needs a whole row (the total of what it leaves), and the token that follows: the smallest v at which the running sum
-// of what is left passes u * total.  A pass leaves the sums of each warp's contiguous part of the row, and the part that holds
-// v is then read again, so that a sequence reads a row (target and drafter) once for each refusal, or once if there was none.
+// Only a refusal needs a row's sum, and the token that follows: the smallest v at which the running sum of R passes u * total.  The
+// sums of the warps' parts say which part holds v, and its block reads that part again, a word a thread.
 // All sums are in 64 bits, so that the token does not depend on how a row is split but for differences of 1e-16.
 template <typename T, Draw kDraw>
-__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Params p) {
-  constexpr int kN = Lane<T>::kN, kStep = 32 * kN;
+__global__ void __launch_bounds__(kThreads, 3) verify_kernel(const Params p) {
+  constexpr int kN = Word<T>::kN, kStep = 32 * kN, kDeep = 4;
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ int32_t token_s[OPW_TREE_MAX_NODES], parent_s[OPW_TREE_MAX_NODES];
   __shared__ float u_s[OPW_TREE_MAX_NODES], p_s[OPW_TREE_MAX_NODES], q_s[OPW_TREE_MAX_NODES];
   __shared__ Refused refused;
-  __shared__ double sum_s[kWarps], rest_s[kWarps];
-  __shared__ double2 total_s[2];          // of the block: what is left, what remains of the proposal; two in turn
+  __shared__ double sum_s[kWarps], rest_s[kWarps], part_s[kMaxCluster + kWarps];
+  __shared__ double2 total_s[2];          // of the block: sums of R (of all tokens by the formula) and of q; two in turn
+  __shared__ int32_t pick_s, some_s;
   const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int b = blockIdx.x / blocks, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
-  int t = p.tree_lens[b];
+  const int64_t row0 = (int64_t)b * p.nodes;
   const bool lead = rank == 0 && tid == 0;
+  int x0 = 0, up0 = -1;
+  float u0 = 0.f;
+  if (tid < p.nodes) {                    // (one round trip with the length)
+    x0 = p.tokens[row0 + tid];
+    up0 = p.parents[row0 + tid];
+    u0 = p.uniforms[row0 + tid];
+  }
+  int t = p.tree_lens[b];
   if (t > p.nodes) {
     t = p.nodes;
     if (lead) atomicOr(p.status, kErrBadPage);
   }
-  const int64_t row0 = (int64_t)b * p.nodes;
   if (t <= 0) {                           // (the same for the whole cluster)
     if (rank == 0 && tid < p.nodes) p.path[row0 + tid] = -1;
     if (lead) {
@@ -115,49 +116,60 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Params p) {
   const T* target = static_cast<const T*>(p.target) + row0 * p.target_stride;
   const T* draft = kDraw == kCertain ? nullptr : static_cast<const T*>(p.draft) + row0 * p.draft_stride;
   if (tid < t) {
-    const int x = tid ? p.tokens[row0 + tid] : 0, up = tid ? p.parents[row0 + tid] : -1;
-    const bool ok = tid == 0 || (x >= 0 && x < p.vocab && up >= 0 && up < tid);
-    if (!ok && rank == 0) atomicOr(p.status, kErrBadPage);
-    token_s[tid] = x;
-    parent_s[tid] = ok ? up : -1;         // a node that hangs nowhere is never asked for
-    u_s[tid] = p.uniforms[row0 + tid];
-    p_s[tid] = ok && tid ? to_float(target[up * p.target_stride + x]) : 0.f;
-    q_s[tid] = ok && tid && kDraw != kCertain ? to_float(draft[up * p.draft_stride + x]) : 0.f;
+    const bool ok = tid > 0 && x0 >= 0 && x0 < p.vocab && up0 >= 0 && up0 < tid;
+    if (tid > 0 && !ok && rank == 0) atomicOr(p.status, kErrBadPage);
+    token_s[tid] = x0;
+    parent_s[tid] = ok ? up0 : -1;        // a node that hangs nowhere is never asked for
+    u_s[tid] = u0;
+    p_s[tid] = ok ? to_float(target[up0 * p.target_stride + x0]) : 0.f;
+    q_s[tid] = kDraw == kCertain ? 1.f : ok ? to_float(draft[up0 * p.draft_stride + x0]) : 0.f;
   }
   if (rank == 0 && tid < p.nodes) p.path[row0 + tid] = tid == 0 ? 0 : -1;
+  if (tid == 0) {
+    pick_s = INT32_MAX;
+    some_s = -1;
+  }
   __syncthreads();
 
-  int turn = 0, now = 0, took = 1, n = 0; // node, length of the path, refusals at this node
+  int turn = 0, now = 0, took = 1, n = 0; // node, length of the path, tokens refused at this node
   const T* prow = target;
   const T* qrow = draft;
-  int first = 0, last = 0;                // this warp's part of the row, from where the row's 16-byte words begin (at or before token 0)
-  bool wide = false;                      // the two rows' words begin at the same tokens
+  bool wide = false;                      // the two rows' 16-byte words begin at the same tokens
+  int shift = 0;                          // tokens from where the row's first word begins to token 0
+  int64_t steps = 0;
   auto at_node = [&](int i) {
     prow = target + i * p.target_stride;
     qrow = kDraw == kCertain ? prow : draft + i * p.draft_stride;
     wide = ((uintptr_t)prow - (uintptr_t)qrow) % 16 == 0;
-    const int shift = wide ? (int)((uintptr_t)prow % 16 / sizeof(T)) : 0;
-    const int64_t parts = (int64_t)blocks * kWarps, steps = ((int64_t)p.vocab + shift + kStep - 1) / kStep, w = (int64_t)rank * kWarps + warp;
-    first = (int)(steps * w / parts * kStep) - shift;
-    last = (int)(steps * (w + 1) / parts * kStep) - shift;
+    shift = wide ? (int)((uintptr_t)prow % 16 / sizeof(T)) : 0;
+    steps = ((int64_t)p.vocab + shift + kStep - 1) / kStep;
+  };
+  auto begin_of = [&](int block, int w) { // of a warp's part of the row
+    return (int)(steps * ((int64_t)block * kWarps + w) / ((int64_t)blocks * kWarps) * kStep) - shift;
   };
   at_node(0);
-  // sums over the vocabulary of R_n and Q_n: this block's warps' of R_n in sum_s, and the totals
-  auto pass = [&](int n) -> double2 {
+  // sums over the vocabulary by the formula: this block's warps' in sum_s, the totals of R and q
+  auto pass = [&](double a, bool needs_q) -> double2 {
     double sum = 0.0, rest = 0.0;
-    const bool needs_q = kDraw != kCertain && n > 0;
-#pragma unroll 2
-    for (int v0 = first; v0 < last; v0 += kStep) {
-      const int v = v0 + lane * kN;
-      Lane<T> a, c;
-      a.load(prow, v, p.vocab, wide);
-      if (needs_q) c.load(qrow, v, p.vocab, wide);
+    const int first = begin_of(rank, warp), last = begin_of(rank, warp + 1);
+    for (int v0 = first + lane * kN; v0 < last; v0 += kDeep * kStep) {
+      Word<T> x[kDeep], y[kDeep];
 #pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        double q;
-        sum += left_of<kDraw>(v + i, a.x[i], needs_q ? c.x[i] : 0.f, refused, n, q);
-        if (kDraw == kDistinct) rest += q;
-      }
+      for (int k = 0; k < kDeep; ++k)
+        if (v0 + k * kStep < last) {
+          x[k].load(prow, v0 + k * kStep, p.vocab, wide);
+          if (needs_q) y[k].load(qrow, v0 + k * kStep, p.vocab, wide);
+        }
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k)
+        if (v0 + k * kStep < last) {
+#pragma unroll
+          for (int i = 0; i < kN; ++i) {
+            const float q = needs_q ? to_float(y[k].x[i]) : 0.f;
+            sum += left_of<kDraw>(to_float(x[k].x[i]), q, a);
+            if (kDraw == kDistinct) rest += (double)fmaxf(q, 0.f);
+          }
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -187,87 +199,135 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Params p) {
     ++turn;
     return all;
   };
+  // what the list adds to the sum of the tokens [from, to) by the formula
+  auto correction = [&](double a, int from, int to) {
+    double d = 0.0;
+    if (kDraw != kAgain)
+      for (int j = 0; j < n; ++j)
+        if (refused.token[j] >= from && refused.token[j] < to) d += refused.r[j] - left_of<kDraw>(refused.p[j], refused.q[j], a);
+    return d;
+  };
 
-  bool at_hand = false;                   // the sums in shared memory are those of R_n
-  double total = 1.0, q_total = 1.0;      // C_n, S_n
+  bool at_hand = false;                   // the sums in shared memory are those of R by the formula with this a
+  double a = 0.0, c_total = 1.0, s_total = 1.0;
+  double raw = 0.0;                       // kCertain: the row's sum, once it is known
   for (int i = 1; i < t; ++i) {
     if (parent_s[i] != now) continue;
-    double q;
     const int32_t x = token_s[i];
-    const double r = left_of<kDraw>(x, p_s[i], q_s[i], refused, n, q);
-    if (kDraw == kCertain) q = 1.0;
-    if ((double)u_s[i] * q * total < r * q_total) {
+    int listed = -1;                      // its place in the list
+    if (kDraw != kAgain && n > 0) {
+      const uint32_t lo = __ballot_sync(0xffffffffu, lane < n && refused.token[lane] == x);
+      const uint32_t hi = n > 32 ? __ballot_sync(0xffffffffu, lane + 32 < n && refused.token[(lane + 32) & 63] == x) : 0u;
+      listed = lo ? __ffs(lo) - 1 : hi ? __ffs(hi) + 31 : -1;
+    }
+    const double r = listed >= 0 ? refused.r[listed] : left_of<kDraw>(p_s[i], q_s[i], a);
+    const double q = kDraw == kCertain ? 1.0 : listed >= 0 ? 0.0 : (double)fmaxf(q_s[i], 0.f);
+    if ((double)u_s[i] * q * c_total < r * s_total) {
       if (lead) p.path[row0 + took] = i;
       now = i;
       ++took;
       n = 0;
-      total = q_total = 1.0;
+      a = 0.0;
+      c_total = s_total = 1.0;
       at_hand = false;
       at_node(now);
       continue;
     }
-    __syncthreads();                      // everybody has read the list
-    if (tid == 0) {
-      refused.token[n] = x;
-      refused.c[n] = total / q_total;
-    }
-    __syncthreads();
-    const double2 all = pass(++n);
-    at_hand = all.x > 0.0;
-    if (at_hand) total = all.x;
-    else {                                // (every thread has left the pass: its last barrier is behind the reads of the list)
-      if (tid == 0) refused.c[n - 1] = 0.0;
+    const double c = c_total / s_total;
+    double next = a;
+    if (kDraw != kCertain) next += c;
+    if (kDraw != kAgain) {
+      __syncthreads();                    // everybody has read the list
+      if (listed < 0) listed = n++;
+      if (tid == 0) {
+        refused.token[listed] = x;
+        refused.p[listed] = p_s[i];
+        refused.q[listed] = q_s[i];
+        refused.r[listed] = fmax(r - c * q, 0.0);
+      }
       __syncthreads();
     }
-    if (kDraw == kDistinct) q_total = all.y > 0.0 ? all.y : 1.0;   // (Q is 0 everywhere then)
-  }
-  if (!at_hand) total = pass(n).x;
-
-  // the token that follows: block, warp, step, lane, element of the first running sum above u * total; if rounding leaves none, the last
-  // element that has anything.  (One warp ends up here.)
-  const double limit = (double)fmaxf(u_s[0], 0.f) * total;
-  double before = 0.0, at = 0.0;
-  int found = -1;
-  for (int k = 0; k < blocks; ++k) {
-    const double s = cluster.map_shared_rank(&total_s[(turn - 1) & 1], k)->x;
-    if (s > 0.0) {
-      found = k;
-      before = at;
-      if (at + s > limit) break;
+    double2 all;
+    if (kDraw == kCertain && at_hand) all.x = raw;
+    else all = pass(next, kDraw != kCertain);
+    if (kDraw == kCertain) raw = all.x;
+    const double left = all.x + correction(next, 0, p.vocab);
+    if (left > 0.0) {
+      a = next;
+      c_total = left;
+      at_hand = true;
+    } else {                              // nothing would be left: R stays
+      at_hand = kDraw == kCertain;
+      if (kDraw != kAgain) {
+        __syncthreads();
+        if (tid == 0) refused.r[listed] = r;
+        __syncthreads();
+      }
     }
-    at += s;
+    if (kDraw == kDistinct) {
+      s_total = all.y;
+      for (int j = 0; j < n; ++j) s_total -= (double)fmaxf(refused.q[j], 0.f);
+      if (!(s_total > 0.0)) s_total = 1.0;                        // (Q is 0 everywhere then)
+    }
   }
-  cluster.sync();                         // nobody leaves while its sums are read
+  const bool needs_q = kDraw != kCertain && a > 0.0;
+  if (!at_hand) raw = pass(a, needs_q).x;
+  else if (kDraw != kCertain) raw = 0.0;
+  const double total = at_hand && kDraw != kCertain ? c_total : raw + correction(a, 0, p.vocab);
+
+  // The token that follows: block, warp, thread, element of the first running sum above u * total; if rounding leaves none, the last
+  // element that has anything.
+  if (tid < blocks) part_s[tid] = cluster.map_shared_rank(&total_s[(turn - 1) & 1], tid)->x + correction(a, begin_of(tid, 0), begin_of(tid + 1, 0));
+  else if (tid >= 32 && tid < 32 + kWarps)
+    part_s[kMaxCluster + tid - 32] = sum_s[tid - 32] + correction(a, begin_of(rank, tid - 32), begin_of(rank, tid - 31));
+  cluster.sync();                         // (nobody leaves while its sums are read)
+  const double limit = (double)fmaxf(u_s[0], 0.f) * total;
+  double at = 0.0;
+  auto choose = [&](const double* part, int count) {              // the part that holds it; `at` becomes the sum before
+    int found = -1;
+    double before = at;
+    for (int k = 0; k < count; ++k) {
+      const double s = part[k];
+      if (s > 0.0) {
+        found = k;
+        before = at;
+        if (at + s > limit) break;
+        at += s;
+      }
+    }
+    at = before;
+    return found;
+  };
+  const int block = choose(part_s, blocks);
   if (lead) {
     p.path_lens[b] = took;
-    if (found < 0) p.next_tokens[b] = -1;
+    if (block < 0) p.next_tokens[b] = -1;
   }
-  if (found != rank) return;
-  int mine = -1;
-  at = before;
-  for (int w = 0; w < kWarps; ++w) {
-    const double s = sum_s[w];
-    if (s > 0.0) {
-      mine = w;
-      before = at;
-      if (at + s > limit) break;
-    }
-    at += s;
+  if (block != rank) return;
+  const int w = choose(part_s + kMaxCluster, kWarps);
+  if (w < 0) {                            // (rounding: the block's sum was next to nothing)
+    if (tid == 0) p.next_tokens[b] = -1;
+    return;
   }
-  if (mine != warp) return;
-  int32_t best = -1;                      // the last element with anything, so far
-  at = before;
-  const bool needs_q = kDraw != kCertain && n > 0;
-  for (int v0 = first; v0 < last; v0 += kStep) {
-    const int v = v0 + lane * kN;
-    Lane<T> a, c;
-    a.load(prow, v, p.vocab, wide);
-    if (needs_q) c.load(qrow, v, p.vocab, wide);
-    double r[kN], sum = 0.0, q;
+  const int first = begin_of(rank, w), last = begin_of(rank, w + 1);
+  for (int v0 = first; v0 < last; v0 += kThreads * kN) {
+    const int v = v0 + tid * kN;
+    double r[kN], sum = 0.0;
+    if (v < last) {
+      Word<T> x, y;
+      x.load(prow, v, p.vocab, wide);
+      if (needs_q) y.load(qrow, v, p.vocab, wide);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      r[i] = left_of<kDraw>(v + i, a.x[i], needs_q ? c.x[i] : 0.f, refused, n, q);
-      sum += r[i];
+      for (int i = 0; i < kN; ++i) r[i] = left_of<kDraw>(to_float(x.x[i]), needs_q ? to_float(y.x[i]) : 0.f, a);
+      if (kDraw != kAgain)
+        for (int j = 0; j < n; ++j) {
+          const int e = refused.token[j] - v;
+#pragma unroll
+          for (int i = 0; i < kN; ++i)
+            if (e == i) r[i] = refused.r[j];
+        }
+#pragma unroll
+      for (int i = 0; i < kN; ++i) sum += r[i];
     }
     double incl = sum;
 #pragma unroll
@@ -275,22 +335,29 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Params p) {
       const double y = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += y;
     }
-    const uint32_t over = __ballot_sync(0xffffffffu, at + incl > limit && sum > 0.0), some = __ballot_sync(0xffffffffu, sum > 0.0);
-    if (some) {
-      const int who = over ? __ffs(over) - 1 : 31 - __clz(some);
-      int32_t pick = -1;
-      double run = at + incl - sum;
+    if (lane == 31) sum_s[warp] = incl;
+    __syncthreads();
+    double run = at;
+    for (int k = 0; k < warp; ++k) run += sum_s[k];
+    for (int k = 0; k < kWarps; ++k) at += sum_s[k];
+    run += incl - sum;
+    if (sum > 0.0) {
+      int pick = -1, some = -1;
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        if (r[i] > 0.0 && !(pick >= 0 && over && run > limit)) pick = v + i;
         run += r[i];
+        if (r[i] > 0.0) {
+          some = v + i;
+          if (pick < 0 && run > limit) pick = v + i;
+        }
       }
-      best = __shfl_sync(0xffffffffu, pick, who);
+      if (pick >= 0) atomicMin(&pick_s, pick);
+      atomicMax(&some_s, some);
     }
-    if (over) break;
-    at += __shfl_sync(0xffffffffu, incl, 31);
+    __syncthreads();
+    if (pick_s != INT32_MAX) break;
   }
-  if (lane == 0) p.next_tokens[b] = best;
+  if (tid == 0) p.next_tokens[b] = pick_s != INT32_MAX ? pick_s : some_s;
 }
 
 template <typename T>
