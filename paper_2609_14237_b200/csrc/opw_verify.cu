@@ -16,7 +16,7 @@ using opw_words::pdl_wait;
 
 constexpr uint32_t kErrBadPage = 1u;      // bit of the stage's status word
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;         // (above 8 a cluster size has to be allowed)
 
 struct Params {
   const void* target;
@@ -57,14 +57,20 @@ __device__ __forceinline__ double left_of(float p, float q, double a) {
   return kDraw == kCertain ? r : fmax(fma(-a, (double)fmaxf(q, 0.f), r), 0.0);
 }
 
+template <bool X>
+struct Flag {
+  static constexpr bool value = X;
+};
+
 // The 16-byte word at token v of a row, 0 for what lies outside of the row.
 template <typename T>
-struct Word {
+struct alignas(16) Word {
   static constexpr int kN = 16 / sizeof(T);
   T x[kN];
+  __device__ __forceinline__ void load_inside(const T* row, int v) { *reinterpret_cast<uint4*>(x) = __ldg(reinterpret_cast<const uint4*>(row + v)); }
   __device__ __forceinline__ void load(const T* row, int v, int vocab, bool wide) {
     if (wide && v >= 0 && v + kN <= vocab) {
-      *reinterpret_cast<uint4*>(x) = __ldg(reinterpret_cast<const uint4*>(row + v));
+      load_inside(row, v);
     } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) x[i] = v + i >= 0 && v + i < vocab ? row[v + i] : T(0.f);
@@ -79,7 +85,7 @@ struct Word {
 // sums of the warps' parts say which part holds v, and its block reads that part again, a word a thread.
 // All sums are in 64 bits, so that the token does not depend on how a row is split but for differences of 1e-16.
 template <typename T, Draw kDraw>
-__global__ void __launch_bounds__(kThreads, 3) verify_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_kernel(const Params p) {
   constexpr int kN = Word<T>::kN, kStep = 32 * kN, kDeep = 4;
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ int32_t token_s[OPW_TREE_MAX_NODES], parent_s[OPW_TREE_MAX_NODES];
@@ -150,27 +156,48 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const Params p) {
   at_node(0);
   // sums over the vocabulary by the formula: this block's warps' in sum_s, the totals of R and q
   auto pass = [&](double a, bool needs_q) -> double2 {
-    double sum = 0.0, rest = 0.0;
     const int first = begin_of(rank, warp), last = begin_of(rank, warp + 1);
-    for (int v0 = first + lane * kN; v0 < last; v0 += kDeep * kStep) {
-      Word<T> x[kDeep], y[kDeep];
+    // (four sums side by side: one would be a chain of 64-bit additions)
+    double sums[4] = {0.0, 0.0, 0.0, 0.0}, rests[4] = {0.0, 0.0, 0.0, 0.0};
+    auto add = [&](const Word<T>& x, const Word<T>& y, bool with_q) {
 #pragma unroll
-      for (int k = 0; k < kDeep; ++k)
-        if (v0 + k * kStep < last) {
-          x[k].load(prow, v0 + k * kStep, p.vocab, wide);
-          if (needs_q) y[k].load(qrow, v0 + k * kStep, p.vocab, wide);
+      for (int i = 0; i < kN; ++i) {
+        const double pd = (double)fmaxf(to_float(x.x[i]), 0.f);
+        if (kDraw == kCertain || !with_q) {
+          sums[i & 3] += pd;
+        } else {
+          const double qd = (double)fmaxf(to_float(y.x[i]), 0.f), r = fma(-a, qd, pd);
+          if (r > 0.0) sums[i & 3] += r;
+          if (kDraw == kDistinct) rests[i & 3] += qd;
         }
+      }
+    };
+    auto walk = [&](auto with_q) {
+      constexpr bool kQ = decltype(with_q)::value;
+      const int inside = min(last, p.vocab);
+      for (int v0 = first; v0 < last;) {
+        if (wide && v0 >= 0 && v0 + kDeep * kStep <= inside) {    // whole words, kDeep of a row in flight
+          Word<T> x[kDeep], y[kDeep];
 #pragma unroll
-      for (int k = 0; k < kDeep; ++k)
-        if (v0 + k * kStep < last) {
-#pragma unroll
-          for (int i = 0; i < kN; ++i) {
-            const float q = needs_q ? to_float(y[k].x[i]) : 0.f;
-            sum += left_of<kDraw>(to_float(x[k].x[i]), q, a);
-            if (kDraw == kDistinct) rest += (double)fmaxf(q, 0.f);
+          for (int k = 0; k < kDeep; ++k) {
+            x[k].load_inside(prow, v0 + k * kStep + lane * kN);
+            if (kQ) y[k].load_inside(qrow, v0 + k * kStep + lane * kN);
           }
+#pragma unroll
+          for (int k = 0; k < kDeep; ++k) add(x[k], y[k], kQ);
+          v0 += kDeep * kStep;
+        } else {
+          Word<T> x, y;
+          x.load(prow, v0 + lane * kN, p.vocab, wide);
+          if (kQ) y.load(qrow, v0 + lane * kN, p.vocab, wide);
+          add(x, y, kQ);
+          v0 += kStep;
         }
-    }
+      }
+    };
+    if (needs_q) walk(Flag<true>{});
+    else walk(Flag<false>{});
+    double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]), rest = (rests[0] + rests[1]) + (rests[2] + rests[3]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -360,12 +387,19 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const Params p) {
   if (tid == 0) p.next_tokens[b] = pick_s != INT32_MAX ? pick_s : some_s;
 }
 
+template <typename T, Draw kDraw>
+cudaError_t launch_as(const opw_stage_view& s, const Params& p, int batch, int cluster, cudaStream_t stream) {
+  if (cluster > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(verify_kernel<T, kDraw>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  return opw_launch(verify_kernel<T, kDraw>, dim3((unsigned)batch * cluster), dim3(kThreads), 0, stream, s.pdl, cluster, p);
+}
 template <typename T>
 cudaError_t launch(const opw_stage_view& s, const Params& p, int draw, int batch, int cluster, cudaStream_t stream) {
-  const dim3 grid((unsigned)batch * cluster), block(kThreads);
-  if (draw == kAgain) return opw_launch(verify_kernel<T, kAgain>, grid, block, 0, stream, s.pdl, cluster, p);
-  if (draw == kDistinct) return opw_launch(verify_kernel<T, kDistinct>, grid, block, 0, stream, s.pdl, cluster, p);
-  return opw_launch(verify_kernel<T, kCertain>, grid, block, 0, stream, s.pdl, cluster, p);
+  return draw == kAgain      ? launch_as<T, kAgain>(s, p, batch, cluster, stream)
+         : draw == kDistinct ? launch_as<T, kDistinct>(s, p, batch, cluster, stream)
+                             : launch_as<T, kCertain>(s, p, batch, cluster, stream);
 }
 
 }  // namespace opw_verify
@@ -414,9 +448,11 @@ extern "C" opw_status_t opw_tree_verify(opw_attn_stage_t* stage, int32_t batch, 
   p.draft_stride = draft_stride;
   p.nodes = nodes;
   p.vocab = vocab;
-  // Blocks per sequence: as many as fit the chip twice over, and no more than give every warp a step.
+  // Blocks per sequence: as many as are resident at once, four an SM, and no more than give every warp four steps of a row.  fp32, us with
+  // 1, 2, 4, 8 and 16 blocks: 1 tree of 64 over 150000 tokens 91, 55, 34, 24, 20; 16 trees of 8 over 131072 108, 59, 35, 23, 19; 64 of them
+  // 128, 72, 44, 31, 37; 256 chains of 4, drafted by a rule, 48, 36, 37, 44, 77; a chain of 4 over 32000 11.4, 8.5, 6.9, 6.4, 6.6.
   int cluster = 1;
-  while (cluster < opw_verify::kMaxCluster && (int64_t)batch * cluster * 2 <= 2 * s.sms && vocab > cluster * opw_verify::kWarps * 128) cluster *= 2;
+  while (cluster < opw_verify::kMaxCluster && (int64_t)batch * cluster * 2 <= 4 * s.sms && vocab > cluster * opw_verify::kWarps * 4 * 128) cluster *= 2;
   opw_device_guard guard(s.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
