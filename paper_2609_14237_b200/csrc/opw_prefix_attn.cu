@@ -42,46 +42,61 @@ PrefixLayout carve(const opw_stage_view& v) {
 }
 
 // Who takes the groups: with more than 16 rows (members x query heads of a kv head) in a group, on average, the tensor cores, in blocks of up
-// to 128 or of up to 256 rows; else, and at head_dim 256 where two accumulators would fill TMEM, the warp kernel's 16 rows.
+// to 128 or of up to 256 rows; else, and at head_dim 256 where two accumulators would fill TMEM, the warp kernel's 16 rows.  Measured, us, by the
+// warp kernel, with 128 and with 256 rows; 32/8 heads of 128 unless said:
+//   8 x 4 samples behind 4k, 16 rows   46, 48, 49        64 behind 8k (256 rows)                  98, 49, 58
+//   32 pairs behind 2k, 8 rows         78, 87, 88        64 behind 8k, 64/8 heads (512 rows)     156, 57, 57
+//   4 samples of 1000, 16 rows         14, 17, 18        256 behind 32k (1024 rows)             1053, 205, 182
 int mode_of(const opw_stage_view& v, int batch, int groups) {
   const int64_t rows = (int64_t)batch * (v.Hq / v.Hkv);
   if (v.D == 256 || rows <= 16 * (int64_t)groups) return kPrefixWarp;
-  return rows <= 128 * (int64_t)groups ? kPrefixNarrow : kPrefixWide;
+  return rows < 512 * (int64_t)groups ? kPrefixNarrow : kPrefixWide;
 }
 
-template <int D, int kMode>
+template <int D, int kMode, bool kHigh>
 cudaError_t raise_smem() {
-  return cudaFuncSetAttribute(prefix_kernel<D, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)PrefixSmem<D, kMode>::bytes(kMaxPrefixBatch, kMaxPrefixGroups));
+  return cudaFuncSetAttribute(prefix_kernel<D, kMode, kHigh>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)PrefixSmem<D, kMode, kHigh>::kMost);
 }
 template <int D>
-cudaError_t raise_all() {
-  cudaError_t e = raise_smem<D, kPrefixWarp>();
+cudaError_t raise_all(bool high) {
+  cudaError_t e = raise_smem<D, kPrefixWarp, true>();
   if constexpr (D != 256) {
-    if (e == cudaSuccess) e = raise_smem<D, kPrefixNarrow>();
-    if (e == cudaSuccess) e = raise_smem<D, kPrefixWide>();
+    if (e == cudaSuccess) e = high ? raise_smem<D, kPrefixNarrow, true>() : raise_smem<D, kPrefixNarrow, false>();
+    if (e == cudaSuccess) e = high ? raise_smem<D, kPrefixWide, true>() : raise_smem<D, kPrefixWide, false>();
   }
   return e;
 }
 
-template <int D, int kMode>
-cudaError_t launch(const opw_stage_view& v, const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream) {
-  using S = PrefixSmem<D, kMode>;
-  cudaError_t e = opw_launch(prefix_kernel<D, kMode>, dim3(v.sms), dim3(S::kThreads), S::bytes(p.batch, p.groups), stream, v.pdl, 1, map, p);
+template <int D, int kMode, bool kHigh>
+cudaError_t launch(const opw_stage_view& v, const CUtensorMap& map, const PrefixParams& group_problem, const PrefixParams& p, cudaStream_t stream) {
+  PrefixProblem<kGroupEnds> groups;
+  PrefixProblem<kRowEnds> rows;
+  static_cast<PrefixParams&>(groups) = group_problem;
+  static_cast<PrefixParams&>(rows) = p;
+  rows.lead = kMode == kPrefixWarp ? p.groups : 0;
+  rows.all = rows.lead + p.batch;
+  using S = PrefixSmem<D, kMode, kHigh>;
+  rows.stages = S::stages(p.batch, p.groups);
+  cudaError_t e = opw_launch(prefix_kernel<D, kMode, kHigh>, dim3(v.sms), dim3(S::kThreads), S::bytes(p.batch, p.groups, rows.stages), stream, v.pdl, 1, map, groups, rows);
   if (e != cudaSuccess) return e;
   *v.launches += 1;
-  const int64_t rows = (int64_t)p.batch * p.Hq, per = kPrefixCombineThreads / 32;
-  e = opw_launch(prefix_combine_kernel<D, kMode>, dim3((unsigned)((rows + per - 1) / per)), dim3(kPrefixCombineThreads), 0, stream, v.pdl, 1, p);
+  const int64_t n = (int64_t)p.batch * p.Hq, per = kPrefixCombineThreads / 32;
+  const dim3 block(kPrefixCombineThreads);
+  e = n < 4 * (int64_t)v.sms
+          ? opw_launch(prefix_combine_kernel<D, kMode, kHigh, 4>, dim3((unsigned)n), block, 0, stream, v.pdl, 1, groups, rows)
+          : opw_launch(prefix_combine_kernel<D, kMode, kHigh, 1>, dim3((unsigned)((n + per - 1) / per)), block, 0, stream, v.pdl, 1, groups, rows);
   if (e == cudaSuccess) *v.launches += 1;
   return e;
 }
 template <int D>
-cudaError_t launch(const opw_stage_view& v, int mode, const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream) {
+cudaError_t launch(const opw_stage_view& v, int mode, const CUtensorMap& map, const PrefixParams& g, const PrefixParams& p, cudaStream_t stream) {
   if constexpr (D != 256) {
-    if (mode == kPrefixNarrow) return launch<D, kPrefixNarrow>(v, map, p, stream);
-    if (mode == kPrefixWide) return launch<D, kPrefixWide>(v, map, p, stream);
+    const bool high = p.G > 8;
+    if (mode == kPrefixNarrow) return high ? launch<D, kPrefixNarrow, true>(v, map, g, p, stream) : launch<D, kPrefixNarrow, false>(v, map, g, p, stream);
+    if (mode == kPrefixWide) return high ? launch<D, kPrefixWide, true>(v, map, g, p, stream) : launch<D, kPrefixWide, false>(v, map, g, p, stream);
   }
-  return launch<D, kPrefixWarp>(v, map, p, stream);
+  return launch<D, kPrefixWarp, true>(v, map, g, p, stream);
 }
 
 }  // namespace
@@ -108,7 +123,7 @@ extern "C" opw_status_t opw_prefix_attn_create(opw_attn_stage_t* stage, uint32_t
   if (workspace_bytes < lay.total) return OPW_ERR_CAPACITY;
   opw_device_guard guard(v.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
-  const cudaError_t e = v.D == 64 ? raise_all<64>() : v.D == 128 ? raise_all<128>() : raise_all<256>();
+  const cudaError_t e = v.D == 64 ? raise_all<64>(v.Hq / v.Hkv > 8) : v.D == 128 ? raise_all<128>(v.Hq / v.Hkv > 8) : raise_all<256>(false);
   if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   opw_prefix_attn* t = new (std::nothrow) opw_prefix_attn();
   if (!t) return OPW_ERR_INVALID_ARG;
@@ -160,11 +175,9 @@ extern "C" opw_status_t opw_prefix_attention(opw_prefix_attn_t* prefix, int32_t 
   p.out = static_cast<__nv_bfloat16*>(out);
   p.lse = lse;
   const PrefixLayout& lay = prefix->lay;
-  p.group_parts = reinterpret_cast<float*>(prefix->ws + lay.group_parts);
-  p.row_parts = reinterpret_cast<float*>(prefix->ws + lay.row_parts);
+  p.partials = reinterpret_cast<float*>(prefix->ws + lay.row_parts);
+  p.cum = reinterpret_cast<int64_t*>(prefix->ws + lay.row_cum);
   p.whole = reinterpret_cast<float*>(prefix->ws + lay.whole);
-  p.group_cum = reinterpret_cast<int64_t*>(prefix->ws + lay.group_cum);
-  p.row_cum = reinterpret_cast<int64_t*>(prefix->ws + lay.row_cum);
   p.info = reinterpret_cast<GroupInfo*>(prefix->ws + lay.info);
   p.split = reinterpret_cast<PrefixSplit*>(prefix->ws + lay.split);
   p.status = v.status;
@@ -178,15 +191,20 @@ extern "C" opw_status_t opw_prefix_attention(opw_prefix_attn_t* prefix, int32_t 
   p.max_pages = v.max_pages;
   p.window = v.window[layer];
   p.scale_log2e = v.scale_log2e;
+  p.lead = p.all = p.stages = 0;             // (with the launch)
+  PrefixParams groups_problem = p;
+  groups_problem.partials = reinterpret_cast<float*>(prefix->ws + lay.group_parts);
+  groups_problem.cum = reinterpret_cast<int64_t*>(prefix->ws + lay.group_cum);
+  groups_problem.lead = groups_problem.all = groups;
   opw_device_guard guard(v.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int mode = mode_of(v, batch, groups);
   static const CUtensorMap none = {};
   const CUtensorMap& map = prefix->maps.empty() ? none : prefix->maps[layer];
-  const cudaError_t e = v.D == 64    ? launch<64>(v, mode, map, p, stream)
-                        : v.D == 128 ? launch<128>(v, mode, map, p, stream)
-                                     : launch<256>(v, mode, map, p, stream);
+  const cudaError_t e = v.D == 64    ? launch<64>(v, mode, map, groups_problem, p, stream)
+                        : v.D == 128 ? launch<128>(v, mode, map, groups_problem, p, stream)
+                                     : launch<256>(v, mode, map, groups_problem, p, stream);
   if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   return OPW_OK;
 }

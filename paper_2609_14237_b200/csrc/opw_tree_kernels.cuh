@@ -22,6 +22,8 @@ namespace opw_tree {
 constexpr int kMaxTreeBatch = 4096;
 
 struct TreeParams {
+  static constexpr int kEnds = 0;        // units that a segment (entity, kv head, row block) counts for besides its tiles, in front of them
+  static constexpr int kLeastPages = 4;  // units a worker has at least where they are pages
   const __nv_bfloat16* pool;
   const __nv_bfloat16* q;
   const uint64_t* mask;
@@ -96,7 +98,8 @@ __device__ __forceinline__ void scan_units(const Problem& p, int64_t* cum, int r
     if (b < batch) {
       const Span s = span_of(p, b, row_block);
       if (s.cut && record) atomicOr(p.status, kErrBadPage);
-      cnt = (int64_t)tiles_of(s, keys) * s.blocks * p.Hkv;
+      const int32_t tiles = tiles_of(s, keys);
+      cnt = tiles > 0 ? (int64_t)(tiles + Problem::kEnds) * s.blocks * p.Hkv : 0;
     }
     int64_t incl = cnt;
 #pragma unroll
@@ -119,8 +122,9 @@ __device__ __forceinline__ void scan_units(const Problem& p, int64_t* cum, int r
 // How many of the launched workers share U units: never more than there are units, and with single pages as units (a warp each) at least
 // four of them per worker -- a short step would otherwise leave a partial per page (63 of them at 1000 keys: the
 // combine took 110 us).
+template <class Problem>
 __device__ __forceinline__ int64_t workers_for(int64_t U, int64_t launched, int keys) {
-  const int64_t most = keys == kPage ? U / 4 : U;
+  const int64_t most = keys == kPage ? U / Problem::kLeastPages : U;
   return most < 1 ? 1 : most < launched ? most : launched;
 }
 // the sequence that holds unit u < cum[batch]
@@ -224,14 +228,15 @@ struct WarpTree {
 template <int D, int kWarps, class Problem>
 __device__ __forceinline__ void warp_body(const Problem& p, unsigned char* smem, const int64_t* cum, int block, int blocks) {
   using C = WarpTree<D>;
+  constexpr int kEnds = Problem::kEnds;
   constexpr int KS = D / 16, NT = D / 8, ROWB = D * 2, TILE = C::kTile;
-  constexpr uint32_t kFirst = 1u << 28, kLast = 1u << 29, kBad = 1u << 30, kPageBits = kFirst - 1;
+  constexpr uint32_t kFirst = 1u << 28, kLast = 1u << 29, kBad = 1u << 30, kNone = 1u << 31, kPageBits = kFirst - 1;   // kNone: no tile
   const int warps = kWarps, stages = C::kStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (size_t)warps * stages * TILE);
   const int batch = entities(p);
   const int64_t U = cum[batch];
-  const int64_t workers = workers_for(U, (int64_t)blocks * warps, kPage), worker = (int64_t)warp * blocks + block;
+  const int64_t workers = workers_for<Problem>(U, (int64_t)blocks * warps, kPage), worker = (int64_t)warp * blocks + block;
   const uint32_t ring = smem_u32(smem + (size_t)warp * stages * TILE);
   const uint32_t bar0 = smem_u32(bars + warp * stages);
   if (lane == 0) {
@@ -251,7 +256,11 @@ __device__ __forceinline__ void warp_body(const Problem& p, unsigned char* smem,
     const Span s = span_of(p, b, C::kRows);
     const int32_t cnt = tiles_of(s, kPage);
     const int64_t rem = u - cum[b];
-    const int32_t ri = (int32_t)(rem / cnt), i = (int32_t)(rem - (int64_t)ri * cnt), g = ri / s.blocks;
+    const int32_t ri = (int32_t)(rem / (cnt + kEnds)), i = (int32_t)(rem - (int64_t)ri * (cnt + kEnds)) - kEnds, g = ri / s.blocks;
+    if (kEnds > 0 && i < 0) {
+      d.page = kNone;
+      return d;
+    }
     const int32_t lp = s.lo / kPage + i;
     int64_t pid = p.page_table[(int64_t)s.table_row * p.max_pages + lp];
     d.page = (uint32_t)lp | (i == 0 ? kFirst : 0u) | (i == cnt - 1 ? kLast : 0u);
@@ -274,6 +283,13 @@ __device__ __forceinline__ void warp_body(const Problem& p, unsigned char* smem,
   auto issue = [&](int64_t u, int slot) {
     const int rel = (int)(u - wbase);
     const int32_t a = __shfl_sync(0xffffffffu, wa.tile, rel & 31), b = __shfl_sync(0xffffffffu, wb.tile, rel & 31);
+    if (kEnds > 0) {
+      const uint32_t pa = __shfl_sync(0xffffffffu, wa.page, rel & 31), pb = __shfl_sync(0xffffffffu, wb.page, rel & 31);
+      if ((rel < 32 ? pa : pb) & kNone) {     // nothing to copy: the place's barrier completes all the same
+        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar0 + 8 * slot) : "memory");
+        return;
+      }
+    }
     if (lane == 0) {
       const uint32_t bar = bar0 + 8 * slot;
       mbar_expect_tx(bar, TILE);
@@ -291,7 +307,7 @@ __device__ __forceinline__ void warp_body(const Problem& p, unsigned char* smem,
   int b = 0, g = 0, rb = 0, rows = 0;
   int32_t border = 0;
   Span sp = {0, 0, 0, 0, 1, 0, 0, false};
-  bool from_first = false, on_first_row = true, failed = false;
+  bool from_first = false, on_first_row = true, failed = false, fresh = true;
   int slot = 0;
   uint32_t phase = 0;
 
@@ -303,11 +319,22 @@ __device__ __forceinline__ void warp_body(const Problem& p, unsigned char* smem,
     }
     const uint32_t page = __shfl_sync(0xffffffffu, wa.page, (int)(u - wbase));
     const bool last = page & kLast;
-    if (u == u0 || (page & kFirst)) {         // a new row block: its queries, an empty state
+    if (kEnds > 0 && (page & kNone)) {
+      if (!mbar_wait(bar0 + 8 * slot, phase)) { failed = true; break; }
+      --inflight;
+      if (u + stages < u1) {
+        issue(u + stages, slot);
+        ++inflight;
+      }
+      if (++slot == stages) { slot = 0; phase ^= 1u; }
+      continue;
+    }
+    if (fresh || (page & kFirst)) {           // a new row block: its queries, an empty state
+      fresh = false;
       from_first = page & kFirst;
       b = find_sequence(cum, batch, u);
       sp = span_of(p, b, C::kRows);
-      const int32_t ri = (int32_t)((u - cum[b]) / tiles_of(sp, kPage));
+      const int32_t ri = (int32_t)((u - cum[b]) / (tiles_of(sp, kPage) + kEnds));
       g = ri / sp.blocks;
       rb = ri - g * sp.blocks;
       rows = sp.tree * p.G - rb * C::kRows;   // of this block; may exceed it
@@ -561,7 +588,7 @@ __global__ void __launch_bounds__(kTreeCombineThreads, V == 1 ? 1 : D == 256 ? 2
     if (p.lse && lane8 == 0) p.lse[row] = -INFINITY;
   }
   if (cnt == 0 || rb * c.row_block + (int)blockIdx.y * kRows >= live) return;   // (the same for the whole block)
-  const int64_t workers = workers_for(U, c.workers, c.keys);
+  const int64_t workers = workers_for<TreeParams>(U, c.workers, c.keys);
   const int64_t first = before + ((int64_t)g * s.blocks + rb) * cnt, end = first + cnt;
   const int64_t wf = worker_of(U, first, workers), wl = worker_of(U, end - 1, workers);
   if (wf == wl) return;                                          // finished by its worker

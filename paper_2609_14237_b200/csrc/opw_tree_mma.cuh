@@ -181,7 +181,7 @@ __device__ __forceinline__ bool mbar_wait_or_dead(uint32_t bar, uint32_t parity,
 // The row blocks of a worker's share, one after the other; every role walks the same list.
 struct Segment {
   int b, g, rb, rows;          // rows of the block that exist
-  int32_t t0, n;               // first key tile and number of tiles
+  int32_t t0, n, step;         // first key tile and number of tiles; units (0 tiles: nothing to do but to step over them)
   bool first, last;            // the block's first / last tile is among them
   bool shared;                 // both slots on every tile (more than 128 rows), or alternate tiles
   Span sp;
@@ -191,14 +191,16 @@ __device__ __forceinline__ Segment segment_at(const Problem& p, const int64_t* c
   Segment s;
   s.b = find_sequence(cum, entities(p), u);
   s.sp = span_of(p, s.b, kRows);
-  const int32_t cnt = tiles_of(s.sp, kMmaKeys);
+  constexpr int kEnds = Problem::kEnds;
+  const int32_t cnt = tiles_of(s.sp, kMmaKeys), all = cnt + kEnds;
   const int64_t rem = u - cum[s.b];
-  const int32_t ri = (int32_t)(rem / cnt);
-  s.t0 = (int32_t)(rem - (int64_t)ri * cnt);
+  const int32_t ri = (int32_t)(rem / all), at = (int32_t)(rem - (int64_t)ri * all);
+  s.t0 = kEnds > 0 ? max(at - kEnds, 0) : at;
   s.g = ri / s.sp.blocks;
   s.rb = ri - s.g * s.sp.blocks;
   s.rows = min(s.sp.tree * p.G - s.rb * kRows, kRows);
-  s.n = (int32_t)min((int64_t)(cnt - s.t0), u1 - u);
+  s.step = (int32_t)min((int64_t)(all - at), u1 - u);
+  s.n = kEnds > 0 ? max(at + s.step - kEnds - s.t0, 0) : s.step;
   s.first = s.t0 == 0;
   s.last = s.t0 + s.n == cnt;
   s.shared = kRows > 128 && s.rows > 128;
@@ -250,7 +252,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
   tc_after();
   constexpr uint32_t tmem = 0;                        // all 512 columns are this block's: they begin at column 0
   const int64_t U = cum[entities(p)];
-  const int64_t workers = workers_for(U, blocks, kMmaKeys);
+  const int64_t workers = workers_for<Problem>(U, blocks, kMmaKeys);
   const bool spare = block >= workers;                // fewer units than blocks
   const int64_t u0 = spare ? U : worker_begin(U, block, workers), u1 = spare ? U : worker_begin(U, block + 1, workers);
   // The combine kernel may queue up behind the first blocks that finish: its blocks do not fit beside one of these (registers), and
@@ -282,6 +284,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
     bool ok = true;
     for (int64_t u = u0; u < u1 && ok;) {
       const Segment s = segment_at<C::kRows>(p, cum, u, u1);
+      if (Problem::kEnds > 0 && s.n == 0) { u += s.step; continue; }
       const int32_t page0 = s.sp.lo / kPage + s.t0 * kTilePages + (lane & (kTilePages - 1));
       auto fetch = [&](int t) -> int32_t {            // this lane's page of tile t: raw id, or -2 where there is none
         const int32_t lp = page0 + t * kTilePages;
@@ -318,7 +321,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
         id = next;
         next = after;
       }
-      u += s.n;
+      u += s.step;
     }
     // every copy lands before the block's shared memory is given up
     for (uint32_t i = issued > stages ? issued - stages : 0; i < issued; ++i)
@@ -356,6 +359,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
     };
     for (int64_t u = u0; u < u1;) {
       const Segment s = segment_at<C::kRows>(p, cum, u, u1);
+      if (Problem::kEnds > 0 && s.n == 0) { u += s.step; continue; }
       const uint32_t step = s.shared ? 1u : 2u, end = tiles + (uint32_t)s.n;
       uint32_t t = s.shared ? tiles : tiles + x;
       // An issuer arrives for a segment itself, and only once it has seen the one before: its waits go by parity, and a slot without
@@ -391,7 +395,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
       }
       if (!ok) break;
       tiles = end;
-      u += s.n;
+      u += s.step;
     }
     __syncwarp();
     if (el) {                                        // nothing is in flight when the TMEM is given back
@@ -414,6 +418,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
     bool on_first = true;
     for (int64_t u = u0; u < u1;) {
       const Segment s = segment_at<C::kRows>(p, cum, u, u1);
+      if (Problem::kEnds > 0 && s.n == 0) { u += s.step; continue; }
       const Span& sp = s.sp;
       const int r = s.shared ? x * 128 + row : row;    // row of the block
       const bool live = r < s.rows;
@@ -659,35 +664,63 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
       float* pb = p.partials + (2 * (int64_t)block + (on_first ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
       const int64_t grow = live ? global_row(r) : 0;
       const RowPart part = complete && !finish ? whole_row(p, sp, grow) : RowPart{pb + r * D, pb + C::kRows * D + r, pb + C::kRows * (D + 1) + r};
-#pragma unroll 1
-      for (int c = c0; c < c1; c += 32) {
-        uint32_t o[32];
-        tm_ld32(o_addr + c, o);
+      auto columns = [&](int c, uint32_t (&o)[16]) {   // 16 of this thread's row, of both slots' accumulators
+        tm_ld16(o_addr + c, o);
         tm_wait_ld();
         if (!s.shared) {
-          uint32_t o2[32];
-          tm_ld32(lane_addr + 256 + (x ^ 1) * 128 + c, o2);
+          uint32_t o2[16];
+          tm_ld16(lane_addr + 256 + (x ^ 1) * 128 + c, o2);
           tm_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            o[e] = __float_as_uint(__uint_as_float(o[e]) * scale0 + __uint_as_float(o2[e]) * scale1);
+          for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale0 + __uint_as_float(o2[e]) * scale1);
         }
-        if (live && finish) {
+      };
+      if (finish) {
+#pragma unroll 1
+        for (int c = c0; c < (idle ? c0 : c1); c += 16) {
+          uint32_t o[16];
+          columns(c, o);
+          if (live) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint4 w;
-            w.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-            w.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-            w.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-            w.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-            *reinterpret_cast<uint4*>(p.out + grow * D + c + e) = w;
+            for (int e = 0; e < 16; e += 8) {
+              uint4 w;
+              w.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+              w.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+              w.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+              w.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+              *reinterpret_cast<uint4*>(p.out + grow * D + c + e) = w;
+            }
           }
-        } else if (live) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<uint4*>(part.o + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          __syncwarp();
         }
-        __syncwarp();
+      } else {
+        // A part of a row block.  A thread has a row, 512 bytes from the next one's: 16 columns at a time go through the warp's 2 KB of the
+        // query tile (whose products are done), so that a store takes eight whole pieces of 64 bytes and not 32 of 16.
+        const uint32_t mine_s = qs + (uint32_t)(kWide ? warp & 3 : warp) * 2048u;
+        const uint64_t at = live ? reinterpret_cast<uint64_t>(part.o) : 0ull;
+#pragma unroll 1
+        for (int c = c0; c < (idle ? c0 : c1); c += 16) {
+          uint32_t o[16];
+          columns(c, o);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(mine_s + (uint32_t)(lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4))), "r"(o[4 * e]),
+                         "r"(o[4 * e + 1]), "r"(o[4 * e + 2]), "r"(o[4 * e + 3])
+                         : "memory");
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int rw = (lane >> 2) + 8 * i, e = lane & 3;
+            const uint64_t to = __shfl_sync(0xffffffffu, at, rw);
+            uint4 w;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                         : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                         : "r"(mine_s + (uint32_t)(rw * 64 + ((e ^ ((rw >> 1) & 3)) << 4))));
+            if (to) *reinterpret_cast<uint4*>(reinterpret_cast<float*>(to) + c + 4 * e) = w;
+          }
+          __syncwarp();
+        }
+        if (s.shared) named_sync(2 + x, 128);          // the next queries go where other warps' columns were
       }
       if (live && (s.shared || x == 0)) {
         if (!finish) {
@@ -703,7 +736,7 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
         tc_after();
       }
       on_first = false;
-      u += s.n;
+      u += s.step;
     }
   }
   tc_before();
