@@ -214,10 +214,12 @@ __global__ void __launch_bounds__(kListThreads) free_pages_kernel(const int32_t*
 //   row starts                every block scans the requests' tokens
 //   entries without a page    each block looks at its share of the requests' table entries and counts
 //   pages dealt               the counts meet through shared memory; every block scans them
-//   table, counts, lengths, places of the rows: all threads of the cluster, a row's request found by bisection of the starts
-// Nothing is written before the cluster barrier behind the counts, so no block sees a table that is half changed.
+//   table, counts, places of the rows   all threads of the cluster, a page or a row each, whose request is found by bisection
+// Nothing is written before the cluster barrier behind the counts, so no block sees a table that is half changed.  It is a chain of round
+// trips (requests, entries, list, counts) and barriers: 64 decodes 6.6 us, 1000 decodes and 24 prompts of together 31000 tokens 9.6 (a warp
+// per long request instead of a thread per page: 22).
 constexpr int kExtendBlocks = 8, kExtendThreads = 1024, kExtendMax = 8192, kExtendRows = 1 << 18;
-constexpr int kLongPages = 4;              // entries that a thread walks by itself; beyond, its warp does
+constexpr int kLongPages = 4;              // entries that a thread looks at by itself; beyond, its warp does
 struct ExtendParams {
   const int32_t* rows;
   const int32_t* old_lens;
@@ -236,23 +238,24 @@ struct ExtendParams {
   int64_t num_pages, max_list;
   int32_t n, num_rows, max_pages, max_rows;
 };
-size_t extend_smem(int n, int num_rows) { return (size_t)(2 * ((num_rows + 31) / 32) + 3 * n + 2) * 4; }
+size_t extend_smem(int n, int num_rows) { return (size_t)(2 * ((num_rows + 31) / 32) + 4 * n + 2) * 4; }
 
 __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendParams p) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   extern __shared__ int32_t extend_s[];
   __shared__ int64_t wsum[kExtendThreads / 32];
+  __shared__ int32_t given_s;
   const int bits = (p.num_rows + 31) / 32, n = p.n;
   uint32_t* once = reinterpret_cast<uint32_t*>(extend_s);        // rows that are named, and named twice
   uint32_t* twice = once + bits;
   int32_t* need = extend_s + 2 * bits;                            // pages a request lacks, -1 if it is refused or idle
-  int32_t* base = need + n;                                       // the first of its pages in the list, -1 if it gets none
-  int32_t* start = base + n;                                      // [n + 1] its first row
+  int32_t* entry = need + n;                                      // its first entry without a page; -2 - entry where others behind it have one
+  int32_t* before = entry + n;                                    // pages that the requests before it lack
+  int32_t* start = before + n;                                    // [n + 1] its first row
   const int rank = (int)cluster.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
   for (int i = tid; i < 2 * bits; i += kExtendThreads) once[i] = 0u;
-  __syncthreads();
   const int per = (n + kExtendThreads - 1) / kExtendThreads, f0 = min(tid * per, n), f1 = min(f0 + per, n);   // requests this thread scans
   // exclusive prefix over the threads of one value each; `all`: the sum
   auto scan = [&](int64_t v, int64_t& all) -> int64_t {
@@ -274,36 +277,35 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
       wsum[lane] = w;
     }
     __syncthreads();
-    const int64_t before = (warp ? wsum[warp - 1] : 0) + incl - v;
+    const int64_t front = (warp ? wsum[warp - 1] : 0) + incl - v;
     all = wsum[31];
     __syncthreads();
-    return before;
+    return front;
   };
+  const int64_t count = min((int64_t)*p.free_count, p.max_list), begin = p.free_begin ? max(*p.free_begin, 0) : 0;
   int64_t tokens = 0, all_tokens;
+  for (int f = f0; f < f1; ++f) tokens += max(p.new_tokens[f], 0);
+  if (tid == 0) given_s = 0;
+  int64_t at = scan(tokens, all_tokens);                          // (its barriers also close the clearing of the bits)
+  const int64_t room = p.max_rows >= 0 ? p.max_rows : INT32_MAX;
   for (int f = f0; f < f1; ++f) {
     const int32_t row = p.rows[f];
     if (row >= 0 && row < p.num_rows) {
       const uint32_t bit = 1u << (row & 31);
       if (atomicOr(once + (row >> 5), bit) & bit) atomicOr(twice + (row >> 5), bit);
     }
-    tokens += max(p.new_tokens[f], 0);
-  }
-  int64_t at = scan(tokens, all_tokens);                          // (its barriers also close the bits)
-  const int64_t room = p.max_rows >= 0 ? p.max_rows : INT32_MAX;
-  for (int f = f0; f < f1; ++f) {
     start[f] = (int32_t)min(at, room);
     at += max(p.new_tokens[f], 0);
-    base[f] = at > room ? -1 : 0;                                 // do its rows fit?
+    before[f] = at > room;                                        // do its rows not fit?
   }
   if (tid == 0) start[n] = (int32_t)min(all_tokens, room);
-  const int64_t count = min((int64_t)*p.free_count, p.max_list), begin = p.free_begin ? max(*p.free_begin, 0) : 0;
   __syncthreads();
 
   // a thread per request of this block's share; long ones by the warp
   const int s0 = (int)((int64_t)n * rank / kExtendBlocks), s1 = (int)((int64_t)n * (rank + 1) / kExtendBlocks);
   for (int g0 = s0 + warp * 32; g0 < s1; g0 += kExtendThreads) {
     const int f = g0 + lane;
-    int32_t row = -1, c = 0, first = 0, end = 0, lacks = -1;
+    int32_t row = -1, c = 0, first = 0, end = 0, lacks = -1, hole = INT32_MAX;   // hole: the first entry without a page
     bool bad = false;
     if (f < s1) {
       row = p.rows[f];
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
       const int32_t m = p.new_tokens[f];
       if (row >= 0) {
         bad = row >= p.num_rows || (twice[row >> 5] >> (row & 31) & 1u) || c < 0 || m < 0 ||
-              (int64_t)c + m > min((int64_t)p.max_pages * kPage, (int64_t)INT32_MAX) || base[f] < 0;
+              (int64_t)c + m > min((int64_t)p.max_pages * kPage, (int64_t)INT32_MAX) || before[f] != 0;
         if (!bad) {
           lacks = 0;
           if (m > 0) {
@@ -321,8 +323,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
         }
       }
     }
-    auto look = [&](int32_t row, int32_t c, int32_t i, bool& wrong) -> int {   // does entry i lack a page?
-      const int32_t id = p.table[(int64_t)row * p.max_pages + i];
+    auto look = [&](int32_t id, int32_t c, int32_t i, bool& wrong) -> int {   // does entry i, which holds id, lack a page?
       if (id < 0) {
         wrong |= i == c / kPage && c % kPage != 0;                // the tokens in it are gone
         return 1;
@@ -330,20 +331,47 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
       wrong |= id >= p.num_pages || p.refs[id] != 1;              // tokens must not be written to a page that others hold
       return 0;
     };
-    if (end - first <= kLongPages)
-      for (int i = first; i < end; ++i) lacks += look(row, c, i, bad);
+    if (end - first <= kLongPages) {
+      int32_t id[kLongPages];
+#pragma unroll
+      for (int k = 0; k < kLongPages; ++k) id[k] = first + k < end ? p.table[(int64_t)row * p.max_pages + first + k] : 0;
+#pragma unroll
+      for (int k = 0; k < kLongPages; ++k)
+        if (first + k < end && look(id[k], c, first + k, bad)) {
+          ++lacks;
+          hole = min(hole, first + k);
+        }
+    }
     uint32_t rest = __ballot_sync(0xffffffffu, end - first > kLongPages);
     for (; rest; rest &= rest - 1) {
       const int who = __ffs(rest) - 1;
       const int32_t r = __shfl_sync(0xffffffffu, row, who), cc = __shfl_sync(0xffffffffu, c, who);
       const int32_t a = __shfl_sync(0xffffffffu, first, who), e = __shfl_sync(0xffffffffu, end, who);
-      int32_t sum = 0;
+      const int32_t* entries = p.table + (int64_t)r * p.max_pages;
+      int32_t sum = 0, least = INT32_MAX;
       bool wrong = false;
-      for (int i = a + lane; i < e; i += 32) sum += look(r, cc, i, wrong);
+      for (int i0 = a; i0 < e; i0 += 4 * 32) {
+        int32_t id[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + 32 * k + lane;
+          id[k] = i < e ? entries[i] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + 32 * k + lane;
+          if (i < e && look(id[k], cc, i, wrong)) {
+            ++sum;
+            least = min(least, i);
+          }
+        }
+      }
       sum = __reduce_add_sync(0xffffffffu, sum);
+      least = __reduce_min_sync(0xffffffffu, least);
       wrong = __any_sync(0xffffffffu, wrong);
       if (lane == who) {
         lacks = sum;
+        hole = least;
         bad = wrong;
       }
     }
@@ -351,88 +379,93 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
       lacks = -1;
       atomicOr(p.status, kErrBadPage);
     }
-    if (f < s1) need[f] = lacks;
+    if (f < s1) {
+      need[f] = lacks;
+      entry[f] = lacks <= 0 ? 0 : end - hole == lacks ? hole : -2 - hole;
+    }
   }
   cluster.sync();
   for (int f = tid; f < n; f += kExtendThreads) {                 // the other blocks' counts
     int r = (int)((int64_t)f * kExtendBlocks / n);
     while (f >= (int)((int64_t)n * (r + 1) / kExtendBlocks)) ++r;
     while (f < (int)((int64_t)n * r / kExtendBlocks)) --r;
-    if (r != rank) need[f] = *cluster.map_shared_rank(need + f, r);
+    if (r != rank) {
+      need[f] = *cluster.map_shared_rank(need + f, r);
+      entry[f] = *cluster.map_shared_rank(entry + f, r);
+    }
   }
   cluster.sync();                                                 // (nobody leaves, or changes the table, while its counts are read)
   int64_t pages = 0, all_pages;
   for (int f = f0; f < f1; ++f) pages += max(need[f], 0);
   at = scan(pages, all_pages);
+  // what is dealt out is a prefix of the list: up to the end of the last request that it is long enough for
   const int64_t avail = max(count - begin, (int64_t)0);
-  int64_t given = 0;
+  int32_t mine = 0;
   for (int f = f0; f < f1; ++f) {
-    const int32_t k = need[f];
-    if (k > 0) at += k;
-    base[f] = k < 0 || (k > 0 && at > avail) ? -1 : (int32_t)(at - max(k, 0));
-    if (k > 0 && at <= avail) given = at;
+    const int32_t k = max(need[f], 0);
+    before[f] = (int32_t)min(at, (int64_t)INT32_MAX);
+    at += k;
+    if (k > 0 && at <= avail) mine = (int32_t)at;
   }
-  // what is dealt out is a prefix of the list: the largest end of a request that was served
-  for (int o = 16; o > 0; o >>= 1) given = max(given, __shfl_xor_sync(0xffffffffu, given, o));
-  if (lane == 0) wsum[warp] = given;
+  mine = __reduce_max_sync(0xffffffffu, mine);
+  if (lane == 0 && mine > 0) atomicMax(&given_s, mine);
   __syncthreads();
-  if (p.free_end && rank == 0 && tid == 0) {
-    for (int w = 0; w < kExtendThreads / 32; ++w) given = max(given, wsum[w]);
-    *p.free_end = (int32_t)(begin + given);
-  }
+  const int32_t given = given_s;
+  auto served = [&](int f) { return need[f] == 0 || (need[f] > 0 && (int64_t)before[f] + need[f] <= given); };
 
   const int all = kExtendBlocks * kExtendThreads, gt = rank * kExtendThreads + tid;
+  auto deal = [&](int32_t* to, int64_t k) {                       // the k-th page from where dealing begins
+    const int32_t id = p.free_list[begin + k];
+    if (id < 0 || id >= p.num_pages || atomicCAS(p.refs + id, 0, 1) != 0) atomicOr(p.status, kErrBadPage);
+    else *to = id;
+  };
+  auto request_of = [&](const int32_t* from, int32_t x) {         // the last request f with from[f] <= x
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (from[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+  };
+  for (int k = gt; k < given; k += all) {                         // (requests that lack nothing lie before the one found)
+    const int f = request_of(before, k);
+    if (entry[f] >= 0) deal(p.table + (int64_t)p.rows[f] * p.max_pages + entry[f] + (k - before[f]), k);
+  }
   for (int g0 = gt - lane; g0 < n; g0 += all) {
     const int f = g0 + lane;
-    int32_t row = -1, c = 0, first = 0, end = 0, from = -1;
+    bool holes = false;
     if (f < n) {
-      from = base[f];
-      c = p.old_lens[f];
-      const int32_t m = p.new_tokens[f];
+      const int32_t c = p.old_lens[f];
       if (p.row_starts) p.row_starts[f] = start[f];
-      if (p.new_lens) p.new_lens[f] = from >= 0 ? c + m : c;
-      if (from >= 0 && need[f] > 0) {
-        row = p.rows[f];
-        first = c / kPage;
-        end = (c + m - 1) / kPage + 1;
-      }
+      if (p.new_lens) p.new_lens[f] = served(f) ? c + p.new_tokens[f] : c;
+      holes = need[f] > 0 && entry[f] < 0 && served(f);
     }
-    auto deal = [&](int32_t* entry, int64_t k) {                  // the k-th page from the cursor
-      const int32_t id = p.free_list[begin + k];
-      if (id < 0 || id >= p.num_pages || atomicCAS(p.refs + id, 0, 1) != 0) atomicOr(p.status, kErrBadPage);
-      else *entry = id;
-    };
-    int32_t* mine = p.table + (int64_t)row * p.max_pages;
-    if (end - first <= kLongPages)
-      for (int i = first; i < end; ++i)
-        if (mine[i] < 0) deal(mine + i, from++);
-    uint32_t rest = __ballot_sync(0xffffffffu, end - first > kLongPages);
-    for (; rest; rest &= rest - 1) {
-      const int who = __ffs(rest) - 1;
-      int32_t* theirs = p.table + (int64_t)__shfl_sync(0xffffffffu, row, who) * p.max_pages;
-      const int32_t a = __shfl_sync(0xffffffffu, first, who), e = __shfl_sync(0xffffffffu, end, who);
-      int32_t k = __shfl_sync(0xffffffffu, from, who);
-      for (int i0 = a; i0 < e; i0 += 32) {
+    uint32_t rest = __ballot_sync(0xffffffffu, holes);
+    for (; rest; rest &= rest - 1) {                              // pages here and there: the warp walks them
+      const int h = g0 + __ffs(rest) - 1;
+      int32_t* entries = p.table + (int64_t)p.rows[h] * p.max_pages;
+      const int end = (p.old_lens[h] + p.new_tokens[h] - 1) / kPage + 1;
+      int32_t k = before[h];
+      for (int i0 = -2 - entry[h]; i0 < end; i0 += 32) {
         const int i = i0 + lane;
-        const bool wants = i < e && theirs[i] < 0;
+        const bool wants = i < end && entries[i] < 0;
         const uint32_t who_wants = __ballot_sync(0xffffffffu, wants);
-        if (wants) deal(theirs + i, k + __popc(who_wants & ((1u << lane) - 1u)));
+        if (wants) deal(entries + i, k + __popc(who_wants & ((1u << lane) - 1u)));
         k += __popc(who_wants);
       }
     }
   }
-  if (p.row_starts && gt == 0) p.row_starts[n] = start[n];
+  if (gt == 0) {
+    if (p.row_starts) p.row_starts[n] = start[n];
+    if (p.free_end) *p.free_end = (int32_t)(begin + given);
+  }
   for (int r = gt; r < p.max_rows; r += all) {
     int32_t seq = -1, slot = -1;
     if (r < start[n]) {
-      int lo = 0, hi = n;                                         // start[lo] <= r < start[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= r) lo = mid; else hi = mid;
-      }
-      if (base[lo] >= 0) {
-        seq = p.rows[lo];
-        slot = p.old_lens[lo] + (r - start[lo]);
+      const int f = request_of(start, r);
+      if (served(f)) {
+        seq = p.rows[f];
+        slot = p.old_lens[f] + (r - start[f]);
       }
     }
     p.seq[r] = seq;
