@@ -20,7 +20,7 @@ constexpr int kPage = 16;
 constexpr uint32_t kErrBadPage = 1u;      // bit of the stage's status word
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 128;
-constexpr int kWarpRows = 8;              // from this many rows per SM on, a warp takes a row (as in the append without norms)
+constexpr int kWarpRows = 3;              // from this many rows per SM on, a warp takes a row (measurements at the kernel)
 
 struct Params {
   const __nv_bfloat16* q;
@@ -52,9 +52,14 @@ enum Kind { kHalf, kInterleaved, kHalfOdd };   // halves a whole number of words
 //   kHalfOdd      words 2j and 2j + 1; partners through shared memory
 // The lane keeps its place within the head, so its cosines and (where all heads share them) weights stay in registers.
 // kPerHead: a row of weights for each head.
+// Measured at 32/8 heads of 128, rotary 128 half, us with a block and with a warp per row: 128 rows 4.9 / 7.7, 512 rows 8.8 / 8.0, 1184 rows -
+// / 7.9, 8192 rows - / 43.5 (4.6 TB/s of the bytes that have to move); there rotary 64 interleaved 43.6, 34 half 82, weights per head 48.  Bound by latency: a
+// lane has the sum, the shuffles and the root of a head between its load and its store, 24 warps an SM hide it (80 registers), and the next
+// head's words are all that is under way meanwhile.  16 warps with two heads each 48.9, 32 warps with spills 44 to 56; two elements at a time
+// with weights and rotation in one factor, a third fewer instructions, 44.0.
 template <int kKind, int kGroup, bool kPerHead>
-__global__ void __launch_bounds__(kThreads, 2) norm_rope_kernel(const Params p) {
-  constexpr int kRows = kThreads / kGroup, kWarps = kThreads / 32, kDeep = 2;
+__global__ void __launch_bounds__(kThreads, 3) norm_rope_kernel(const Params p) {
+  constexpr int kRows = kThreads / kGroup, kWarps = kThreads / 32;
   __shared__ float2 cs_s[kRows][kMaxPairs];
   __shared__ float stage_s[kKind == kHalfOdd ? kWarps : 1][kKind == kHalfOdd ? 32 * 17 : 1];
   pdl_launch_dependents();
@@ -63,10 +68,32 @@ __global__ void __launch_bounds__(kThreads, 2) norm_rope_kernel(const Params p) 
   const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / kGroup;
   float2* cs = cs_s[threadIdx.x / kGroup];
   if (r >= p.rows) return;                                        // (a whole group)
+  const int D = p.D, pairs = p.rot >> 1, words = D >> 3, lanes = D >> 4;
+  // this lane's words of a head
+  const int j = tid & (lanes - 1), half = p.rot >> 4, head0 = tid / lanes, step = kGroup / lanes;
+  int c0 = 2 * j, c1 = 2 * j + 1;
+  if (kKind == kHalf) {
+    if (j < half) { c0 = j; c1 = j + half; }
+    else { c0 = 2 * half + 2 * (j - half); c1 = c0 + 1; }
+  }
   const int32_t b = p.seq[r];
   if (b < 0) return;
+  struct Two { uint4 a, c; };
+  auto fetch = [&](const __nv_bfloat16* src, int h, int n) {
+    Two w = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+    if (h < n) {
+      const uint4* s = reinterpret_cast<const uint4*>(src + (int64_t)h * D);
+      w.a = s[c0];
+      w.c = s[c1];
+    }
+    return w;
+  };
+  const __nv_bfloat16* qr = p.q + r * p.q_stride;
+  const __nv_bfloat16* kr = p.k + r * p.k_stride;
+  const int Hq = p.q ? p.Hq : 0;
+  Two q_first = fetch(qr, head0, Hq);                             // under way while the row's place and cosines are found
+  const Two k_first = fetch(kr, head0, p.Hkv);
   const int32_t pos = p.positions[r], slot = p.slots[r];
-  const int D = p.D, pairs = p.rot >> 1, words = D >> 3, lanes = D >> 4;
   __nv_bfloat16* kv = nullptr;                                    // where the row's keys and values go: null if it is not appended
   const int lp = slot / kPage, t = slot % kPage;
   if (b < p.num_rows && slot >= 0 && lp < p.max_pages) {
@@ -100,13 +127,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_rope_kernel(const Params p) 
   if (kGroup == 32) __syncwarp();
   else __syncthreads();
 
-  // this lane's words, and the cosines and sines of its pairs: (e of word 0, e of word 1), or (2e, 2e + 1 of the 16)
-  const int j = tid & (lanes - 1), half = p.rot >> 4;
-  int c0 = 2 * j, c1 = 2 * j + 1;
-  if (kKind == kHalf) {
-    if (j < half) { c0 = j; c1 = j + half; }
-    else { c0 = 2 * half + 2 * (j - half); c1 = c0 + 1; }
-  }
+  // the cosines and sines of this lane's pairs: (e of word 0, e of word 1), or (2e, 2e + 1 of the 16)
   float2 cs_r[kKind == kHalfOdd ? 1 : 8];
   uint32_t turns = 0;                                             // bit e: pair e is rotated
   if (kKind != kHalfOdd) {
@@ -121,7 +142,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_rope_kernel(const Params p) 
   float* mine = stage_s[kKind == kHalfOdd ? threadIdx.x >> 5 : 0];
   const float inv_d = 1.f / (float)D;
 
-  auto walk = [&](const __nv_bfloat16* src, const float* weight, uint4* dst, int64_t dst_words, uint32_t flip, int n) {
+  auto walk = [&](Two w, const __nv_bfloat16* src, const float* weight, uint4* dst, int64_t dst_words, uint32_t flip, int n) {
     float w0[8], w1[8];
     auto weights = [&](int h) {
       const float* w = weight + (kPerHead ? (int64_t)h * D : 0);
@@ -138,89 +159,76 @@ __global__ void __launch_bounds__(kThreads, 2) norm_rope_kernel(const Params p) 
     } else if (!kPerHead) {
       weights(0);
     }
-    const int step = kGroup / lanes;
     // (all lanes of a warp make the same number of rounds: they meet in the shuffles)
-    for (int base = 0; base < n; base += kDeep * step) {
-      uint4 a[kDeep], c[kDeep];
+    for (int base = 0; base < n; base += step) {
+      const int h = base + head0;
+      const Two ahead = fetch(src, h + step, n);
+      float x[8], y[8];
+      unpack8(w.a, x);
+      unpack8(w.c, y);
+      float sum = 0.f;
 #pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const int h = base + u * step + tid / lanes;
-        a[u] = c[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (h < n) {
-          const uint4* s = reinterpret_cast<const uint4*>(src + (int64_t)h * D);
-          a[u] = s[c0];
-          c[u] = s[c1];
-        }
+      for (int e = 0; e < 8; ++e) sum += x[e] * x[e] + y[e] * y[e];
+      for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const float scale = rsqrtf(sum * inv_d + p.eps);
+      if (kPerHead && weight != nullptr && h < n) weights(h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] *= scale * w0[e];
+        y[e] *= scale * w1[e];
       }
+      if (kKind == kHalf) {
+        if (turns) {
 #pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const int h = base + u * step + tid / lanes;
-        float x[8], y[8];
-        unpack8(a[u], x);
-        unpack8(c[u], y);
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += x[e] * x[e] + y[e] * y[e];
-        for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float scale = rsqrtf(sum * inv_d + p.eps);
-        if (kPerHead && weight != nullptr && h < n) weights(h);
+          for (int e = 0; e < 8; ++e) {
+            const float z = x[e] * cs_r[e].x - y[e] * cs_r[e].y;
+            y[e] = y[e] * cs_r[e].x + x[e] * cs_r[e].y;
+            x[e] = z;
+          }
+        }
+      } else if (kKind == kInterleaved) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[e] *= scale * w0[e];
-          y[e] *= scale * w1[e];
-        }
-        if (kKind == kHalf) {
-          if (turns) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float z = x[e] * cs_r[e].x - y[e] * cs_r[e].y;
-              y[e] = y[e] * cs_r[e].x + x[e] * cs_r[e].y;
-              x[e] = z;
-            }
-          }
-        } else if (kKind == kInterleaved) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float& lo = e < 4 ? x[2 * e & 7] : y[2 * e & 7];
-            float& hi = e < 4 ? x[(2 * e & 7) + 1] : y[(2 * e & 7) + 1];
-            if ((turns >> e) & 1u) {
-              const float z = lo * cs_r[e].x - hi * cs_r[e].y;
-              hi = hi * cs_r[e].x + lo * cs_r[e].y;
-              lo = z;
-            }
-          }
-        } else {
-          float* head = mine + lane / lanes * lanes * 17;         // a lane's 16 values, a word of padding behind
-          __syncwarp();
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            head[j * 17 + e] = x[e];
-            head[j * 17 + 8 + e] = y[e];
-          }
-          __syncwarp();
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int d = 16 * j + e;
-            float& own = e < 8 ? x[e & 7] : y[e & 7];
-            if (d < p.rot) {
-              const bool upper = d >= pairs;
-              const int i = upper ? d - pairs : d, other = upper ? i : d + pairs;
-              const float2 t2 = cs[i];
-              const float o = head[(other >> 4) * 17 + (other & 15)];
-              own = upper ? own * t2.x + o * t2.y : own * t2.x - o * t2.y;
-            }
+          float& lo = e < 4 ? x[2 * e & 7] : y[2 * e & 7];
+          float& hi = e < 4 ? x[(2 * e & 7) + 1] : y[(2 * e & 7) + 1];
+          if ((turns >> e) & 1u) {
+            const float z = lo * cs_r[e].x - hi * cs_r[e].y;
+            hi = hi * cs_r[e].x + lo * cs_r[e].y;
+            lo = z;
           }
         }
-        if (h < n) {
-          uint4* out = dst + h * dst_words;
-          out[c0 ^ flip] = pack8(x);
-          out[c1 ^ flip] = pack8(y);
+      } else {
+        float* head = mine + lane / lanes * lanes * 17;         // a lane's 16 values, a word of padding behind
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          head[j * 17 + e] = x[e];
+          head[j * 17 + 8 + e] = y[e];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int d = 16 * j + e;
+          float& own = e < 8 ? x[e & 7] : y[e & 7];
+          if (d < p.rot) {
+            const bool upper = d >= pairs;
+            const int i = upper ? d - pairs : d, other = upper ? i : d + pairs;
+            const float2 t2 = cs[i];
+            const float o = head[(other >> 4) * 17 + (other & 15)];
+            own = upper ? own * t2.x + o * t2.y : own * t2.x - o * t2.y;
+          }
         }
       }
+      if (h < n) {
+        uint4* out = dst + h * dst_words;
+        out[c0 ^ flip] = pack8(x);
+        out[c1 ^ flip] = pack8(y);
+      }
+      w = ahead;
     }
   };
-  if (p.q) walk(p.q + r * p.q_stride, p.q_weight, reinterpret_cast<uint4*>(p.q_out + r * p.Hq * D), words, 0u, p.Hq);
-  if (kv) walk(p.k + r * p.k_stride, p.k_weight, k_dst, 2 * tile_words, swap, p.Hkv);
+  walk(q_first, qr, p.q_weight, reinterpret_cast<uint4*>(p.q_out + r * p.Hq * D), words, 0u, Hq);
+  if (kv) walk(k_first, kr, p.k_weight, k_dst, 2 * tile_words, swap, p.Hkv);
 }
 
 template <int kKind, int kGroup, bool kPerHead>
