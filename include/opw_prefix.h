@@ -42,7 +42,8 @@ opw_status_t opw_prefix_attn_destroy(opw_prefix_attn_t *prefix); /* NULL is acce
  * out and lse as opw_decode_attention computes them from q, kv_lens and page_table, provided that the sequences of a group hold the same
  * pages where they say so: for group g < groups, the rows group_starts[g] .. group_starts[g + 1] - 1 name, in their first
  * prefix_lens[g] / page_size entries (whole pages only), the same pages as far as their own kv_lens reach.  Only the entries of the group's
- * longest row (the first of those) are read there.  A group of one row, or with a prefix of less than a page, is fine and shares nothing;
+ * longest row (the first of those) are read there, on a window layer from the first key on that any row of the group sees: that row has to hold
+ * them all.  A group of one row, or with a prefix of less than a page, is fine and shares nothing;
  * rows may be shorter than their group's prefix, or inactive (kv_lens <= 0: out = 0, lse = -inf).
  * On a window layer each row sees the last W keys of its own, in the prefix and behind it.
  * Cached rows that a sequence does not see do not touch its result, whatever they hold (NaN and infinities included).  Scores, maxima, sums
@@ -53,7 +54,7 @@ opw_status_t opw_prefix_attn_destroy(opw_prefix_attn_t *prefix); /* NULL is acce
  *   group_starts : DEVICE int32 [groups + 1], from 0 to batch, not descending.  Other starts share nothing (the result is the same) and
  *                are recorded
  *   prefix_lens  : DEVICE int32 [groups]; negative ones count as 0
- *   page_table : DEVICE int32 [batch, max_pages_per_seq]; entries wholly before a row's window are not read for that row alone
+ *   page_table : DEVICE int32 [batch, max_pages_per_seq]; entries wholly before the windows of all of a group's rows are never read
  *   lse        : DEVICE float [batch, Hq] or NULL
  * groups >= 1.  batch <= max_batch, batch <= OPW_PREFIX_MAX_BATCH and groups <= OPW_PREFIX_MAX_GROUPS (OPW_ERR_CAPACITY).  Enqueues two
  * kernels.  How the keys are split depends on batch, groups, starts, lengths and the window only, never on page ids, and the result does

@@ -807,18 +807,20 @@ class Stage:
         [heads, head_dim] with a row for each head; either may be None (ones)."""
         where, D, dev = "norm_rope_append", self.head_dim, self.index
         a, c = self._append_args(where, rope, q, k, v, seq, slots, positions, page_table, q_out)
-        per_head, ptrs = None, []
-        for w, heads in ((q_weight, self.num_q_heads), (k_weight, self.num_kv_heads)):
-            if w is None:
-                ptrs.append(None)
-                continue
-            rows = len(w.shape) == 2
-            if w.shape != ((heads, D) if rows else (D,)) or per_head not in (None, rows):
-                raise ValueError(f"{where}: weights must both be [{D}], or [{self.num_q_heads}, {D}] and [{self.num_kv_heads}, {D}]")
-            _need(where, dev, self._f32, -1, w)
-            per_head = rows
-            ptrs.append(w.data_ptr())
-        rc = self._lib.opw_norm_rope_append(self.handle, layer, *a, ptrs[0], ptrs[1], 1 if per_head else 0, eps, *c)
+        q_ptr = k_ptr = None
+        one = q_weight if q_weight is not None else k_weight
+        per_head = one is not None and one.dim() == 2
+        fits = True
+        if q_weight is not None:
+            fits = q_weight.shape == ((self.num_q_heads, D) if per_head else (D,))
+            q_ptr = q_weight.data_ptr()
+        if k_weight is not None:
+            fits = fits and k_weight.shape == ((self.num_kv_heads, D) if per_head else (D,))
+            k_ptr = k_weight.data_ptr()
+        if not fits:
+            raise ValueError(f"{where}: weights must both be [{D}], or [{self.num_q_heads}, {D}] and [{self.num_kv_heads}, {D}]")
+        _need(where, dev, self._f32, -1, *[w for w in (q_weight, k_weight) if w is not None])
+        rc = self._lib.opw_norm_rope_append(self.handle, layer, *a, q_ptr, k_ptr, 1 if per_head else 0, eps, *c)
         if rc:
             _check(rc, "opw_norm_rope_append")
 

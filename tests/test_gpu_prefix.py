@@ -252,6 +252,20 @@ def test_the_largest_batch_and_number_of_groups(Hq, Hkv, D):
         check(out[dev(pick)], lse[dev(pick)], ref, 120)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (32, 8, 128), (6, 2, 256), (16, 1, 128)])
+def test_one_large_group_among_single_rows(Hq, Hkv, D):
+    rng = np.random.default_rng(9550 + D)
+    sizes = [1] * 9 + [70] + [1] * 12
+    prefix = [int(x) for x in rng.integers(0, 200, size=len(sizes))]
+    prefix[9] = 777
+    lens = [int(prefix[g] + rng.integers(1, 90)) for g, s in enumerate(sizes) for _ in range(s)]
+    pool, tab, q, starts = shared_batch(rng, sizes, prefix, lens, Hq, Hkv, D)
+    for window in (0, 300):
+        out, lse, rc = run(pool, tab, q, lens, starts, prefix, Hq, Hkv, D, window)
+        assert rc == B.OPW_OK
+        check(out, lse, step.decode_attention(pool, Hq, Hkv, D, q, lens, tab, window), 900)
+
+
 @pytest.mark.parametrize("Hq,Hkv,D,members", [(32, 8, 128, 33), (8, 2, 64, 20), (16, 2, 256, 4)])
 @pytest.mark.parametrize("shape", ["rise", "fall", "alternate"])
 def test_scores_that_rise_and_fall_along_the_keys(Hq, Hkv, D, members, shape):

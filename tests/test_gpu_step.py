@@ -391,6 +391,24 @@ def test_the_first_new_token_is_distributed_as_the_targets(draw):
     assert st.poll_error() == B.OPW_OK and (took > 1).any() and (took == 1).any()
 
 
+def test_verify_of_the_largest_batch_and_vocabulary():
+    rng = np.random.default_rng(7400)
+    st = small_stage()
+    n = 65535
+    p = torch.zeros(n, 1, 3, device="cuda")
+    last = torch.from_numpy(rng.integers(0, 3, size=n)).cuda()
+    p.scatter_(2, last[:, None, None], 1.0)
+    path, took, follows = run_verify(st, p, None, np.zeros((n, 1)), np.full((n, 1), -1), np.ones(n), rng.random((n, 1)))
+    assert torch.equal(follows.long(), last) and (took == 1).all() and (path == 0).all()
+    V = 1 << 24
+    p, q = torch.zeros(1, 2, V, device="cuda"), torch.zeros(1, 2, V, device="cuda")
+    p[0, 0, V - 2:], p[0, 1, V - 1], q[0, 0, 5] = 0.5, 1.0, 1.0
+    for token, u, want in ((5, (0.4, 0.9), (1, V - 2)), (5, (0.6, 0.0), (1, V - 1)), (V - 1, (0.1, 0.9), (2, V - 1))):
+        path, took, follows = run_verify(st, p, q, [[0, token]], [[-1, 0]], [2], [u])
+        assert (took.item(), follows.item()) == want
+    assert st.poll_error() == B.OPW_OK
+
+
 def test_verify_refuses():
     st, V, T, n = small_stage(), 64, 4, 3
     target, q = torch.rand(n, T, V, device="cuda"), torch.rand(n, T, V, device="cuda")
