@@ -216,9 +216,9 @@ __global__ void __launch_bounds__(kListThreads) free_pages_kernel(const int32_t*
 //   pages dealt               the counts meet through shared memory; every block scans them
 //   table, counts, places of the rows   all threads of the cluster, a page or a row each, whose request is found by bisection
 // Nothing is written before the cluster barrier behind the counts, so no block sees a table that is half changed.  It is a chain of round
-// trips (requests, entries, list, counts) and barriers: 64 decodes 6.6 us, 1000 decodes and 24 prompts of together 31000 tokens 9.6 (a warp
-// per long request instead of a thread per page: 22).
-constexpr int kExtendBlocks = 8, kExtendThreads = 1024, kExtendMax = 8192, kExtendRows = 1 << 18;
+// trips (requests, entries, list, counts) and barriers.  64 decodes 6.4 us in one block (kExtendFew requests and a row a thread at most), 7.6 in
+// eight; 1000 decodes and 24 prompts of together 31000 tokens 14 (with a warp per long request instead of a thread per page 22).
+constexpr int kExtendBlocks = 8, kExtendFew = 256, kExtendThreads = 1024, kExtendMax = 8192, kExtendRows = 1 << 18;
 constexpr int kLongPages = 4;              // entries that a thread looks at by itself; beyond, its warp does
 struct ExtendParams {
   const int32_t* rows;
@@ -240,6 +240,7 @@ struct ExtendParams {
 };
 size_t extend_smem(int n, int num_rows) { return (size_t)(2 * ((num_rows + 31) / 32) + 4 * n + 2) * 4; }
 
+template <int kBlocks>
 __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendParams p) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
   __syncthreads();
 
   // a thread per request of this block's share; long ones by the warp
-  const int s0 = (int)((int64_t)n * rank / kExtendBlocks), s1 = (int)((int64_t)n * (rank + 1) / kExtendBlocks);
+  const int s0 = (int)((int64_t)n * rank / kBlocks), s1 = (int)((int64_t)n * (rank + 1) / kBlocks);
   for (int g0 = s0 + warp * 32; g0 < s1; g0 += kExtendThreads) {
     const int f = g0 + lane;
     int32_t row = -1, c = 0, first = 0, end = 0, lacks = -1, hole = INT32_MAX;   // hole: the first entry without a page
@@ -386,9 +387,9 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
   }
   cluster.sync();
   for (int f = tid; f < n; f += kExtendThreads) {                 // the other blocks' counts
-    int r = (int)((int64_t)f * kExtendBlocks / n);
-    while (f >= (int)((int64_t)n * (r + 1) / kExtendBlocks)) ++r;
-    while (f < (int)((int64_t)n * r / kExtendBlocks)) --r;
+    int r = (int)((int64_t)f * kBlocks / n);
+    while (f >= (int)((int64_t)n * (r + 1) / kBlocks)) ++r;
+    while (f < (int)((int64_t)n * r / kBlocks)) --r;
     if (r != rank) {
       need[f] = *cluster.map_shared_rank(need + f, r);
       entry[f] = *cluster.map_shared_rank(entry + f, r);
@@ -413,7 +414,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
   const int32_t given = given_s;
   auto served = [&](int f) { return need[f] == 0 || (need[f] > 0 && (int64_t)before[f] + need[f] <= given); };
 
-  const int all = kExtendBlocks * kExtendThreads, gt = rank * kExtendThreads + tid;
+  const int all = kBlocks * kExtendThreads, gt = rank * kExtendThreads + tid;
   auto deal = [&](int32_t* to, int64_t k) {                       // the k-th page from where dealing begins
     const int32_t id = p.free_list[begin + k];
     if (id < 0 || id >= p.num_pages || atomicCAS(p.refs + id, 0, 1) != 0) atomicOr(p.status, kErrBadPage);
@@ -459,17 +460,47 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
     if (p.row_starts) p.row_starts[n] = start[n];
     if (p.free_end) *p.free_end = (int32_t)(begin + given);
   }
-  for (int r = gt; r < p.max_rows; r += all) {
-    int32_t seq = -1, slot = -1;
-    if (r < start[n]) {
-      const int f = request_of(start, r);
-      if (served(f)) {
-        seq = p.rows[f];
-        slot = p.old_lens[f] + (r - start[f]);
-      }
+  // eight rows in a row a thread (one where there are few): one bisection, then along the requests; what is read of them is read side by side
+  const bool wide = ((uintptr_t)p.seq | (uintptr_t)p.slots) % 16 == 0;
+  if (p.max_rows <= all) {
+    if (gt < p.max_rows) {
+      const int f = gt < start[n] ? request_of(start, gt) : n;
+      const bool live = f < n && served(f);
+      p.seq[gt] = live ? p.rows[f] : -1;
+      p.slots[gt] = live ? p.old_lens[f] + (gt - start[f]) : -1;
     }
-    p.seq[r] = seq;
-    p.slots[r] = slot;
+    return;
+  }
+  for (int r0 = 8 * gt; r0 < p.max_rows; r0 += 8 * all) {
+    int32_t seq[8], slot[8];
+    int f = r0 < start[n] ? request_of(start, r0) : n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      while (f < n && r0 + i >= start[f + 1]) ++f;
+      const bool live = f < n && served(f);
+      seq[i] = live ? f : -1;
+      slot[i] = live ? r0 + i - start[f] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (seq[i] >= 0) {
+        slot[i] += p.old_lens[seq[i]];
+        seq[i] = p.rows[seq[i]];
+      }
+    if (wide && r0 + 8 <= p.max_rows) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) {
+        *reinterpret_cast<int4*>(p.seq + r0 + i) = make_int4(seq[i], seq[i + 1], seq[i + 2], seq[i + 3]);
+        *reinterpret_cast<int4*>(p.slots + r0 + i) = make_int4(slot[i], slot[i + 1], slot[i + 2], slot[i + 3]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < p.max_rows) {
+          p.seq[r0 + i] = seq[i];
+          p.slots[r0 + i] = slot[i];
+        }
+    }
   }
 }
 
@@ -635,13 +666,16 @@ extern "C" opw_status_t opw_kv_extend(opw_attn_stage_t* stage, int32_t n, const 
   opw_device_guard guard(v.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
   const size_t smem = opw_pages::extend_smem(n, num_rows);
-  cudaError_t e = cudaSuccess;
-  if (smem > 40 * 1024)
-    e = cudaFuncSetAttribute(opw_pages::extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)opw_pages::extend_smem(opw_pages::kExtendMax, opw_pages::kExtendRows));
-  if (e == cudaSuccess)
-    e = opw_launch(opw_pages::extend_kernel, dim3(opw_pages::kExtendBlocks), dim3(opw_pages::kExtendThreads), smem,
-                   static_cast<cudaStream_t>(cuda_stream), v.pdl, opw_pages::kExtendBlocks, p);
+  const bool few = n <= opw_pages::kExtendFew && max_rows <= 8 * opw_pages::kExtendThreads;
+  auto launch = [&](auto kernel, int blocks) {
+    if (smem > 40 * 1024) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)opw_pages::extend_smem(opw_pages::kExtendMax, opw_pages::kExtendRows));
+      if (e != cudaSuccess) return e;
+    }
+    return opw_launch(kernel, dim3(blocks), dim3(opw_pages::kExtendThreads), smem, static_cast<cudaStream_t>(cuda_stream), v.pdl, blocks, p);
+  };
+  const cudaError_t e = few ? launch(opw_pages::extend_kernel<1>, 1) : launch(opw_pages::extend_kernel<opw_pages::kExtendBlocks>, opw_pages::kExtendBlocks);
   if (e != cudaSuccess) { (void)cudaGetLastError(); return OPW_ERR_CUDA; }
   *v.launches += 1;
   return OPW_OK;

@@ -47,8 +47,8 @@ PrefixLayout carve(const opw_stage_view& v) {
 // rows would take the warp kernel over the shared keys ten times a kv head.  Measured, us, by the warp kernel, with 128 and with 256 rows; 32/8 heads of
 // 128 unless said:
 //   4 samples of 1000, 16 rows         14, 17, 18        64 behind 8k (256 rows)                  98, 45, 58
-//   8 x 4 samples behind 4k, 16 rows   46, 48, 49        64 behind 8k, 64/8 heads (512 rows)     156, 61, 57
-//   32 pairs behind 2k, 8 rows         78, 87, 88        256 behind 32k (1024 rows)             1053, 205, 182
+//   8 x 4 samples behind 4k, 16 rows   46, 47, 49        64 behind 8k, 64/8 heads (512 rows)     156, 61, 57
+//   32 pairs behind 2k, 8 rows         78, 80, 88        256 behind 32k (1024 rows)             1053, 205, 182
 int mode_of(const opw_stage_view& v, int batch, int groups) {
   const int64_t G = v.Hq / v.Hkv, most = batch > groups ? batch - groups + 1 : 1;
   if (v.D == 256 || most * G <= 16) return kPrefixWarp;

@@ -3,9 +3,16 @@
 // The shared keys of a group are a problem of their own: its rows are the group's members x G query heads of a kv head, all of which see
 // (almost) the same keys, so that a key tile that is read once serves up to 256 rows on the tensor cores.  The keys behind the prefix are
 // the ordinary split-KV decode problem, G rows a sequence.  Both are the problems that the kernels of tree attention take
-// (opw_tree_kernels.cuh), solved in ONE launch: some blocks run the tensor-core kernel over the groups, the others the warp kernel over the
+// (opw_tree_kernels.cuh), solved in ONE launch: some blocks run the tensor-core kernel over the groups, the others a warp kernel over the
 // sequences, divided by what either costs.  The parts of a row's result -- one per worker that had keys of it -- are left in fp32
 // and merged by a second kernel.
+//
+// Measured, 32/8 heads of 128, in a replayed graph.  16 groups of 16 behind 16k, 16 to 2048 keys of their own: 369 us for 2.16 GB, 5.9 TB/s (90 % of
+// what a copy reaches); either half ends where the other does to 10 %.  64 behind 8k, 1 to 1024 of their own: 44.5 us, floor 26: of it 3 us of
+// survey, 6 of merge, and 35 in which 48 blocks take 2 x 128 rows of 128 tiles a head (0.8 us a tile while the whole chip reads, 0.6 of compute)
+// and 100 the 17000 pages of the rows.  The two launched one after the other had no share of each other's idle unit, and a launch more.  What it
+// took from 62 us: shares that count the ends of short rows (tail of 27 us gone), rows of one sequence with the products the other way
+// round (row_body), whole numbers of blocks a segment, partials stored in whole pieces.
 #pragma once
 
 #include "opw_tree_mma.cuh"
