@@ -810,16 +810,18 @@ class Stage:
         q_ptr = k_ptr = None
         one = q_weight if q_weight is not None else k_weight
         per_head = one is not None and one.dim() == 2
-        fits = True
+        fits, f32 = True, self._f32
         if q_weight is not None:
-            fits = q_weight.shape == ((self.num_q_heads, D) if per_head else (D,))
+            fits = (q_weight.dtype is f32 and q_weight.get_device() == dev and q_weight.is_contiguous()
+                    and q_weight.shape == ((self.num_q_heads, D) if per_head else (D,)))
             q_ptr = q_weight.data_ptr()
-        if k_weight is not None:
-            fits = fits and k_weight.shape == ((self.num_kv_heads, D) if per_head else (D,))
+        if fits and k_weight is not None:
+            fits = (k_weight.dtype is f32 and k_weight.get_device() == dev and k_weight.is_contiguous()
+                    and k_weight.shape == ((self.num_kv_heads, D) if per_head else (D,)))
             k_ptr = k_weight.data_ptr()
         if not fits:
-            raise ValueError(f"{where}: weights must both be [{D}], or [{self.num_q_heads}, {D}] and [{self.num_kv_heads}, {D}]")
-        _need(where, dev, self._f32, -1, *[w for w in (q_weight, k_weight) if w is not None])
+            raise ValueError(f"{where}: weights must be contiguous float32 on {self.device}, both [{D}], or [{self.num_q_heads}, {D}] and "
+                             f"[{self.num_kv_heads}, {D}]")
         rc = self._lib.opw_norm_rope_append(self.handle, layer, *a, q_ptr, k_ptr, 1 if per_head else 0, eps, *c)
         if rc:
             _check(rc, "opw_norm_rope_append")

@@ -120,7 +120,7 @@ extern "C" opw_status_t opw_prefix_attn_create(opw_attn_stage_t* stage, uint32_t
                                                opw_prefix_attn_t** out) {
   if (!stage || !out || !workspace || flags != 0 || (uintptr_t)workspace % 256) return OPW_ERR_INVALID_ARG;
   const opw_stage_view v = opw_view_of(stage);
-  if (!keys_fit(v)) return OPW_ERR_UNSUPPORTED;
+  if (!keys_fit(v) || v.sms < 2) return OPW_ERR_UNSUPPORTED;      // (groups and rows have blocks of their own)
   const PrefixLayout lay = carve(v);
   if (workspace_bytes < lay.total) return OPW_ERR_CAPACITY;
   opw_device_guard guard(v.device);

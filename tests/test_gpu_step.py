@@ -391,6 +391,25 @@ def test_the_first_new_token_is_distributed_as_the_targets(draw):
     assert st.poll_error() == B.OPW_OK and (took > 1).any() and (took == 1).any()
 
 
+@pytest.mark.parametrize("batch,vocab,kind", [(1, 150001, torch.float32), (9, 70000, torch.bfloat16), (40, 33000, torch.float32)])
+@pytest.mark.parametrize("draw", ["again", "distinct", "certain"])
+def test_verify_over_many_blocks_a_sequence_captured(batch, vocab, kind, draw):
+    rng = np.random.default_rng(7500 + batch)
+    st, T = small_stage(), 5
+    target, q, tokens, parents, size, u = random_verify(rng, batch, T, vocab, kind, draw, sharp=2.0)
+    ints, du = [i32(x) for x in (tokens, parents, size)], torch.zeros(batch, T, device="cuda")
+    path, took, follows = (torch.empty(s, dtype=torch.int32, device="cuda") for s in ((batch, T), batch, batch))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.tree_verify(target, q, *ints, du, path, took, follows, distinct=draw == "distinct")
+    for k in range(3):
+        u = rng.random((batch, T)) if k else np.full((batch, T), 0.99999)
+        du.copy_(torch.from_numpy(u.astype(np.float32)))
+        graph.replay()
+        same_as_oracle((path, took, follows), target, q, tokens, parents, size, u, draw)
+    assert st.poll_error() == B.OPW_OK
+
+
 def test_verify_of_the_largest_batch_and_vocabulary():
     rng = np.random.default_rng(7400)
     st = small_stage()
