@@ -186,7 +186,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {      // of the warp
 //     S^T (16 keys x 8) = K Q^T,   O^T (16 dimensions x 8) += V^T P^T,
 // which takes half the instructions of a tile whose upper eight rows are empty.  Hidden keys are hidden from all rows, so that clearing their
 // values is all that a masked page needs.  The ring has as many places a warp as fit beside the tables (p.stages).
-// 100 SMs read 50 GB/s each this way beside 48 that take groups, 1.3 us a page and warp; with the tile of 16 rows 41.
+// 100 SMs read 48 GB/s each this way beside 48 that take groups, 1.4 us a page and warp; with the tile of 16 rows 44.
 template <int D, int kWarps, class Problem>
 __device__ __forceinline__ void row_body(const Problem& p, unsigned char* smem, const int64_t* cum, int block, int blocks) {
   constexpr int KS = D / 16, ROWB = D * 2, TILE = WarpTree<D>::kTile, kEnds = Problem::kEnds;
