@@ -45,11 +45,11 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162f
 //     kDistinct  the same, but for the refused tokens, whose R stays what their refusal left; S = the sum of q without them
 //     kCertain   R = p, but for the refused tokens, whose R is max(R - C, 0)
 // So a refusal costs a pass over the row for the new sum (kCertain: the first at a node only), and a token a product and a sum however many were
-// refused.
-struct Refused {                          // tokens refused at this node, each once
+// refused.  kDistinct keeps the refused tokens in a list, kCertain those of all the node's children, and the passes leave the listed ones out: they
+// may be all but 1e-20 of the sum (a sure drafter's likeliest token), so that the rest is added up by itself and never found by subtraction.
+struct List {                             // each token once
   int32_t token[OPW_TREE_MAX_NODES];
-  float p[OPW_TREE_MAX_NODES], q[OPW_TREE_MAX_NODES];
-  double r[OPW_TREE_MAX_NODES];           // what is left of them
+  double r[OPW_TREE_MAX_NODES];           // its R
 };
 template <Draw kDraw>
 __device__ __forceinline__ double left_of(float p, float q, double a) {
@@ -95,10 +95,10 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ int32_t token_s[OPW_TREE_MAX_NODES], parent_s[OPW_TREE_MAX_NODES];
   __shared__ float u_s[OPW_TREE_MAX_NODES], p_s[OPW_TREE_MAX_NODES], q_s[OPW_TREE_MAX_NODES];
-  __shared__ Refused refused;
+  __shared__ List list;
   __shared__ double sum_s[kWarps], rest_s[kWarps], part_s[kMaxCluster + kWarps];
   __shared__ double2 total_s[2];          // of the block: sums of R (of all tokens by the formula) and of q; two in turn
-  __shared__ int32_t pick_s, some_s;
+  __shared__ int32_t pick_s, some_s, listed_s;
   const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int b = blockIdx.x / blocks, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
   }
   __syncthreads();
 
-  int turn = 0, now = 0, took = 1, n = 0; // node, length of the path, tokens refused at this node
+  int turn = 0, now = 0, took = 1, n = 0; // node, length of the path, tokens in the list (0 until a refusal)
   const T* prow = target;
   const T* qrow = draft;
   bool wide = false;                      // the two rows' 16-byte words begin at the same tokens
@@ -158,10 +158,17 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
   auto begin_of = [&](int block, int w) { // of a warp's part of the row
     return (int)(steps * ((int64_t)block * kWarps + w) / ((int64_t)blocks * kWarps) * kStep) - shift;
   };
+  int first = 0, last = -1;               // this warp's part of the node's row, once it is asked for
+  uint64_t mine = 0ull;                   // bit j: the list's token j lies in it
+  auto find_part = [&]() {
+    if (last >= first) return;
+    first = begin_of(rank, warp);
+    last = begin_of(rank, warp + 1);
+  };
   at_node(0);
-  // sums over the vocabulary by the formula: this block's warps' in sum_s, the totals of R and q
+  // sums over the vocabulary without the list, by the formula: this block's warps' in sum_s, the totals of R and q
   auto pass = [&](double a, bool needs_q) -> double2 {
-    const int first = begin_of(rank, warp), last = begin_of(rank, warp + 1);
+    find_part();
     // (four sums side by side: one would be a chain of 64-bit additions)
     double sums[4] = {0.0, 0.0, 0.0, 0.0}, rests[4] = {0.0, 0.0, 0.0, 0.0};
     auto add = [&](const Word<T>& x, const Word<T>& y, bool with_q) {
@@ -177,6 +184,21 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
         }
       }
     };
+    auto leave_out = [&](auto& x, auto& y, int v0) {              // the list's tokens of these words count as 0
+      constexpr int kWords = sizeof(x) / sizeof(Word<T>);
+      uint32_t out = 0u;                  // bit per token of this lane's words
+      for (uint64_t rest = mine; rest; rest &= rest - 1) {
+        const int e = list.token[__ffsll(rest) - 1] - v0;
+        if ((unsigned)e < (unsigned)(kWords * kStep) && e % kStep / kN == lane) out |= 1u << (e / kStep * kN + e % kN);
+      }
+      if (out) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k)
+#pragma unroll
+          for (int i = 0; i < kN; ++i)
+            if (out >> (k * kN + i) & 1u) x[k].x[i] = y[k].x[i] = T(0.f);
+      }
+    };
     auto walk = [&](auto with_q) {
       constexpr bool kQ = decltype(with_q)::value;
       const int inside = min(last, p.vocab);
@@ -188,14 +210,16 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
             x[k].load_inside(prow, v0 + k * kStep + lane * kN);
             if (kQ) y[k].load_inside(qrow, v0 + k * kStep + lane * kN);
           }
+          if (kDraw != kAgain && mine) leave_out(x, y, v0);
 #pragma unroll
           for (int k = 0; k < kDeep; ++k) add(x[k], y[k], kQ);
           v0 += kDeep * kStep;
         } else {
-          Word<T> x, y;
-          x.load(prow, v0 + lane * kN, p.vocab, wide);
-          if (kQ) y.load(qrow, v0 + lane * kN, p.vocab, wide);
-          add(x, y, kQ);
+          Word<T> x[1], y[1];
+          x[0].load(prow, v0 + lane * kN, p.vocab, wide);
+          if (kQ) y[0].load(qrow, v0 + lane * kN, p.vocab, wide);
+          if (kDraw != kAgain && mine) leave_out(x, y, v0);
+          add(x[0], y[0], kQ);
           v0 += kStep;
         }
       }
@@ -231,12 +255,17 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
     ++turn;
     return all;
   };
-  // what the list adds to the sum of the tokens [from, to) by the formula
-  auto correction = [&](double a, int from, int to) {
+  auto listed_sum = [&]() {               // of their R
+    double d = 0.0;
+#pragma unroll 1
+    for (int j = 0; j < n; ++j) d += list.r[j];
+    return d;
+  };
+  auto listed_in = [&](int from, int to) {                        // the same of the tokens in [from, to)
     double d = 0.0;
     if (kDraw != kAgain)
       for (int j = 0; j < n; ++j)
-        if (refused.token[j] >= from && refused.token[j] < to) d += refused.r[j] - left_of<kDraw>(refused.p[j], refused.q[j], a);
+        if (list.token[j] >= from && list.token[j] < to) d += list.r[j];
     return d;
   };
 
@@ -248,11 +277,11 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
     const int32_t x = token_s[i];
     int listed = -1;                      // its place in the list
     if (kDraw != kAgain && n > 0) {
-      const uint32_t lo = __ballot_sync(0xffffffffu, lane < n && refused.token[lane] == x);
-      const uint32_t hi = n > 32 ? __ballot_sync(0xffffffffu, lane + 32 < n && refused.token[(lane + 32) & 63] == x) : 0u;
+      const uint32_t lo = __ballot_sync(0xffffffffu, lane < n && list.token[lane] == x);
+      const uint32_t hi = n > 32 ? __ballot_sync(0xffffffffu, lane + 32 < n && list.token[(lane + 32) & 63] == x) : 0u;
       listed = lo ? __ffs(lo) - 1 : hi ? __ffs(hi) + 31 : -1;
     }
-    const double r = listed >= 0 ? refused.r[listed] : left_of<kDraw>(p_s[i], q_s[i], a);
+    const double r = listed >= 0 ? list.r[listed] : left_of<kDraw>(p_s[i], q_s[i], a);
     const double q = kDraw == kCertain ? 1.0 : listed >= 0 ? 0.0 : (double)fmaxf(q_s[i], 0.f);
     if ((double)u_s[i] * q * c_total < r * s_total) {
       if (lead) p.path[row0 + took] = i;
@@ -263,27 +292,66 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
       c_total = s_total = 1.0;
       at_hand = false;
       at_node(now);
+      first = 0;
+      last = -1;
+      mine = 0ull;
       continue;
     }
     const double c = c_total / s_total;
     double next = a;
     if (kDraw != kCertain) next += c;
     if (kDraw != kAgain) {
+      const double after = fmax(r - c * q, 0.0);
+      find_part();
       __syncthreads();                    // everybody has read the list
-      if (listed < 0) listed = n++;
-      if (tid == 0) {
-        refused.token[listed] = x;
-        refused.p[listed] = p_s[i];
-        refused.q[listed] = q_s[i];
-        refused.r[listed] = fmax(r - c * q, 0.0);
+      if (kDraw == kCertain && n == 0) {
+        if (warp == 0) {                  // the children's tokens, each where it comes first; this one is the first child
+          bool here = lane < t && parent_s[lane] == now, here2 = lane + 32 < t && parent_s[(lane + 32) & 63] == now;
+          const int32_t x1 = token_s[lane], x2 = token_s[(lane + 32) & 63];
+          uint32_t some = __ballot_sync(0xffffffffu, here);
+          if (here) here = __ffs(__match_any_sync(some, x1)) - 1 == lane;
+          some = __ballot_sync(0xffffffffu, here2);
+          if (here2) here2 = __ffs(__match_any_sync(some, x2)) - 1 == lane;
+          const uint32_t lo = __ballot_sync(0xffffffffu, here), before = (1u << lane) - 1u;
+          if (t > 32)
+            for (uint32_t rest = lo; rest; rest &= rest - 1)
+              if (__shfl_sync(0xffffffffu, x1, __ffs(rest) - 1) == x2) here2 = false;
+          const uint32_t hi = __ballot_sync(0xffffffffu, here2);
+          const int k1 = __popc(lo & before), k2 = __popc(lo) + __popc(hi & before);
+          if (here) {
+            list.token[k1] = x1;
+            list.r[k1] = lane == i ? after : (double)fmaxf(p_s[lane], 0.f);
+          }
+          if (here2) {
+            list.token[k2] = x2;
+            list.r[k2] = lane + 32 == i ? after : (double)fmaxf(p_s[lane + 32], 0.f);
+          }
+          if (lane == 0) listed_s = __popc(lo) + __popc(hi);
+        }
+        listed = 0;
+      } else {
+        if (listed < 0) {                 // (kDistinct)
+          listed = n++;
+          if (x >= first && x < last) mine |= 1ull << listed;
+        }
+        if (tid == 0) {
+          list.token[listed] = x;
+          list.r[listed] = after;
+        }
       }
       __syncthreads();
+      if (kDraw == kCertain && n == 0) {
+        n = listed_s;
+        const int32_t x1 = list.token[lane], x2 = list.token[lane + 32];
+        mine = __ballot_sync(0xffffffffu, lane < n && x1 >= first && x1 < last) |
+               (uint64_t)__ballot_sync(0xffffffffu, lane + 32 < n && x2 >= first && x2 < last) << 32;
+      }
     }
     double2 all;
     if (kDraw == kCertain && at_hand) all.x = raw;
     else all = pass(next, kDraw != kCertain);
     if (kDraw == kCertain) raw = all.x;
-    const double left = all.x + correction(next, 0, p.vocab);
+    const double left = kDraw == kAgain ? all.x : all.x + listed_sum();
     if (left > 0.0) {
       a = next;
       c_total = left;
@@ -292,26 +360,25 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
       at_hand = kDraw == kCertain;
       if (kDraw != kAgain) {
         __syncthreads();
-        if (tid == 0) refused.r[listed] = r;
+        if (tid == 0) list.r[listed] = r;
         __syncthreads();
       }
     }
     if (kDraw == kDistinct) {
       s_total = all.y;
-      for (int j = 0; j < n; ++j) s_total -= (double)fmaxf(refused.q[j], 0.f);
       if (!(s_total > 0.0)) s_total = 1.0;                        // (Q is 0 everywhere then)
     }
   }
   const bool needs_q = kDraw != kCertain && a > 0.0;
   if (!at_hand) raw = pass(a, needs_q).x;
   else if (kDraw != kCertain) raw = 0.0;
-  const double total = at_hand && kDraw != kCertain ? c_total : raw + correction(a, 0, p.vocab);
+  const double total = at_hand && kDraw != kCertain ? c_total : kDraw == kAgain ? raw : raw + listed_sum();
 
   // The token that follows: block, warp, thread, element of the first running sum above u * total; if rounding leaves none, the last
   // element that has anything.
-  if (tid < blocks) part_s[tid] = cluster.map_shared_rank(&total_s[(turn - 1) & 1], tid)->x + correction(a, begin_of(tid, 0), begin_of(tid + 1, 0));
+  if (tid < blocks) part_s[tid] = cluster.map_shared_rank(&total_s[(turn - 1) & 1], tid)->x + listed_in(begin_of(tid, 0), begin_of(tid + 1, 0));
   else if (tid >= 32 && tid < 32 + kWarps)
-    part_s[kMaxCluster + tid - 32] = sum_s[tid - 32] + correction(a, begin_of(rank, tid - 32), begin_of(rank, tid - 31));
+    part_s[kMaxCluster + tid - 32] = sum_s[tid - 32] + listed_in(begin_of(rank, tid - 32), begin_of(rank, tid - 31));
   cluster.sync();                         // (nobody leaves while its sums are read)
   const double limit = (double)fmaxf(u_s[0], 0.f) * total;
   double at = 0.0;
@@ -341,11 +408,11 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
     if (tid == 0) p.next_tokens[b] = -1;
     return;
   }
-  const int first = begin_of(rank, w), last = begin_of(rank, w + 1);
-  for (int v0 = first; v0 < last; v0 += kThreads * kN) {
+  const int begin = begin_of(rank, w), end = begin_of(rank, w + 1);
+  for (int v0 = begin; v0 < end; v0 += kThreads * kN) {
     const int v = v0 + tid * kN;
     double r[kN], sum = 0.0;
-    if (v < last) {
+    if (v < end) {
       Word<T> x, y;
       x.load(prow, v, p.vocab, wide);
       if (needs_q) y.load(qrow, v, p.vocab, wide);
@@ -353,10 +420,10 @@ __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_k
       for (int i = 0; i < kN; ++i) r[i] = left_of<kDraw>(to_float(x.x[i]), needs_q ? to_float(y.x[i]) : 0.f, a);
       if (kDraw != kAgain)
         for (int j = 0; j < n; ++j) {
-          const int e = refused.token[j] - v;
+          const int e = list.token[j] - v;
 #pragma unroll
           for (int i = 0; i < kN; ++i)
-            if (e == i) r[i] = refused.r[j];
+            if (e == i) r[i] = list.r[j];
         }
 #pragma unroll
       for (int i = 0; i < kN; ++i) sum += r[i];

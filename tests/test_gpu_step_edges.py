@@ -1,0 +1,81 @@
+"""The operators around a step's attention where they are easiest to get wrong: drafters that are sure of themselves, uniforms of 0 behind refused
+tokens, groups that are empty, lengths that are cut where no row has keys of its own, maps at the end of 32 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_14237_b200 import binding as B
+from test_gpu_step import run_verify, same_as_oracle, small_stage
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    B.build()
+    assert torch.cuda.is_available()
+
+
+# ---------------------------------------------------------------------------- verification ---
+
+def sure_drafter(rng, n, T, V, tail, kind, near):
+    """A drafter that gives all but `tail` to one token and the rest to seven others, a target that spreads over a dozen; the drafted siblings
+    are the likely ones, drawn without replacement.  `near`: all of them among the first tokens, else anywhere."""
+    target, q = np.zeros((n, T, V)), np.zeros((n, T, V))
+    tokens, parents = np.zeros((n, T), np.int64), np.zeros((n, T), np.int64)
+    parents[:, 0] = -1
+    for b in range(n):
+        pick = rng.permutation(min(V, 40) if near else V)[:16]
+        for i in range(T):
+            target[b, i, pick[:12]] = rng.dirichlet(np.ones(12))
+            q[b, i, pick[0]] = 1.0
+            q[b, i, pick[1:8]] = tail * rng.dirichlet(np.ones(7))
+        way = np.concatenate([pick[:1], rng.permutation(pick[1:8])])
+        for i in range(1, T):
+            if b % 3 == 2 and i > T // 2:                                 # (some below the first child)
+                parents[b, i] = 1
+            tokens[b, i] = way[(parents[b, :i] == parents[b, i]).sum()]
+    u = rng.random((n, T))
+    u[:, 1] = np.where(rng.random(n) < 0.8, 1 - 2.0 ** -24, u[:, 1])      # the likeliest is refused unless the target has nothing else
+    f = lambda x: torch.from_numpy(x).to(kind).cuda()  # noqa: E731
+    return f(target), f(q), tokens, parents, np.full(n, T), u
+
+
+@pytest.mark.parametrize("tail", [1e-6, 1e-13, 1e-16, 1e-17, 1e-22, 1e-30])
+@pytest.mark.parametrize("n,V,near", [(40, 40, True), (64, 4099, True), (1, 70001, False), (300, 1000, False)])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_verify_distinct_behind_a_sure_drafter(tail, n, V, near, kind):
+    """What the drafter has left once its likeliest token is refused is not lost beside it: the next sibling counts with its share of that."""
+    rng = np.random.default_rng(9000 + V)
+    st = small_stage()
+    for T in (3, 6, 9):
+        args = sure_drafter(rng, n, T, V, tail, kind, near)
+        same_as_oracle(run_verify(st, *args, distinct=True), *args, "distinct")
+    assert st.poll_error() == B.OPW_OK
+
+
+@pytest.mark.parametrize("V,batch", [(257, 200), (4099, 64), (70001, 3)])
+@pytest.mark.parametrize("draw", ["distinct", "certain"])
+def test_verify_draws_behind_parts_of_refused_tokens(V, batch, draw):
+    """Uniforms of 0 where nothing but refused tokens come first: the token that follows is the first that is left, never one of those and never
+    none, whatever the rounding of sums over them."""
+    rng = np.random.default_rng(9100 + V)
+    st, T = small_stage(), 7
+    parents = np.zeros((batch, T), np.int64)
+    parents[:, 0] = -1
+    target, q = np.zeros((batch, T, V)), np.zeros((batch, T, V))
+    tokens, u = np.zeros((batch, T), np.int64), np.full((batch, T), 1 - 2.0 ** -24)
+    u[:, 0] = 0.0
+    for b in range(batch):
+        kids = rng.permutation(min(V - 5, 200))[:T - 1]
+        small = 10.0 ** -rng.uniform(0.5, 14, size=T - 1)
+        target[b, :, kids] = np.minimum(0.4 * small / small.sum(), 0.1)[:, None]     # less than the drafter's, whose rest is 0.6 at most:
+        target[b, :, V - 3:V - 1] = 0.3                                              # refused, and left nothing
+        q[b, :, kids] = 0.9 / (T - 1)
+        q[b, :, 0] += 0.1
+        tokens[b, 1:] = kids
+    f = lambda x: torch.from_numpy(x).to(torch.float32).cuda()  # noqa: E731
+    args = (f(target), None if draw == "certain" else f(q), tokens, parents, np.full(batch, T), u)
+    got = run_verify(st, *args, distinct=draw == "distinct")
+    want = same_as_oracle(got, *args, draw)
+    assert (want[1] == 1).all() and (want[2] == V - 3).all() and st.poll_error() == B.OPW_OK
