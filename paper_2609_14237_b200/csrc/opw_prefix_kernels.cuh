@@ -89,8 +89,7 @@ __device__ __forceinline__ Span group_span(const PrefixParams& p, const GroupInf
 // One row and the keys of its own.
 __device__ __forceinline__ Span row_span(const PrefixParams& p, int32_t shared, int b) {
   const int32_t n = length_of(p, b);
-  Span s = no_span();
-  s.cut = p.lens[b] > n;
+  Span s = no_span();                        // (a length that was cut is recorded by survey_groups)
   if (n <= 0) return s;
   s.tree = 1;
   s.ctx = s.n = n;
@@ -422,10 +421,16 @@ __device__ __forceinline__ void row_body(const Problem& p, unsigned char* smem, 
   }
 }
 
-// Fills infos and starts.  Starts that do not ascend from 0 to the batch share nothing and are recorded.
+// Fills infos and starts.  Starts that do not ascend from 0 to the batch share nothing and are recorded, as are lengths beyond the table (here,
+// where a block looks at every row: there may be no block for the rows' own keys).
 __device__ __forceinline__ void survey_groups(const PrefixParams& p) {
   int32_t* first = starts_of(p);
   GroupInfo* info = infos();
+  auto length = [&](int b) {
+    const int32_t n = length_of(p, b);
+    if (blockIdx.x == 0 && p.lens[b] > n) atomicOr(p.status, kErrBadPage);
+    return n;
+  };
   // (until the last step info holds: the longest length and, inverted, its first row as one word; the shortest; the number of active rows)
   bool wrong = false;
   for (int g = threadIdx.x; g <= p.groups; g += blockDim.x) {
@@ -444,7 +449,7 @@ __device__ __forceinline__ void survey_groups(const PrefixParams& p) {
   const int lane = threadIdx.x & 31;
   for (int b0 = threadIdx.x - lane; b0 < p.batch; b0 += blockDim.x) {
     const int b = b0 + lane;
-    const int32_t n = b < p.batch ? length_of(p, b) : 0;
+    const int32_t n = b < p.batch ? length(b) : 0;
     const int g = group_of(first, p.groups, min(b, p.batch - 1));
     unsigned long long best = n > 0 ? ((unsigned long long)(uint32_t)n << 32) | (0xffffffffu - (uint32_t)b) : 0ull;
     int32_t least = n > 0 ? n : INT32_MAX, active = n > 0 ? 1 : 0;
@@ -557,7 +562,7 @@ __global__ void __launch_bounds__(PrefixSmem<D, kMode, kHigh>::kThreads, 1) pref
       mma_body<D, kMode == kPrefixWide>(map, groups, room, reinterpret_cast<int64_t*>(room + S::kTiles), blockIdx.x, group_n);
   } else {
     int64_t* cum = reinterpret_cast<int64_t*>(room + S::ring(p.stages));
-    scan_units(p, cum, WarpTree<D>::kRows, kPage, (int)blockIdx.x == group_n);
+    scan_units(p, cum, WarpTree<D>::kRows, kPage, false);
     if (!S::kMma) row_units = cum[p.all];
     if (S::kThreads == S::kWarps * 32 || threadIdx.x < S::kWarps * 32) {
       // 256 x 224 + 128 x 56 = 256 x 200 + 128 x 104 = 384 x 168
