@@ -43,16 +43,17 @@ PrefixLayout carve(const opw_stage_view& v) {
 
 // Who takes the groups: where one may have more than 16 rows (members x query heads of a kv head), the tensor cores, in blocks of up to 128 or, with
 // 512 rows a group on average, of up to 256; else, and at head_dim 256 where two accumulators would fill TMEM, the warp kernel's 16 rows.
-// How the batch is divided is known on the device only, so the largest group counts that there can be: a batch of one group of 40 and 24 single
-// rows would take the warp kernel over the shared keys ten times a kv head.  Measured, us, by the warp kernel, with 128 and with 256 rows; 32/8 heads of
-// 128 unless said:
+// How the batch is divided is known on the device only, and groups may be empty (a captured step has as many as it may ever need): the largest that
+// there can be is the whole batch.  Measured, us, by the warp kernel, with 128 and with 256 rows; 32/8 heads of 128 unless said:
 //   4 samples of 1000, 16 rows         14, 17, 18        64 behind 8k (256 rows)                  98, 45, 58
 //   8 x 4 samples behind 4k, 16 rows   46, 47, 49        64 behind 8k, 64/8 heads (512 rows)     156, 61, 57
 //   32 pairs behind 2k, 8 rows         78, 80, 88        256 behind 32k (1024 rows)             1053, 205, 182
+// What this costs a batch that shares nothing, as many groups as rows: 64 rows of 1000 to 3000 keys 94, 100; 256 rows 220, 230; 5 rows of 500
+// 14, 14; 8/2 heads of 64, 64 rows 25, 26.  Empty groups count in the average: 256 behind 32k among 255 of them is taken 128 rows at a time.
 int mode_of(const opw_stage_view& v, int batch, int groups) {
-  const int64_t G = v.Hq / v.Hkv, most = batch > groups ? batch - groups + 1 : 1;
-  if (v.D == 256 || most * G <= 16) return kPrefixWarp;
-  return batch * G < 512 * (int64_t)groups ? kPrefixNarrow : kPrefixWide;
+  const int64_t rows = (int64_t)batch * (v.Hq / v.Hkv);
+  if (v.D == 256 || rows <= 16) return kPrefixWarp;
+  return rows < 512 * (int64_t)groups ? kPrefixNarrow : kPrefixWide;
 }
 
 template <int D, int kMode, bool kHigh>

@@ -1,4 +1,4 @@
-"""Decode attention behind shared prefixes: lengths that are cut where the groups take every block."""
+"""Decode attention behind shared prefixes: groups that are empty, and lengths that are cut where the groups take every block."""
 import numpy as np
 import pytest
 import torch
@@ -14,6 +14,23 @@ pytestmark = pytest.mark.gpu
 def built():
     B.build()
     assert torch.cuda.is_available()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,members", [(32, 8, 128, 40), (8, 2, 64, 64), (16, 1, 128, 9)])
+@pytest.mark.parametrize("where", ["front", "behind", "around"])
+def test_empty_groups_change_nothing(Hq, Hkv, D, members, where):
+    """A captured step has as many groups as it may ever need: the empty ones neither change the result nor which kernel takes the others
+    (the two would differ in their last bits)."""
+    rng = np.random.default_rng(9100 + members)
+    lens = [int(700 + rng.integers(1, 200)) for _ in range(members)]
+    pool, tab, q, starts = shared_batch(rng, [members], [700], lens, Hq, Hkv, D)
+    want, want_lse, rc = run(pool, tab, q, lens, starts, [700], Hq, Hkv, D)
+    assert rc == B.OPW_OK
+    check(want, want_lse, step.decode_attention(pool, Hq, Hkv, D, q, lens, tab), 900)
+    front = {"front": members - 1, "behind": 0, "around": members // 2}[where]
+    behind = members - 1 - front
+    out, lse, rc = run(pool, tab, q, lens, [0] * (front + 1) + [members] * (behind + 1), [700] * members, Hq, Hkv, D)
+    assert rc == B.OPW_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
 @pytest.mark.parametrize("Hq,Hkv,D,members", [(8, 2, 64, 8), (8, 1, 128, 5), (16, 4, 128, 6), (32, 8, 128, 5), (6, 2, 256, 4)])
