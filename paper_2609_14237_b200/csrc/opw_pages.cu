@@ -428,9 +428,10 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
     }
     return lo;
   };
-  for (int k = gt; k < given; k += all) {                         // (requests that lack nothing lie before the one found)
-    const int f = request_of(before, k);
-    if (entry[f] >= 0) deal(p.table + (int64_t)p.rows[f] * p.max_pages + entry[f] + (k - before[f]), k);
+  // (Counters of pages and rows have no sign: the ends are below 2^31, and the next of a thread's may lie beyond it.)
+  for (uint32_t k = gt; k < (uint32_t)given; k += all) {          // (requests that lack nothing lie before the one found)
+    const int f = request_of(before, (int32_t)k);
+    if (entry[f] >= 0) deal(p.table + (int64_t)p.rows[f] * p.max_pages + entry[f] + ((int32_t)k - before[f]), k);
   }
   for (int g0 = gt - lane; g0 < n; g0 += all) {
     const int f = g0 + lane;
@@ -471,15 +472,16 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
     }
     return;
   }
-  for (int r0 = 8 * gt; r0 < p.max_rows; r0 += 8 * all) {
+  const uint32_t placed = (uint32_t)start[n], max_rows = (uint32_t)p.max_rows;
+  for (uint32_t r0 = 8 * gt; r0 < max_rows; r0 += 8 * all) {
     int32_t seq[8], slot[8];
-    int f = r0 < start[n] ? request_of(start, r0) : n;
+    int f = r0 < placed ? request_of(start, (int32_t)r0) : n;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      while (f < n && r0 + i >= start[f + 1]) ++f;
+      while (f < n && r0 + i >= (uint32_t)start[f + 1]) ++f;
       const bool live = f < n && served(f);
       seq[i] = live ? f : -1;
-      slot[i] = live ? r0 + i - start[f] : -1;
+      slot[i] = live ? (int32_t)(r0 + i) - start[f] : -1;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -487,7 +489,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
         slot[i] += p.old_lens[seq[i]];
         seq[i] = p.rows[seq[i]];
       }
-    if (wide && r0 + 8 <= p.max_rows) {
+    if (wide && r0 + 8 <= max_rows) {
 #pragma unroll
       for (int i = 0; i < 8; i += 4) {
         *reinterpret_cast<int4*>(p.seq + r0 + i) = make_int4(seq[i], seq[i + 1], seq[i + 2], seq[i + 3]);
@@ -496,7 +498,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (r0 + i < p.max_rows) {
+        if (r0 + i < max_rows) {
           p.seq[r0 + i] = seq[i];
           p.slots[r0 + i] = slot[i];
         }

@@ -79,3 +79,23 @@ def test_verify_draws_behind_parts_of_refused_tokens(V, batch, draw):
     got = run_verify(st, *args, distinct=draw == "distinct")
     want = same_as_oracle(got, *args, draw)
     assert (want[1] == 1).all() and (want[2] == V - 3).all() and st.poll_error() == B.OPW_OK
+
+
+# ---------------------------------------------------------------------------- pages for requests ---
+
+@pytest.mark.parametrize("room,off", [((1 << 31) - 1, 0), ((1 << 31) - 1, 1), ((1 << 31) - 65536 + 8, 0)])
+def test_extend_with_maps_at_the_end_of_32_bits(room, off):
+    """The largest maps there can be: a thread's next rows lie beyond 32 bits and are not written.  (Also at an odd address, word by word.)"""
+    st = small_stage(width=8)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    tab = torch.full((4, 8), -1, dtype=torch.int32, device="cuda")
+    refs, free, starts, lens = torch.zeros(40, dtype=torch.int32, device="cuda"), torch.arange(40, device="cuda").int(), i32([0] * 4), i32([0] * 3)
+    seq, slots = (torch.full((room + off,), -77, dtype=torch.int32, device="cuda") for _ in range(2))
+    st.kv_extend(i32([2, 0, 3]), i32([0, 0, 0]), i32([100, 1, 17]), tab, refs, free, i32([40]), row_starts=starts, new_lens=lens, seq=seq[off:],
+                 slots=slots[off:])
+    assert st.poll_error() == B.OPW_OK and starts.tolist() == [0, 100, 101, 118] and lens.tolist() == [100, 1, 17]
+    assert seq[off:off + 118].tolist() == [2] * 100 + [0] + [3] * 17 and slots[off:off + 118].tolist() == [*range(100), 0, *range(17)]
+    for x in (seq, slots):
+        assert (x[:off] == -77).all()
+        for lo in range(off + 118, room + off, 1 << 28):
+            assert (x[lo:lo + (1 << 28)] == -1).all()
