@@ -216,8 +216,12 @@ __global__ void __launch_bounds__(kListThreads) free_pages_kernel(const int32_t*
 //   pages dealt               the counts meet through shared memory; every block scans them
 //   table, counts, places of the rows   all threads of the cluster, a page or a row each, whose request is found by bisection
 // Nothing is written before the cluster barrier behind the counts, so no block sees a table that is half changed.  It is a chain of round
-// trips (requests, entries, list, counts) and barriers.  64 decodes 6.4 us in one block (kExtendFew requests and a row a thread at most), 7.6 in
-// eight; 1000 decodes and 24 prompts of together 31000 tokens 14 (with a warp per long request instead of a thread per page 22).
+// trips (requests, entries, list, counts) and barriers.  1000 decodes and 24 prompts of together 31000 tokens 14 us (with a warp per long request
+// instead of a thread per page 22).
+// One block instead of a cluster of eight where there are few requests and no more for a thread to do than a row, or without maps a page (what they
+// add is known on the device only; a table's whole rows is what there may be).  Us in one block and in eight, the release of the dealt pages included:
+// with maps 64 and 256 decodes 7.6, 8.7 and 8.3, 9.3; 256 requests of 32 tokens 11.4, 9.9; 8 of 1024 14.4, 9.4; without maps 64 decodes
+// 7.4, 8.5; 8, 64 and 256 prompts of 8000 tokens 27, 11, then 106, 29 and 223, 94.
 constexpr int kExtendBlocks = 8, kExtendFew = 256, kExtendThreads = 1024, kExtendMax = 8192, kExtendRows = 1 << 18;
 constexpr int kLongPages = 4;              // entries that a thread looks at by itself; beyond, its warp does
 struct ExtendParams {
@@ -463,7 +467,7 @@ __global__ void __launch_bounds__(kExtendThreads, 1) extend_kernel(const ExtendP
   }
   // eight rows in a row a thread (one where there are few): one bisection, then along the requests; what is read of them is read side by side
   const bool wide = ((uintptr_t)p.seq | (uintptr_t)p.slots) % 16 == 0;
-  if (p.max_rows <= all) {
+  if (kBlocks == 1 || p.max_rows <= all) {                        // (one block is never given more)
     if (gt < p.max_rows) {
       const int f = gt < start[n] ? request_of(start, gt) : n;
       const bool live = f < n && served(f);
@@ -668,7 +672,7 @@ extern "C" opw_status_t opw_kv_extend(opw_attn_stage_t* stage, int32_t n, const 
   opw_device_guard guard(v.device);
   if (!guard.ok()) return OPW_ERR_CUDA;
   const size_t smem = opw_pages::extend_smem(n, num_rows);
-  const bool few = n <= opw_pages::kExtendFew && max_rows <= 8 * opw_pages::kExtendThreads;
+  const bool few = n <= opw_pages::kExtendFew && (max_rows >= 0 ? max_rows : (int64_t)n * v.max_pages) <= opw_pages::kExtendThreads;
   auto launch = [&](auto kernel, int blocks) {
     if (smem > 40 * 1024) {
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
