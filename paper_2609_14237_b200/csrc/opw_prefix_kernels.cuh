@@ -103,6 +103,7 @@ __device__ __forceinline__ Span row_span(const PrefixParams& p, int32_t shared, 
 template <int kEnds_>
 struct PrefixProblem : PrefixParams {
   static constexpr int kEnds = kEnds_, kLeastPages = kEnds_ + 1;
+  static constexpr bool kMerged = true;      // it takes groups only, and all of their rows go to the merge
 };
 // What every block finds out for itself, at the beginning of its shared memory: the groups' infos, then starts.
 __device__ __forceinline__ GroupInfo* infos() {

@@ -24,6 +24,7 @@ constexpr int kMaxTreeBatch = 4096;
 struct TreeParams {
   static constexpr int kEnds = 0;        // units that a segment (entity, kv head, row block) counts for besides its tiles, in front of them
   static constexpr int kLeastPages = 4;  // units a worker has at least where they are pages
+  static constexpr bool kMerged = false; // the tensor-core kernel finishes the rows that it has seen all of
   const __nv_bfloat16* pool;
   const __nv_bfloat16* q;
   const uint64_t* mask;

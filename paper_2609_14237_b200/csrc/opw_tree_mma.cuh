@@ -659,30 +659,34 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
         c1 = c0 + D / 2;
       }
       tc_after();
-      const bool complete = s.first && s.last, finish = complete && finished_at_once(p, sp);
+      constexpr bool kMerged = Problem::kMerged;
+      const bool complete = s.first && s.last, finish = complete && !kMerged;
       const float inv = !finish ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
       float* pb = p.partials + (2 * (int64_t)block + (on_first ? 0 : 1)) * (int64_t)(C::kRows * (D + 2));
       const int64_t grow = live ? global_row(r) : 0;
-      const RowPart part = complete && !finish ? whole_row(p, sp, grow) : RowPart{pb + r * D, pb + C::kRows * D + r, pb + C::kRows * (D + 1) + r};
-      auto columns = [&](int c, uint32_t (&o)[16]) {   // 16 of this thread's row, of both slots' accumulators
-        tm_ld16(o_addr + c, o);
+      const RowPart part = complete && kMerged ? whole_row(p, sp, grow) : RowPart{pb + r * D, pb + C::kRows * D + r, pb + C::kRows * (D + 1) + r};
+      auto columns = [&](int c, auto& o) {             // of this thread's row, of both slots' accumulators
+        constexpr bool k32 = sizeof(o) == 32 * sizeof(uint32_t);
+        if constexpr (k32) tm_ld32(o_addr + c, o);
+        else tm_ld16(o_addr + c, o);
         tm_wait_ld();
         if (!s.shared) {
-          uint32_t o2[16];
-          tm_ld16(lane_addr + 256 + (x ^ 1) * 128 + c, o2);
+          uint32_t o2[k32 ? 32 : 16];
+          if constexpr (k32) tm_ld32(lane_addr + 256 + (x ^ 1) * 128 + c, o2);
+          else tm_ld16(lane_addr + 256 + (x ^ 1) * 128 + c, o2);
           tm_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale0 + __uint_as_float(o2[e]) * scale1);
+          for (int e = 0; e < (k32 ? 32 : 16); ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale0 + __uint_as_float(o2[e]) * scale1);
         }
       };
-      if (finish) {
+      if constexpr (!kMerged) {
 #pragma unroll 1
-        for (int c = c0; c < (idle ? c0 : c1); c += 16) {
-          uint32_t o[16];
+        for (int c = c0; c < c1; c += 32) {
+          uint32_t o[32];
           columns(c, o);
-          if (live) {
+          if (live && finish) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 8) {
+            for (int e = 0; e < 32; e += 8) {
               uint4 w;
               w.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
               w.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
@@ -690,12 +694,17 @@ __device__ __forceinline__ void mma_body(const CUtensorMap& map, const Problem& 
               w.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
               *reinterpret_cast<uint4*>(p.out + grow * D + c + e) = w;
             }
+          } else if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<uint4*>(part.o + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
           __syncwarp();
         }
       } else {
-        // A part of a row block.  A thread has a row, 512 bytes from the next one's: 16 columns at a time go through the warp's 2 KB of the
-        // query tile (whose products are done), so that a store takes eight whole pieces of 64 bytes and not 32 of 16.
+        // A thread has a row, 512 bytes from the next one's: 16 columns at a time go through the warp's 2 KB of the query tile (whose products
+        // are done), so that a store takes eight whole pieces of 64 bytes and not 32 of 16.  (Where everything is merged it pays; tree
+        // attention, most of whose rows are finished here, lost by it: chain of 4 11.7 -> 12.1 us, trees of 8 130.3 -> 131.3.)
         const uint32_t mine_s = qs + (uint32_t)(kWide ? warp & 3 : warp) * 2048u;
         const uint64_t at = live ? reinterpret_cast<uint64_t>(part.o) : 0ull;
 #pragma unroll 1
