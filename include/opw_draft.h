@@ -206,7 +206,8 @@ opw_status_t opw_tree_attention(opw_tree_attn_t *tree, int32_t layer, int32_t ba
  *     q_{j+1} = q_j (AGAIN), or q_j without x, divided by its sum (DISTINCT); CERTAIN: q_j is 1 at x and 0 elsewhere
  * until no child is accepted.  Then next_tokens[b] is the smallest token v with sum_{w <= v} r(w) > uniforms[b,0] * sum_w r(w), of the
  * r that is left (the last token with r > 0 where rounding leaves none; -1 if all are 0).  All of this in 64 bits, from the
- * probabilities as they are; negative ones and NaN count as 0.  Neither r_0 nor q_0 is rescaled to a sum of 1.
+ * probabilities as they are; negative ones and NaN count as 0.  Neither r_0 nor q_0 is rescaled to a sum of 1.  What refused tokens leave
+ * is summed without them (not found by subtraction), so that a q_j or r_j of 1e-20 beside a refused token of 1 still counts in full.
  *     path[b, 0 .. path_lens[b])   the accepted nodes, ascending, node 0 first: what opw_kv_commit takes; -1 behind
  * Sequences with tree_lens[b] <= 0 are inactive: path_lens 0, next_tokens -1.  tree_lens beyond nodes is cut and recorded
  * (OPW_ERR_BAD_PAGE); a node whose token is outside [0, vocab) or whose parent is not an earlier node is passed over, and recorded.

@@ -73,12 +73,13 @@ opw_status_t opw_kv_free_pages(opw_attn_stage_t *stage, const int32_t *refcounts
  * that follow), and its entries stay.  A request gets nothing
  *   - if it lacks pages, and they and those that the requests before it lack are more than the list has left: not an error;
  *   - if rows[f] < 0: not an error, the request is idle;
- *   - and is recorded, if rows[f] >= num_rows or is named by another request too, a length is negative, c + m is beyond the table, the
- *     page that holds its last c % page_size tokens is missing, one of the entries that its tokens go to names a page outside
- *     [0, num_pages) or one whose count is not 1 (its tokens would show up in other sequences), or its rows end beyond max_rows.
+ *   - and is recorded, if rows[f] >= num_rows or is named by another request too, a length is negative, c + m is beyond the table, its rows end
+ *     beyond max_rows, or (m > 0; the table is not looked at for less) the page that holds its last c % page_size tokens is missing, or one of
+ *     the entries that its tokens go to names a page outside [0, num_pages) or one whose count is not 1 (its tokens would show up in
+ *     other sequences).
  * Requests that are refused or idle take nothing from the list; those for whom it was too short come after all that were served
  * from it.  An id of the list that is out of range or not free (a list that is out of date) is not dealt: its entry stays as it
- * is, and it is recorded.
+ * is, and it is recorded.  An id that the list names twice is dealt once and recorded; which of the two entries gets it may vary.
  *   rows, old_lens, new_tokens : DEVICE int32 [n]
  *   page_table : DEVICE int32 [num_rows, max_pages_per_seq];  refcounts : DEVICE int32 [num_pages]; both changed in place
  *   free_list  : DEVICE int32 [max_list];  free_count : DEVICE int32 [1]: the list's length is min(*free_count, max_list)
@@ -87,7 +88,7 @@ opw_status_t opw_kv_free_pages(opw_attn_stage_t *stage, const int32_t *refcounts
  *   row_starts : DEVICE int32 [n + 1] or NULL; starts beyond max_rows count as max_rows
  *   new_lens   : DEVICE int32 [n] or NULL
  *   seq, slots : DEVICE int32 [max_rows]; rows behind the last request's get -1, so that a captured step may have more rows than
- *                tokens.  max_rows = -1: NULL both, no rows are placed and none is too many
+ *                tokens.  max_rows = -1: NULL both, no rows are placed, and only rows beyond INT32_MAX are too many
  * What is written must not overlap what is read, nor each other.  n <= 8192 and num_rows <= 262144 (OPW_ERR_CAPACITY).
  */
 opw_status_t opw_kv_extend(opw_attn_stage_t *stage, int32_t n, const int32_t *rows, const int32_t *old_lens, const int32_t *new_tokens,

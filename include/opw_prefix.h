@@ -44,7 +44,8 @@ opw_status_t opw_prefix_attn_destroy(opw_prefix_attn_t *prefix); /* NULL is acce
  * prefix_lens[g] / page_size entries (whole pages only), the same pages as far as their own kv_lens reach.  Only the entries of the group's
  * longest row (the first of those) are read there, on a window layer from the first key on that any row of the group sees: that row has to hold
  * them all.  A group of one row, or with a prefix of less than a page, is fine and shares nothing;
- * rows may be shorter than their group's prefix, or inactive (kv_lens <= 0: out = 0, lse = -inf).
+ * rows may be shorter than their group's prefix, or inactive (kv_lens <= 0: out = 0, lse = -inf).  A group may be empty, so that a captured step can
+ * have as many as it may ever need.
  * On a window layer each row sees the last W keys of its own, in the prefix and behind it.
  * Cached rows that a sequence does not see do not touch its result, whatever they hold (NaN and infinities included).  Scores, maxima, sums
  * and the accumulated output are fp32; the weights are rounded to bf16 for the product with V, not for the sum, as in opw_tree_attention; the

@@ -85,10 +85,12 @@ struct alignas(16) Word {
 // sums of the warps' parts say which part holds v, and its block reads that part again, a word a thread.
 // All sums are in 64 bits, so that the token does not depend on how a row is split but for differences of 1e-16.
 //
-// Measured, fp32: 64 trees of 8 over 131072 tokens 31 us (floor 7.7: 50 MB), a chain of 4 over 32000 6.5.  A pass is bound by the loads in flight
-// (four words of either row a lane, 1024 threads an SM: 5.4 TB/s over 256 sequences); what remains of the 31 us is the sequence with most
-// refusals, four passes of about 4 us one after the other, and 6 us around them.  One sum a thread instead of four: 38 us; a walk along the
-// list of refusals for each token: 109.  kDistinct takes 16 registers more (three blocks an SM instead of four).
+// Measured, fp32: a chain of 4 over 32000 tokens 6.4 us, 64 trees of 8 over 131072 30 to 31 (floor 7.7: 50 MB; bf16 26).  A pass is bound by the
+// loads in flight (four words of either row a lane, 1024 threads an SM: 5.4 TB/s over 256 sequences).  The 31 us: 18 until each of the sequences has
+// made one pass over its rows (read from HBM, 67 MB where all of them refuse; of it 6 are one sequence's launch, gather, barriers and choice of the
+// token), and 4.3 for each further pass, the rows now in L2, of the sequence that refuses most, here three.  One sum a thread instead of four: 38
+// us; a walk along the list of refusals for each token: 109.  kDistinct takes 16 registers more (three blocks an SM instead of four) and spills a few
+// where a token of the list is left out: 128 trees of 13 over 50001 in bf16 33.8 us, where the rest found by subtraction took 35.8.
 template <typename T, Draw kDraw>
 __global__ void __launch_bounds__(kThreads, kDraw == kDistinct ? 3 : 4) verify_kernel(const Params p) {
   constexpr int kN = Word<T>::kN, kStep = 32 * kN, kDeep = 4;
@@ -520,9 +522,17 @@ extern "C" opw_status_t opw_tree_verify(opw_attn_stage_t* stage, int32_t batch, 
   p.draft_stride = draft_stride;
   p.nodes = nodes;
   p.vocab = vocab;
-  // Blocks per sequence: as many as are resident at once, four an SM, and no more than give every warp four steps of a row.  fp32, us with
-  // 1, 2, 4, 8 and 16 blocks: 1 tree of 64 over 150000 tokens 91, 55, 34, 24, 20; 16 trees of 8 over 131072 108, 59, 35, 23, 19; 64 of them
-  // 128, 72, 44, 31, 37; 256 chains of 4, drafted by a rule, 48, 36, 37, 44, 77; a chain of 4 over 32000 11.4, 8.5, 6.9, 6.4, 6.6.
+  // Blocks per sequence, a power of two: as many as four an SM allow, and no more than give every warp four steps of a row in fp32, two in bf16.
+  // (Without replacement three are resident, so that 128 sequences' last blocks begin when others have ended; half as many are slower still.)
+  // Us with 1, 2, 4, 8 and 16 blocks, fp32, then bf16:
+  //   again     1 tree of 64, 150000 tokens   90, 54, 33, 24, 20     60, 38, 27, 20, 18       a chain of 4 over 32000 11.5, 8.7, 7.0, 6.5, 6.8
+  //             16 trees of 8, 131072        106, 59, 34, 23, 18     93, 52, 31, 21, 18
+  //             64 trees of 8, 131072        127, 72, 43, 31, 37    108, 60, 37, 27, 34
+  //   distinct  64 trees of 8, 131072        127, 72, 48, 39, 49    106, 61, 40, 34, 46       1 tree of 64, 150000, 48, 30, 21, 19, 17
+  //             128 trees of 13, 50001        69, 50, 38, 49, 87     57, 43, 34, 43, 75
+  //             256 chains of 4, 131072       66, 62, 57, 69, 120    48, 48, 48, 64, 115      (fp32: 62 by the rule)
+  //   certain   64 trees of 8, 131072         60, 35, 24, 19, 30     31, 20, 16, 15, 26
+  //             256 chains of 4, 131072       48, 36, 37, 44, 79     30, 24, 27, 37, 72
   int cluster = 1;
   while (cluster < opw_verify::kMaxCluster && (int64_t)batch * cluster * 2 <= 4 * s.sms && vocab > cluster * opw_verify::kWarps * 4 * 128) cluster *= 2;
   opw_device_guard guard(s.device);
