@@ -81,6 +81,41 @@ def test_verify_draws_behind_parts_of_refused_tokens(V, batch, draw):
     assert (want[1] == 1).all() and (want[2] == V - 3).all() and st.poll_error() == B.OPW_OK
 
 
+@pytest.mark.parametrize("draw", ["distinct", "certain"])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("batch,V", [(3, 1031), (2, 4099), (1, 70001)])
+def test_verify_leaves_out_tokens_wherever_they_lie(draw, kind, batch, V):
+    """Refused tokens at the ends of the row, of words, of a warp's steps and of the blocks' parts, many of them side by side; rows that begin
+    anywhere, alike and not."""
+    rng = np.random.default_rng(9300 + V)
+    st, T = small_stage(), 40
+    spots = np.unique(np.clip([0, 1, 2, 3, 4, 7, 8, 9, 15, 16, 31, 32, 63, 64, 126, 127, 128, 129, 255, 256, 257, 511, 512, 513, 514, 515, 1023, 1024, 1025,
+                               V // 2 - 1, V // 2, V // 2 + 1, 4095, 4096, V - 4, V - 3, V - 2, V - 1], 0, V - 1))
+    soft = lambda z: np.exp(z) / np.exp(z).sum(-1, keepdims=True)  # noqa: E731
+    for pad, off, off_q in ((0, 0, 0), (5, 1, 1), (3, 3, 2)):
+        x = rng.standard_normal((batch, T, V))
+        y = x + rng.standard_normal((batch, T, V))
+        x[:, :, spots] += -3.0 if draw == "distinct" else 2.0             # (refused: the drafter likes them more)
+        y[:, :, spots] += 3.0
+        tokens, parents = np.zeros((batch, T), np.int64), np.zeros((batch, T), np.int64)
+        parents[:, 0] = -1
+        for b in range(batch):
+            way = rng.permutation(spots)[:T - 1]
+            tokens[b, 1:1 + len(way)] = way
+            tokens[b, 1 + len(way):] = way[0]                             # (a token that is refused already)
+        u = np.full((batch, T), 1 - 2.0 ** -24)
+        u[:, 0] = rng.random(batch)
+        views = []
+        for z, o in ((x, off), (y, off_q)):
+            flat = torch.full((batch * T * (V + pad) + o + 64,), float("nan"), dtype=kind, device="cuda")
+            view = flat[o:o + batch * T * (V + pad)].view(batch, T, V + pad)[..., :V]
+            view.copy_(torch.from_numpy(soft(z)))
+            views.append(view)
+        args = (views[0], None if draw == "certain" else views[1], tokens, parents, np.full(batch, T), u)
+        same_as_oracle(run_verify(st, *args, distinct=draw == "distinct"), *args, draw)
+    assert st.poll_error() == B.OPW_OK
+
+
 # ---------------------------------------------------------------------------- pages for requests ---
 
 @pytest.mark.parametrize("room,off", [((1 << 31) - 1, 0), ((1 << 31) - 1, 1), ((1 << 31) - 65536 + 8, 0)])
